@@ -841,3 +841,7 @@ def clq_clps_search(X, W, Y0, block, perm=None, gamma=0.01, grid=20, workspace=N
                                 block, gamma, grid, _ptr(workspace), workspace.numel(), _ptr(alphas),
                                 _ptr(errors), _ptr(best), _stream(stream)), "clq_clps_search")
     return alphas, errors, best
+
+
+# the microscaled 4-bit operators and the expert layer (include/clq_mx4.h)
+from .mx4 import *  # noqa: E402,F401,F403

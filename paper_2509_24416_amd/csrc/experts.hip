@@ -1,0 +1,397 @@
+// Expert layer around the MX4 products: routing of tokens to experts, the plan that
+// sorts them by expert, and the weighted sum of the experts' outputs.
+//
+// Routing.  score = softmax or sigmoid of the token's logits; the experts are ranked by
+// score + bias (by the logits themselves where there is neither a bias nor groups:
+// the scores keep their order, and far from 0 round to one value).  With G groups a
+// group counts the sum of its two best ranks and only the experts of the best
+// top_groups groups take part.  The k best experts, ties to the lower index, carry
+// their scores (without the bias), divided by their sum if so asked, times a factor.
+//
+// Plan.  The assignments (token, slot) are sorted by expert, stable in their order;
+// every expert's rows start on a multiple of 32, the row unit of the products, so that
+// a grouped product is the dense one on a run of units.
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "clq_internal.h"
+#include "mx4.h"
+
+namespace clq {
+namespace {
+
+// ---- routing ---------------------------------------------------------------------------
+// One wave per token.  Lane l holds the VPL consecutive experts from l * VPL, so that
+// among equal ranks the lowest lane's first one is the lowest index.  What bounds it:
+// reading the logits, then k rounds of a wave maximum.
+constexpr int kRouteWaves = 4;
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+struct RouteArgs {
+    const void *logits;
+    MxType type;
+    int64_t ld, T;
+    int E, k, groups, top_groups;
+    bool sigmoid, renormalize;
+    const float *bias;
+    float scale;
+    int32_t *ids;
+    float *weights;
+};
+
+__device__ __forceinline__ float load_logit(const RouteArgs &a, int64_t i) {
+    if (a.type == MxType::F32) return static_cast<const float *>(a.logits)[i];
+    const uint16_t h = static_cast<const uint16_t *>(a.logits)[i];
+    return a.type == MxType::BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
+}
+
+template <int VPL>
+__global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
+{
+    __shared__ float sh[kRouteWaves][VPL * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr float kNone = -INFINITY;
+    for (int64_t t0 = (int64_t)blockIdx.x * kRouteWaves; t0 < a.T; t0 += (int64_t)gridDim.x * kRouteWaves) {
+        const int64_t t = t0 + wave;
+        if (t >= a.T) return;   // (no workgroup barrier below)
+        float x[VPL], score[VPL], rank[VPL];
+        bool open[VPL];   // may be chosen
+        bool nan = false;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+            const int e = lane * VPL + v;
+            open[v] = e < a.E;
+            x[v] = open[v] ? load_logit(a, t * a.ld + e) : kNone;
+            nan |= x[v] != x[v];
+        }
+        // a NaN leaves the token's weights NaN and ranks last
+        nan = __any(nan);
+        if (a.sigmoid) {
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) score[v] = 1.0f / (1.0f + expf(-x[v]));
+        } else {
+            float m = kNone;
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) m = fmaxf(m, x[v]);
+            m = wave_max(m);
+            // (the sum in 64 bits, so that the rounded sum does not depend on the order)
+            double s = 0.0;
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) {
+                score[v] = m == kNone ? 0.0f : expf(x[v] - m);
+                if (open[v]) s += (double)score[v];
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+            const float sum = m == kNone ? 1.0f : (float)s;
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) score[v] = score[v] / sum;
+        }
+        const bool by_logit = a.bias == nullptr && a.groups == 1;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+            const int e = lane * VPL + v;
+            float r = by_logit ? x[v] : a.bias ? score[v] + (open[v] ? a.bias[e] : 0.0f) : score[v];
+            rank[v] = r == r ? r : kNone;
+        }
+        if (a.groups > 1) {
+            // the two best of each group: lanes take groups in turn
+            const int gs = a.E / a.groups;
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) sh[wave][lane * VPL + v] = rank[v];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            float best = kNone;
+            if (lane < a.groups) {
+                float b0 = kNone, b1 = kNone;
+                for (int i = 0; i < gs; ++i) {
+                    const float r = sh[wave][lane * gs + i];
+                    b1 = fmaxf(b1, fminf(b0, r));
+                    b0 = fmaxf(b0, r);
+                }
+                best = gs > 1 ? b0 + b1 : b0;
+                if (best != best) best = kNone;   // (biases of both infinities)
+            }
+            // a group is kept if fewer than top_groups groups come before it
+            int before = 0;
+            for (int g = 0; g < a.groups; ++g) {
+                const float o = __shfl(best, g);
+                before += o > best || (o == best && g < lane);
+            }
+            const uint64_t kept = __ballot(lane < a.groups && before < a.top_groups);
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) {
+                const int e = lane * VPL + v;
+                if (e < a.E) open[v] = (kept >> (e / gs)) & 1;
+            }
+        }
+        // k rounds: the best open rank, its lowest index
+        int my_id = 0;
+        float my_w = 0.0f, total = 0.0f;
+        for (int j = 0; j < a.k; ++j) {
+            float m = kNone;
+            bool any = false;
+#pragma unroll
+            for (int v = 0; v < VPL; ++v)
+                if (open[v]) {
+                    m = fmaxf(m, rank[v]);
+                    any = true;
+                }
+            const float top = wave_max(m);
+            const uint64_t has = __ballot(any && m == top);
+            const int from = __ffsll((unsigned long long)has) - 1;
+            int id = 0;
+            float w = 0.0f;
+            bool found = false;
+#pragma unroll
+            for (int v = 0; v < VPL; ++v)
+                if (!found && open[v] && rank[v] == top) {
+                    found = true;
+                    id = lane * VPL + v;
+                    w = score[v];
+                    if (lane == from) open[v] = false;
+                }
+            id = __shfl(id, from);
+            w = __shfl(w, from);
+            total += w;
+            if (lane == j) {
+                my_id = id;
+                my_w = w;
+            }
+        }
+        // (a total of 0, where every score is, leaves weights of 0)
+        if (a.renormalize) my_w = total > 0.0f ? my_w / total : total == 0.0f ? 0.0f : total;
+        my_w *= a.scale;
+        if (nan) my_w = __uint_as_float(0x7fc00000u);
+        if (lane < a.k) {
+            a.ids[t * a.k + lane] = my_id;
+            a.weights[t * a.k + lane] = my_w;
+        }
+    }
+}
+
+// ---- plan ---------------------------------------------------------------------------------
+// A stable counting sort.  A block owns a run of kPlanRun assignments; the first kernel
+// counts its experts, the second adds the counts of the runs before (every block for
+// itself: they are a few hundred rows of E counts), and places its own.  Up to one run
+// is a single launch.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kPlanPer = 4, kPlanRun = kPlanThreads * kPlanPer;
+
+__global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const int32_t *ids, int64_t n, int E, int32_t *hist)
+{
+    extern __shared__ int32_t count[];
+    for (int e = threadIdx.x; e < E; e += kPlanThreads) count[e] = 0;
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * kPlanRun;
+    for (int j = 0; j < kPlanPer; ++j) {
+        const int64_t i = i0 + j * kPlanThreads + threadIdx.x;
+        if (i < n) {
+            const int id = ids[i];
+            if (id >= 0 && id < E) atomicAdd(&count[id], 1);   // (whole numbers: any order)
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += kPlanThreads) hist[(int64_t)blockIdx.x * E + e] = count[e];
+}
+
+// hist: counts of every run (nullptr: there is one run, counted here)
+__global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t *ids, int64_t n, int k, int E, int runs,
+                                                                  const int32_t *hist, int32_t *info, int32_t *rows,
+                                                                  int32_t *source)
+{
+    extern __shared__ int32_t sm[];
+    int32_t *wcount = sm;                    // [waves][E]: then the wave's next row of each expert
+    int32_t *all = wcount + kPlanWaves * E;  // [E] counts over all runs
+    int32_t *first = all + E;                // [E + 1] first row unit
+    int32_t *prior = first + E + 1;          // [E] counts of the runs before
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool lead = blockIdx.x == 0;
+    for (int i = tid; i < kPlanWaves * E; i += kPlanThreads) wcount[i] = 0;
+    for (int i = tid; i < E; i += kPlanThreads) all[i] = prior[i] = 0;
+    __syncthreads();
+    // a wave owns 64 * kPlanPer consecutive assignments
+    const int64_t i0 = (int64_t)blockIdx.x * kPlanRun + wave * 64 * kPlanPer;
+    int id[kPlanPer];
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j) {
+        const int64_t i = i0 + j * 64 + lane;
+        id[j] = i < n ? ids[i] : -1;
+        if (id[j] < 0 || id[j] >= E) id[j] = -1;
+        if (id[j] >= 0) atomicAdd(&wcount[wave * E + id[j]], 1);
+    }
+    if (hist)
+        for (int i = tid; i < runs * E; i += kPlanThreads) {
+            const int c = hist[i];
+            if (c) {
+                atomicAdd(&all[i % E], c);
+                if (i / E < (int)blockIdx.x) atomicAdd(&prior[i % E], c);
+            }
+        }
+    __syncthreads();
+    // per expert: the waves' first ranks
+    for (int e = tid; e < E; e += kPlanThreads) {
+        int sum = prior[e];
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const int c = wcount[w * E + e];
+            wcount[w * E + e] = sum;
+            sum += c;
+        }
+        if (!hist) all[e] = sum;
+    }
+    __syncthreads();
+    // per expert: first row units and, for the products, first tiles of 2, 4 and 8 units
+    if (wave < kPlanTables) {
+        int32_t *table = info + plan_table_offset(E, wave);
+        int run = 0;
+        for (int e0 = 0; e0 < E; e0 += 64) {
+            const int e = e0 + lane;
+            const int units = e < E ? (all[e] + 31) >> 5 : 0;
+            const int v = (units + (1 << wave) - 1) >> wave;
+            int s = v;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int t = __shfl_up(s, o);
+                if (lane >= o) s += t;
+            }
+            if (e < E) {
+                if (lead) table[e] = run + s - v;
+                if (wave == 0) first[e] = run + s - v;
+            }
+            run += __shfl(s, 63);
+        }
+        if (lane == 0) {
+            if (lead) table[E] = run;
+            if (wave == 0) first[E] = run;
+        }
+    }
+    if (lead)
+        for (int e = tid; e < E; e += kPlanThreads) info[e] = all[e];
+    __syncthreads();
+    // place: 64 assignments at a time, in order
+#pragma unroll
+    for (int j = 0; j < kPlanPer; ++j) {
+        const int64_t i = i0 + j * 64 + lane;
+        // lanes with the same expert
+        uint64_t same = __ballot(id[j] >= 0);
+        for (int b = 0; (1 << b) < E; ++b) {
+            const bool bit = id[j] >= 0 && (id[j] >> b & 1);
+            const uint64_t m = __ballot(bit);
+            same &= bit ? m : ~m;
+        }
+        int row = -1;
+        if (id[j] >= 0) {
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            const int base = wcount[wave * E + id[j]];
+            row = first[id[j]] * 32 + base + rank;
+            source[row] = (int)(i / k);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        // the lowest lane of each expert moves its count on
+        if (id[j] >= 0 && (same & ((1ull << lane) - 1)) == 0) wcount[wave * E + id[j]] += __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (i < n) rows[i] = row;
+    }
+    // rows that pad an expert's last unit have no source
+    if (lead)
+        for (int i = tid; i < E * 32; i += kPlanThreads) {
+            const int e = i >> 5, r = first[e] * 32 + all[e] + (i & 31);
+            if (r < first[e + 1] * 32) source[r] = -1;
+        }
+}
+
+// ---- combination ------------------------------------------------------------------------------
+// out[t] = sum over the slots, in order and in fp32, of weight * Y[row]; a slot without
+// a row adds nothing.  Eight columns per thread.
+template <class T, bool VEC>
+__global__ void __launch_bounds__(256) combine_kernel(const T *Y, int64_t ldy, const int32_t *rows, const float *weights,
+                                                      int64_t tokens, int k, int64_t N, int64_t plan_rows, T *out,
+                                                      int64_t ldo)
+{
+    const int64_t per = VEC ? N / 8 : N, total = tokens * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / per, c = (i - t * per) * (VEC ? 8 : 1);
+        constexpr int W = VEC ? 8 : 1;
+        float s[W] = {};
+        for (int j = 0; j < k; ++j) {
+            const int r = rows[t * k + j];
+            if (r < 0 || r >= plan_rows) continue;
+            const float w = weights[t * k + j];
+            T v[W];
+            if constexpr (VEC) *reinterpret_cast<uint4 *>(v) = *reinterpret_cast<const uint4 *>(Y + r * ldy + c);
+            else v[0] = Y[r * ldy + c];
+#pragma unroll
+            for (int e = 0; e < W; ++e) s[e] = __builtin_fmaf(w, (float)v[e], s[e]);
+        }
+        T o[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) o[e] = (T)s[e];
+        if constexpr (VEC) *reinterpret_cast<uint4 *>(out + t * ldo + c) = *reinterpret_cast<uint4 *>(o);
+        else out[t * ldo + c] = o[0];
+    }
+}
+
+template <class T>
+void launch_combine(const void *Y, int64_t ldy, const int32_t *rows, const float *weights, int64_t tokens, int k,
+                    int64_t N, int64_t plan_rows, void *out, int64_t ldo, hipStream_t stream) {
+    const bool vec = N % 8 == 0;
+    const int64_t want = (tokens * (vec ? N / 8 : N) + 255) / 256;
+    const dim3 grid((unsigned)(want < (1 << 20) ? want : 1 << 20)), block(256);
+    if (vec)
+        hipLaunchKernelGGL((combine_kernel<T, true>), grid, block, 0, stream, static_cast<const T *>(Y), ldy, rows,
+                           weights, tokens, k, N, plan_rows, static_cast<T *>(out), ldo);
+    else
+        hipLaunchKernelGGL((combine_kernel<T, false>), grid, block, 0, stream, static_cast<const T *>(Y), ldy, rows,
+                           weights, tokens, k, N, plan_rows, static_cast<T *>(out), ldo);
+}
+
+}  // namespace
+
+hipError_t launch_expert_route(const void *logits, MxType type, int64_t ld, int64_t T, int E, int k, bool sigmoid,
+                               const float *bias, int groups, int top_groups, bool renormalize, float scale,
+                               int32_t *ids, float *weights, hipStream_t stream) {
+    const RouteArgs a = {logits, type, ld, T, E, k, groups, top_groups, sigmoid, renormalize, bias, scale, ids, weights};
+    const int64_t want = (T + kRouteWaves - 1) / kRouteWaves;
+    const dim3 grid((unsigned)(want < (1 << 20) ? want : 1 << 20)), block(64 * kRouteWaves);
+    if (E <= 64) hipLaunchKernelGGL((route_kernel<1>), grid, block, 0, stream, a);
+    else if (E <= 128) hipLaunchKernelGGL((route_kernel<2>), grid, block, 0, stream, a);
+    else if (E <= 256) hipLaunchKernelGGL((route_kernel<4>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((route_kernel<8>), grid, block, 0, stream, a);   // (512 at most)
+    return hipGetLastError();
+}
+
+size_t expert_plan_workspace_bytes(int64_t n, int64_t E) {
+    const int64_t runs = (n + kPlanRun - 1) / kPlanRun;
+    return runs > 1 ? (size_t)(runs * E) * sizeof(int32_t) : 0;
+}
+
+hipError_t launch_expert_plan(const int32_t *ids, int64_t n, int k, int E, int32_t *info, int32_t *rows,
+                              int32_t *source, void *workspace, hipStream_t stream) {
+    const int runs = (int)((n + kPlanRun - 1) / kPlanRun);
+    int32_t *hist = runs > 1 ? static_cast<int32_t *>(workspace) : nullptr;
+    if (hist) {
+        hipLaunchKernelGGL(plan_count_kernel, dim3((unsigned)runs), dim3(kPlanThreads), E * sizeof(int32_t), stream, ids,
+                           n, E, hist);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const size_t lds = ((size_t)(kPlanWaves + 3) * E + 1) * sizeof(int32_t);
+    hipLaunchKernelGGL(plan_place_kernel, dim3((unsigned)runs), dim3(kPlanThreads), lds, stream, ids, n, k, E, runs, hist,
+                       info, rows, source);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_combine(const void *Y, MxType type, int64_t ldy, const int32_t *rows, const float *weights,
+                                 int64_t T, int k, int64_t N, int64_t plan_rows, void *out, int64_t ldo,
+                                 hipStream_t stream) {
+    if (type == MxType::BF16)
+        launch_combine<__bf16>(Y, ldy, rows, weights, T, k, N, plan_rows, out, ldo, stream);
+    else launch_combine<_Float16>(Y, ldy, rows, weights, T, k, N, plan_rows, out, ldo, stream);
+    return hipGetLastError();
+}
+
+}  // namespace clq

@@ -1,0 +1,58 @@
+"""An expert MLP on the MX4 products, optionally replayed as one HIP graph.
+
+A transformer block's MLP with `experts` experts of which each token takes top_k:
+
+    ids, weights = route(x . W_router^T)
+    y = sum over the token's experts of weight * (act(x . W1^T + b1) . W2^T + b2)
+
+All products but the router's (a T x experts one, left in fp32) run on MX4 codes with the
+paper's block-Hadamard rotation (CLQ, arXiv 2509.24416, Sec. 3.3) in front of both layers'
+quantizers; the activation, the second rotation and quantizer are part of the first product's
+launch.  Tokens are sorted by expert on the GPU, so nothing waits for the host, and a captured
+graph replays with other tokens, experts and tile counts.
+"""
+import torch
+
+from . import (clq_expert_combine, clq_expert_plan, clq_expert_route, clq_mx4_dispatch, clq_mx4_experts,
+               clq_mx4_experts_mx4, clq_mx4_quantize_weights)
+
+
+class ExpertMLP:
+    """router: [experts, hidden]; w1: [experts, mlp, hidden] (swiglu: 2 * mlp rows, the gates
+    first), b1: [experts, rows of w1]; w2: [experts, hidden, mlp], b2: [experts, hidden]; fp16 or
+    bf16 device tensors, biases of the inputs' type or None.  block: Hadamard block size of both
+    layers (swiglu: 64 at most).  route: further arguments of clq_expert_route."""
+
+    def __init__(self, router, w1, b1, w2, b2, top_k, act="gelu", block=64, **route):
+        self.router = router.float()
+        self.experts, self.top_k, self.act, self.block, self.route = router.shape[0], top_k, act, block, route
+        # weights are rotated and quantized once
+        self.w1 = clq_mx4_quantize_weights(w1, block, gated=act == "swiglu")
+        self.w2 = clq_mx4_quantize_weights(w2, block)
+        self.b1, self.b2 = b1, b2
+        self.graph = None
+
+    def forward(self, x):
+        """x: fp16 or bf16 [tokens, hidden] -> the same shape and type."""
+        ids, weights = clq_expert_route(x.float() @ self.router.t(), self.top_k, **self.route)
+        plan = clq_expert_plan(ids, self.experts)
+        q = clq_mx4_dispatch(x, plan, self.block)
+        h = clq_mx4_experts_mx4(q, plan, self.w1, self.b1, act=self.act, block=self.block)
+        y = clq_mx4_experts(h, plan, self.w2, self.b2, dtype=x.dtype)
+        return clq_expert_combine(y, plan, weights)
+
+    def capture(self, tokens, dtype=torch.float16):
+        """Captures forward for `tokens` tokens as one graph."""
+        dev = self.router.device
+        self.x_in = torch.zeros(tokens, self.router.shape[1], dtype=dtype, device=dev)
+        self.forward(self.x_in)   # every kernel loaded first
+        torch.cuda.synchronize(dev)
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self.x_out = self.forward(self.x_in)
+        return self.graph
+
+    def replay(self, x):
+        self.x_in.copy_(x)
+        self.graph.replay()
+        return self.x_out
