@@ -18,7 +18,6 @@ namespace clq {
 namespace {
 namespace mx {
 
-using tg::dma16;
 using tg::IC;
 using tg::lds_addr;
 using tg::read16;
@@ -43,6 +42,19 @@ struct Args {
     int oK;   // channels of the MX4 output
 };
 
+// Buffer transfers into LDS of 16 and 4 bytes a lane from byte `lane_off` + `off` of a
+// buffer: the compiler counts them among the loads in flight, where behind a transfer
+// by a global address it waits for all of them ahead of every loaded register's use.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const uint8_t *p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, (int)bytes, 0x00027000);
+}
+__device__ __forceinline__ void dma16(Buffer b, uint32_t lane_off, uint32_t off, uint32_t dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (CLQ_LDS void *)(size_t)dst, 16, (int)lane_off, (int)off, 0, 0);
+}
+__device__ __forceinline__ void dma4(Buffer b, uint32_t lane_off, uint32_t off, uint32_t dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (CLQ_LDS void *)(size_t)dst, 4, (int)lane_off, (int)off, 0, 0);
+}
 template <int OFF>
 __device__ __forceinline__ uint32_t read4(uint32_t addr) {
     uint32_t v;
@@ -62,8 +74,9 @@ __device__ __forceinline__ float widen(uint16_t h, bool bf16) {
     return bf16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
 }
 // two outputs, rounded to nearest even
-__device__ __forceinline__ uint32_t narrow2(float a, float b, bool bf16) {
-    if (bf16) {
+template <bool BF16>
+__device__ __forceinline__ uint32_t narrow2(float a, float b) {
+    if constexpr (BF16) {
         typedef __bf16 b2 __attribute__((ext_vector_type(2)));
         const b2 v = {(__bf16)a, (__bf16)b};
         return __builtin_bit_cast(uint32_t, v);
@@ -112,40 +125,36 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 }
 
 // ---- the tile kernel ---------------------------------------------------------------
-// A workgroup of WM waves computes 128 channels x 64 WM tokens, each wave 128 channels x
-// 64 tokens (4 x 2 fragments of 32 x 32).  A k-stage is 64 codes, one matrix
-// instruction per fragment.  Units go global -> LDS without registers through a ring of
-// NS stages; a wave reads a stage's units back one stage ahead of its use.  The scale
-// dwords of four stages (a quad) come the same way through a ring of two, read into
-// registers at the end of the quad before.
+// A workgroup of 4 waves computes 128 channels x 256 tokens, each wave 128 channels x 64
+// tokens (4 x 2 fragments of 32 x 32).  A k-stage is 64 codes, one matrix instruction per
+// fragment.  The channel units are shared by the waves: they go global -> LDS without
+// registers through a ring of NS stages, and a wave reads a stage's units back one stage
+// ahead of its use.  The token units belong to one wave each and go straight to registers,
+// kDepth stages ahead (through LDS the reads and writes of both operands came to 144 of
+// its 128 bytes a clock at full rate).  The scale dwords of four stages (a quad) take the
+// same two ways, the channels' through a ring of two, read at the end of the quad before.
 //
-// Ring protocol: iteration s waits until stage s + 1 has landed (transfers complete in
-// issue order: at most the later stages' may be outstanding) and its own LDS reads of
-// stage s are in, then the workgroup barrier: every wave holds stage s in registers, so
-// its slot is refilled with stage s + NS.  Quad q's scale slot is likewise free after
-// the barrier of the quad's first iteration and refilled there with quad q + 2, needed
-// at the end of quad q + 1.  Transfers past the end repeat the last stage or quad, so
-// the wait counts stay constant.
-template <int WM_, int NS_>
-struct Cfg {
-    static constexpr int WM = WM_, NS = NS_, NT = WM * 64, BN = 128, BM = WM * 64;
-    static constexpr int UNITS = 4 + 2 * WM, STAGE = UNITS * kMxUnit;
-    static constexpr int PPW = UNITS / WM;                 // transfers per wave and stage
-    static constexpr int SQ = UNITS * kMxScaleRow;         // scale bytes of a quad
-    static constexpr int SPIECES = (UNITS + 3) / 4;        // transfers of four units' scales
-    static_assert(UNITS % WM == 0 && UNITS % 4 == 0, "transfers split evenly");
-};
+// Ring protocol: iteration s waits until stage s + 1 has landed (transfers and loads
+// complete in issue order: at most the later stages' may be outstanding) and its own LDS
+// reads of stage s are in, then the workgroup barrier: every wave holds stage s in
+// registers, so its slot is refilled with stage s + NS.  Quad q's scale slot is likewise
+// free after the barrier of the quad's first iteration and refilled there with quad q + 2,
+// needed at the end of quad q + 1.  Transfers past the end repeat the last stage or quad,
+// so the wait counts stay constant.
+constexpr int kWaves = 4, kThreads = kWaves * 64, kBN = 128, kBM = 256;
+constexpr int kStages = 5;                      // ring of channel units
+constexpr int kStageBytes = 4 * kMxUnit;        // one unit transferred by each wave
+constexpr int kQuadBytes = 4 * kMxScaleRow;
+constexpr int kDepth = 4;                       // stages of token units in registers
 
 struct Operands {
-    v4u w[4], x[2];
-    __device__ __forceinline__ void read(uint32_t wa, uint32_t xa, int lane) {
-        const uint32_t wl = wa + lane * 16, xl = xa + lane * 16;
-        static_for<0, 4>([&](auto f) { w[f] = read16<decltype(f)::value * kMxUnit>(wl); });
-        static_for<0, 2>([&](auto f) { x[f] = read16<decltype(f)::value * kMxUnit>(xl); });
+    v4u w[4];
+    __device__ __forceinline__ void read(uint32_t wa) {
+        static_for<0, 4>([&](auto f) { w[f] = read16<decltype(f)::value * kMxUnit>(wa); });
     }
 };
 struct Scales {
-    uint32_t s[6];   // four channel units, two token units
+    uint32_t s[4];
 };
 // At most VM transfers outstanding, the LDS reads in, the workgroup barrier.  The
 // destinations of those reads are named, so that nothing touches them before; a
@@ -155,16 +164,13 @@ struct Scales {
 #define CLQ_MX_WAIT "s_waitcnt vmcnt(%c[vm]) lgkmcnt(0)\n\ts_barrier"
 template <int VM>
 __device__ __forceinline__ void wait_stage(Operands &o) {
-    asm volatile(CLQ_MX_WAIT
-                 : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(o.w[3]), "+v"(o.x[0]), "+v"(o.x[1])
-                 : [vm] "n"(VM)
-                 : "memory");
+    asm volatile(CLQ_MX_WAIT : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(o.w[3]) : [vm] "n"(VM) : "memory");
 }
 template <int VM>
 __device__ __forceinline__ void wait_stage(Operands &o, Scales &s) {
     asm volatile(CLQ_MX_WAIT
-                 : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(o.w[3]), "+v"(o.x[0]), "+v"(o.x[1]), "+v"(s.s[0]),
-                   "+v"(s.s[1]), "+v"(s.s[2]), "+v"(s.s[3]), "+v"(s.s[4]), "+v"(s.s[5])
+                 : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(o.w[3]), "+v"(s.s[0]), "+v"(s.s[1]), "+v"(s.s[2]),
+                   "+v"(s.s[3])
                  : [vm] "n"(VM)
                  : "memory");
 }
@@ -181,11 +187,11 @@ __device__ __forceinline__ int bias_index(int n, int N, bool gated) {
 }
 
 // Stores the plain outputs of a fragment: the lane's 16 channels n0 .. of row m.
-template <bool RAGGED>
+template <bool RAGGED, bool BF16>
 __device__ __forceinline__ void store_plain(const Args &a, const v16f &x, const float *bias, int64_t m, int n0) {
     uint32_t h[8];
 #pragma unroll
-    for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2(x[v] + bias[v], x[v + 1] + bias[v + 1], a.out_bf16);
+    for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2<BF16>(x[v] + bias[v], x[v + 1] + bias[v + 1]);
     uint16_t *dst = a.Y + m * a.ldy + n0;
     if (!RAGGED || n0 <= a.N - 16) {
         reinterpret_cast<v4u *>(dst)[0] = v4u{h[0], h[1], h[2], h[3]};
@@ -198,13 +204,18 @@ __device__ __forceinline__ void store_plain(const Args &a, const v16f &x, const 
 }
 
 // Rotates and quantizes NF fragments of one 32-row unit: f[i][v] is channel
-// 32 i + 16 (lane / 32) + v (of the output) of row lane % 32.  Stage h = 16 pairs
-// the lane halves, 32 and 64 the fragments.  Writes the chunks c0 .. c0 + NF - 1 of unit u.
+// 32 i + 16 (lane / 32) + v (of the output) of row lane % 32.  Writes the chunks
+// c0 .. c0 + NF - 1 of unit u.
+//
+// Stages h = 1 .. 8 stay in the lane, 32 and 64 pair fragments.  Stage 16 pairs the lane
+// halves: one exchange of two registers, v and v + 8, leaves the lower lanes with both
+// halves' values of v and the upper ones with those of v + 8, so that a sum and a
+// difference finish two channels on every lane.  The lane then holds channels 8 h' .. + 7 and
+// 16 + 8 h' .. + 7 of each fragment (h' = lane / 32): two whole dwords of codes.
 template <int B, int NF>
 __device__ __forceinline__ void requantize(const Args &a, float (&f)[NF][16], int lane, int64_t u, int c0) {
     const int h = lane >> 5, row = lane & 31, oK = a.oK;
     if constexpr (B >= 32) {
-        const float sg = h ? -1.0f : 1.0f;
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
 #pragma unroll
@@ -217,15 +228,16 @@ __device__ __forceinline__ void requantize(const Args &a, float (&f)[NF][16], in
                         f[i][v + st] = p - q;
                     }
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const uint32_t b = __float_as_uint(f[i][v]);
-                const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-                // lower half's value + or - upper half's (the product with 1 is exact)
-                f[i][v] = __builtin_fmaf(__uint_as_float(r[1]), sg, __uint_as_float(r[0]));
+            for (int v = 0; v < 8; ++v) {
+                const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(f[i][v]), __float_as_uint(f[i][v + 8]),
+                                                                false, false);
+                const float p = __uint_as_float(r[0]), q = __uint_as_float(r[1]);
+                f[i][v] = p + q;
+                f[i][v + 8] = p - q;
             }
         }
         if constexpr (B >= 64) {
-            static_assert(B < 64 || NF >= 2, "fragments of a rotation block");
+            static_assert(B < 64 || NF >= B / 32, "fragments of a rotation block");
 #pragma unroll
             for (int st = 1; st < B / 32; st <<= 1)
 #pragma unroll
@@ -243,39 +255,41 @@ __device__ __forceinline__ void requantize(const Args &a, float (&f)[NF][16], in
     v2u codes[NF];
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
-        float m = 0.0f;
+        float m0 = 0.0f, m1 = 0.0f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) m = __builtin_elementwise_maximum(m, fabsf(f[i][v]));
-        const uint32_t b = __float_as_uint(m);
+        for (int v = 0; v < 16; v += 4) {
+            m0 = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m0, fabsf(f[i][v])), fabsf(f[i][v + 1]));
+            m1 = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m1, fabsf(f[i][v + 2])), fabsf(f[i][v + 3]));
+        }
+        const uint32_t b = __float_as_uint(__builtin_elementwise_maximum(m0, m1));
         const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-        m = __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        const float m = __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
         byte[i] = mx_scale_byte(__float_as_uint(m) & 0x7fffffffu, 0);
         const float s = mx_scale_value(byte[i], 0);
         codes[i] = v2u{mx_pack8(f[i], s), mx_pack8(f[i] + 8, s)};
     }
-    // a chunk's two halves meet: lanes 0..31 take the even chunk of a pair, 32..63 the odd
+    // a chunk's halves meet: lanes 0..31 take the even chunk of a pair, 32..63 the odd
+    static_assert(NF % 2 == 0, "chunks in pairs");
 #pragma unroll
     for (int i = 0; i < NF; i += 2) {
-        if constexpr (NF >= 2) {
-            const auto lo = __builtin_amdgcn_permlane32_swap(codes[i][0], codes[i + 1][0], false, false);
-            const auto hi = __builtin_amdgcn_permlane32_swap(codes[i][1], codes[i + 1][1], false, false);
-            // lower lanes: own and the upper lanes' chunk i; upper: the lower lanes' and own chunk i + 1
-            const int c = c0 + i + h;
-            if (32 * c < oK) {
-                *reinterpret_cast<v4u *>(a.Oq + mx_code_offset(u, row, c, oK)) = v4u{lo[0], hi[0], lo[1], hi[1]};
-                a.Os[mx_scale_offset(u, row, c, oK)] = (uint8_t)(h ? byte[i + 1] : byte[i]);
-            }
+        const auto lo = __builtin_amdgcn_permlane32_swap(codes[i][0], codes[i + 1][0], false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(codes[i][1], codes[i + 1][1], false, false);
+        const int c = c0 + i + h;
+        if (32 * c < oK) {
+            *reinterpret_cast<v4u *>(a.Oq + mx_code_offset(u, row, c, oK)) =
+                B >= 32 ? v4u{lo[0], lo[1], hi[0], hi[1]} : v4u{lo[0], hi[0], lo[1], hi[1]};
+            a.Os[mx_scale_offset(u, row, c, oK)] = (uint8_t)(h ? byte[i + 1] : byte[i]);
         }
     }
 }
 
-template <class C, Out OUT, int B, bool GROUPED, bool RAGGED>
-__global__ void __launch_bounds__(C::NT, 2) mx_tile_kernel(Args a)
+template <Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+__global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
 {
-    constexpr int NS = C::NS;
+    constexpr int NS = kStages;
     constexpr bool GATED = OUT == Out::Swiglu;
-    __shared__ __align__(16) uint8_t pool[NS * C::STAGE + 2 * C::SQ];
-    __shared__ float ep[C::BN];   // biases
+    __shared__ __align__(16) uint8_t pool[NS * kStageBytes + 2 * kQuadBytes];
+    __shared__ __align__(16) float ep[kBN];   // biases
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nks = a.K >> 6, nq = (a.K + 255) >> 8;
@@ -297,96 +311,102 @@ __global__ void __launch_bounds__(C::NT, 2) mx_tile_kernel(Args a)
         tg::Args t;
         t.group_m = a.group_m; t.tiles_m = a.tiles_m; t.tiles_n = a.tiles_n;
         tg::tile_coords(t, tg::tile_of_block(), tm, tn);
-        rt.unit0 = tm * (C::BM / 32);
+        rt.unit0 = tm * (kBM / 32);
         rt.unit_end = a.xunits;
         rt.expert = 0;
     }
     const uint8_t *Wq = a.Wq + rt.expert * a.w_stride, *Ws = a.Ws + rt.expert * a.ws_stride;
 
-    // ---- producer --------------------------------------------------------------------
-    const uint32_t l16 = (uint32_t)lane * 16;
-    const uint8_t *src[C::PPW];
-    uint32_t dsto[C::PPW];
-    static_for<0, C::PPW>([&](auto ic) {
-        constexpr int i = decltype(ic)::value;
-        const int p = wave * C::PPW + i;   // channel units first
-        src[i] = p < 4 ? Wq + (int64_t)min(tn * 4 + p, a.wunits - 1) * nks * kMxUnit
-                       : a.Xq + (int64_t)min(rt.unit0 + p - 4, rt.unit_end - 1) * nks * kMxUnit;
-        dsto[i] = (uint32_t)(p * kMxUnit);
-    });
-    // scales: a transfer brings the 256 bytes of four units; waves past the last piece
-    // repeat it
-    const int sp = min(wave, C::SPIECES - 1), su = sp * 4 + (lane >> 4);
-    const uint8_t *ssrc = (su < 4 ? Ws + (int64_t)min(tn * 4 + su, a.wunits - 1) * nq * kMxScaleRow
-                                  : a.Xs + (int64_t)min(rt.unit0 + su - 4, rt.unit_end - 1) * nq * kMxScaleRow) +
-                          (lane & 15) * 16;
-    const uint32_t pool0 = lds_addr(pool), spool = pool0 + NS * C::STAGE;
+    // ---- sources: this wave's channel unit, its two token units, their scales -----------
+    const uint32_t l16 = (uint32_t)lane * 16, l4 = (uint32_t)lane * 4;
+    const int64_t wu = min(tn * 4 + wave, a.wunits - 1);
+    const Buffer wsrc = buffer_of(Wq + wu * nks * kMxUnit, (uint32_t)(nks * kMxUnit));
+    const Buffer wssrc = buffer_of(Ws + wu * nq * kMxScaleRow, (uint32_t)(nq * kMxScaleRow));
+    const uint8_t *xsrc[2], *xssrc[2];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+        const int64_t xu = min(rt.unit0 + 2 * wave + f, rt.unit_end - 1);
+        xsrc[f] = a.Xq + xu * nks * kMxUnit;
+        xssrc[f] = a.Xs + xu * nq * kMxScaleRow;
+    }
+    const uint32_t pool0 = lds_addr(pool), spool = pool0 + NS * kStageBytes;
     auto produce = [&](uint32_t slot, int k) __attribute__((always_inline)) {
-        const uint32_t off = l16 + (uint32_t)min(k, nks - 1) * kMxUnit;
-        static_for<0, C::PPW>([&](auto ic) {
-            constexpr int i = decltype(ic)::value;
-            const uint8_t *s = src[i] + off;
-            dma16(s, pool0 + slot + dsto[i]);
-        });
+        dma16(wsrc, l16, (uint32_t)min(k, nks - 1) * kMxUnit, pool0 + slot + (uint32_t)wave * kMxUnit);
     };
     auto produce_scales = [&](uint32_t slot, int q) __attribute__((always_inline)) {
-        const uint8_t *s = ssrc + (uint32_t)min(q, nq - 1) * kMxScaleRow;
-        dma16(s, spool + slot + (uint32_t)sp * 1024);
+        dma4(wssrc, l4, (uint32_t)min(q, nq - 1) * kMxScaleRow, spool + slot + (uint32_t)wave * kMxScaleRow);
+    };
+    v4u x[kDepth][2];        // token units of stages k .. k + kDepth - 1
+    uint32_t xs[2][2];       // token scales of even and odd quads
+    auto load_x = [&](auto dc, int k) __attribute__((always_inline)) {
+        const uint32_t off = l16 + (uint32_t)min(k, nks - 1) * kMxUnit;
+#pragma unroll
+        for (int f = 0; f < 2; ++f) x[decltype(dc)::value][f] = *reinterpret_cast<const v4u *>(xsrc[f] + off);
+    };
+    auto load_xs = [&](auto qc, int q) __attribute__((always_inline)) {
+        const uint32_t off = l4 + (uint32_t)min(q, nq - 1) * kMxScaleRow;
+#pragma unroll
+        for (int f = 0; f < 2; ++f) xs[decltype(qc)::value][f] = *reinterpret_cast<const uint32_t *>(xssrc[f] + off);
     };
 
     // the tile's biases, in registers until the ring is done with
     float bv = 0.0f;
-    if (a.bias && tid < C::BN) {
-        const int n = min(tn * C::BN + tid, a.N - 1);
+    if (a.bias && tid < kBN) {
+        const int n = min(tn * kBN + tid, a.N - 1);
         bv = widen(a.bias[(int64_t)rt.expert * a.N + bias_index(n, a.N, GATED)], a.bias_bf16);
     }
     __builtin_amdgcn_sched_barrier(0);
 
-    // ---- consumer --------------------------------------------------------------------
+    // ---- k loop ------------------------------------------------------------------------
     Operands op[2];
-    Scales sc[2];   // of even and odd quads
-    const uint32_t xo = (uint32_t)((4 + 2 * wave) * kMxUnit);
-    auto read_stage = [&](uint32_t slot, auto pc) __attribute__((always_inline)) {
-        op[decltype(pc)::value].read(pool0 + slot, pool0 + slot + xo, lane);
-    };
-    const uint32_t sw = spool + (uint32_t)lane * 4, sx = sw + (uint32_t)(4 + 2 * wave) * kMxScaleRow;
+    Scales sc[2];   // channel scales of even and odd quads
+    const uint32_t wl = pool0 + l16, sl = spool + l4;
     auto read_scales = [&](auto qc) __attribute__((always_inline)) {
         constexpr int Q = decltype(qc)::value;
-        static_for<0, 4>([&](auto f) { sc[Q].s[f] = read4<Q * C::SQ + decltype(f)::value * kMxScaleRow>(sw); });
-        static_for<0, 2>([&](auto f) {
-            sc[Q].s[4 + decltype(f)::value] = read4<Q * C::SQ + decltype(f)::value * kMxScaleRow>(sx);
-        });
+        static_for<0, 4>([&](auto f) { sc[Q].s[f] = read4<Q * kQuadBytes + decltype(f)::value * kMxScaleRow>(sl); });
     };
     v16f acc[4][2];
     static_for<0, 4>([&](auto i) { static_for<0, 2>([&](auto j) { acc[decltype(i)::value][decltype(j)::value] = v16f{}; }); });
 
     // prologue: two quads of scales and NS stages in flight, stage 0 and quad 0 landed
     produce_scales(0, 0);
-    produce_scales(C::SQ, 1);
-    static_for<0, NS>([&](auto qc) { produce(decltype(qc)::value * C::STAGE, decltype(qc)::value); });
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 1) * C::PPW) : "memory");
-    read_stage(0, IC<0>{});
+    produce_scales(kQuadBytes, 1);
+    load_xs(IC<0>{}, 0);
+    static_for<0, NS>([&](auto qc) {
+        constexpr int Q = decltype(qc)::value;
+        produce(Q * kStageBytes, Q);
+        if constexpr (Q < kDepth) load_x(qc, Q);
+        __builtin_amdgcn_sched_barrier(0);
+    });
+    // after stage 0's transfer: at least that of every other stage
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NS - 1 + 2 * (kDepth - 1)) : "memory");
+    op[0].read(wl);
     read_scales(IC<0>{});
     uint32_t cur = 0;
-    int k = 0, q = 2;
-    // position P of the eight stages of an even and an odd quad
+    int k = 0, q = 1;
+    // position P8 of the eight stages of an even and an odd quad
     auto stage = [&](auto pc) __attribute__((always_inline)) {
         constexpr int P8 = decltype(pc)::value, P = P8 & 3, Q = P8 >> 2, R = P & 1;
-        // outstanding: the last NS - 2 stages, and the scale transfer if a quad began among them
-        constexpr int VM = (NS - 2) * C::PPW + (P >= 1 && P <= NS - 2 ? 1 : 0);
+        // Outstanding: the last NS - 2 stages' transfer and two loads, and the three of the
+        // scales if a quad began among them.
+        constexpr int VM = (NS - 2) * 3 + (P >= 1 && P <= NS - 2 ? 3 : 0);
         if constexpr (P == 0) wait_stage<VM>(op[R], sc[Q]);
         else wait_stage<VM>(op[R]);
-        const uint32_t nxt = cur == (uint32_t)((NS - 1) * C::STAGE) ? 0u : cur + C::STAGE;
-        read_stage(nxt, IC<1 - R>{});
+        const uint32_t nxt = cur == (uint32_t)((NS - 1) * kStageBytes) ? 0u : cur + kStageBytes;
+        op[1 - R].read(wl + nxt);
         if constexpr (P == 3) read_scales(IC<1 - Q>{});
         produce(cur, k + NS);
-        if constexpr (P == 0) produce_scales(Q * C::SQ, q++);
+        if constexpr (P == 0) {
+            load_xs(IC<1 - Q>{}, q);
+            produce_scales(Q * kQuadBytes, ++q);
+        }
         static_for<0, 4>([&](auto fc) {
             static_for<0, 2>([&](auto mc) {
                 constexpr int fn = decltype(fc)::value, fm = decltype(mc)::value;
-                acc[fn][fm] = mfma_mx4<P>(op[R].w[fn], op[R].x[fm], acc[fn][fm], sc[Q].s[fn], sc[Q].s[4 + fm]);
+                acc[fn][fm] = mfma_mx4<P>(op[R].w[fn], x[P][fm], acc[fn][fm], sc[Q].s[fn], xs[Q][fm]);
             });
         });
+        load_x(IC<P>{}, k + kDepth);
         cur = nxt;
         ++k;
     };
@@ -399,7 +419,7 @@ __global__ void __launch_bounds__(C::NT, 2) mx_tile_kernel(Args a)
     // sets are named, so that no register of theirs serves another value meanwhile)
     wait_stage<0>(op[0], sc[0]);
     wait_stage<0>(op[1], sc[1]);
-    if (tid < C::BN) ep[tid] = bv;
+    if (tid < kBN) ep[tid] = bv;
     __syncthreads();
 
     // ---- epilogue: lane owns row m and 16 consecutive channels of each fragment ---------
@@ -412,8 +432,8 @@ __global__ void __launch_bounds__(C::NT, 2) mx_tile_kernel(Args a)
             const int64_t m = (int64_t)u * 32 + (lane & 31);
             static_for<0, 4>([&](auto fc) {
                 constexpr int fn = decltype(fc)::value;
-                const int c = fn * 32 + h16, n0 = tn * C::BN + c;
-                if ((GROUPED || m < a.M) && n0 < a.N) store_plain<RAGGED>(a, acc[fn][fm], ep + c, m, n0);
+                const int c = fn * 32 + h16, n0 = tn * kBN + c;
+                if ((GROUPED || m < a.M) && n0 < a.N) store_plain<RAGGED, BF16>(a, acc[fn][fm], ep + c, m, n0);
             });
         } else if constexpr (GATED) {
             float f[2][16];
@@ -439,31 +459,33 @@ __global__ void __launch_bounds__(C::NT, 2) mx_tile_kernel(Args a)
     });
 }
 
-template <class C, Out OUT, int B, bool GROUPED>
+template <Out OUT, int B, bool GROUPED>
 void launch_kernel(const Args &a, unsigned grid, hipStream_t stream) {
-    const dim3 g(grid), b(C::NT);
+    const dim3 g(grid), b(kThreads);
     if constexpr (OUT == Out::Plain) {
-        if (a.N % 16 != 0) {
-            hipLaunchKernelGGL((mx_tile_kernel<C, OUT, B, GROUPED, true>), g, b, 0, stream, a);
-            return;
-        }
+        const bool ragged = a.N % 16 != 0;
+        if (ragged && a.out_bf16) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, true, true>), g, b, 0, stream, a);
+        else if (ragged) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, true, false>), g, b, 0, stream, a);
+        else if (a.out_bf16) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, false, true>), g, b, 0, stream, a);
+        else hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, false, false>), g, b, 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, false, false>), g, b, 0, stream, a);
     }
-    hipLaunchKernelGGL((mx_tile_kernel<C, OUT, B, GROUPED, false>), g, b, 0, stream, a);
 }
 
-template <class C, bool GROUPED>
+template <bool GROUPED>
 hipError_t launch_out(Args &a, MxAct act, int block, unsigned grid, hipStream_t stream) {
     if (a.Y) {
-        launch_kernel<C, Out::Plain, 0, GROUPED>(a, grid, stream);
+        launch_kernel<Out::Plain, 0, GROUPED>(a, grid, stream);
     } else {
         auto by_block = [&](auto oc) {
             constexpr Out OUT = decltype(oc)::value;
             switch (block) {
-                case 0: launch_kernel<C, OUT, 0, GROUPED>(a, grid, stream); break;
-                case 32: launch_kernel<C, OUT, 32, GROUPED>(a, grid, stream); break;
-                case 64: launch_kernel<C, OUT, 64, GROUPED>(a, grid, stream); break;
+                case 0: launch_kernel<OUT, 0, GROUPED>(a, grid, stream); break;
+                case 32: launch_kernel<OUT, 32, GROUPED>(a, grid, stream); break;
+                case 64: launch_kernel<OUT, 64, GROUPED>(a, grid, stream); break;
                 default:
-                    if constexpr (OUT != Out::Swiglu) launch_kernel<C, OUT, 128, GROUPED>(a, grid, stream);
+                    if constexpr (OUT != Out::Swiglu) launch_kernel<OUT, 128, GROUPED>(a, grid, stream);
                     break;
             }
         };
@@ -480,7 +502,6 @@ hipError_t launch_out(Args &a, MxAct act, int block, unsigned grid, hipStream_t 
 }  // namespace
 
 hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
-    using C = mx::Cfg<4, 5>;
     mx::Args a = {};
     a.Xq = g.Xq; a.Xs = g.Xs; a.Wq = g.Wq; a.Ws = g.Ws;
     a.bias = static_cast<const uint16_t *>(g.bias);
@@ -492,7 +513,7 @@ hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
     a.wunits = (int)(padded_rows(g.N) >> 5);
     a.w_stride = (int64_t)a.wunits * (g.K >> 6) * kMxUnit;
     a.ws_stride = mx_scale_bytes(a.wunits, g.K);
-    a.tiles_n = (int)((g.N + C::BN - 1) / C::BN);
+    a.tiles_n = (int)((g.N + mx::kBN - 1) / mx::kBN);
     a.group_m = 4;
     a.info = g.info;
     a.experts = g.experts;
@@ -505,11 +526,11 @@ hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
         a.log_units = 3;
         a.xunits = (int)g.units;
         const int64_t most = g.units / 8 + (g.experts < g.units ? g.experts : g.units);
-        return mx::launch_out<C, true>(a, g.act, g.block, (unsigned)(most * a.tiles_n), stream);
+        return mx::launch_out<true>(a, g.act, g.block, (unsigned)(most * a.tiles_n), stream);
     }
     a.xunits = (int)(padded_act_rows(g.M) >> 5);
-    a.tiles_m = (int)((g.M + C::BM - 1) / C::BM);
-    return mx::launch_out<C, false>(a, g.act, g.block, (unsigned)((int64_t)a.tiles_m * a.tiles_n), stream);
+    a.tiles_m = (int)((g.M + mx::kBM - 1) / mx::kBM);
+    return mx::launch_out<false>(a, g.act, g.block, (unsigned)((int64_t)a.tiles_m * a.tiles_n), stream);
 }
 
 }  // namespace clq
