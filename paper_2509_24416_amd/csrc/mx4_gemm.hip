@@ -186,20 +186,43 @@ __device__ __forceinline__ int bias_index(int n, int N, bool gated) {
     return t < 32 ? 32 * j + t : N / 2 + 32 * j + (t - 32);
 }
 
-// Stores the plain outputs of a fragment: the lane's 16 channels n0 .. of row m.
+// Stores the plain outputs of one 32-row unit (row0 ..), 128 channels from n0.  A lane's
+// 16 channels of a row are 32 bytes of 32 different rows to a store, and the L2 takes a
+// request for each; so the wave turns the unit in its own part of LDS (rows kRowPitch bytes
+// apart, for the banks) and stores four whole 256-byte row pieces at a time.
+constexpr int kRowPitch = 272, kTurnBytes = 32 * kRowPitch;
+
 template <bool RAGGED, bool BF16>
-__device__ __forceinline__ void store_plain(const Args &a, const v16f &x, const float *bias, int64_t m, int n0) {
-    uint32_t h[8];
+__device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][2], int fm, const float *bias,
+                                            uint8_t *turn, int64_t row0, int64_t row_end, int n0, int lane) {
+    const int h16 = (lane >> 5) * 16;
+    uint8_t *w = turn + (lane & 31) * kRowPitch + h16 * 2;
 #pragma unroll
-    for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2<BF16>(x[v] + bias[v], x[v + 1] + bias[v + 1]);
-    uint16_t *dst = a.Y + m * a.ldy + n0;
-    if (!RAGGED || n0 <= a.N - 16) {
-        reinterpret_cast<v4u *>(dst)[0] = v4u{h[0], h[1], h[2], h[3]};
-        reinterpret_cast<v4u *>(dst)[1] = v4u{h[4], h[5], h[6], h[7]};
-    } else {
+    for (int fn = 0; fn < 4; ++fn) {
+        const v16f &x = acc[fn][fm];
+        const float *b = bias + fn * 32 + h16;
+        uint32_t h[8];
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-            if (n0 + v < a.N) dst[v] = (uint16_t)(h[v >> 1] >> (16 * (v & 1)));
+        for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2<BF16>(x[v] + b[v], x[v + 1] + b[v + 1]);
+        reinterpret_cast<v4u *>(w + fn * 64)[0] = v4u{h[0], h[1], h[2], h[3]};
+        reinterpret_cast<v4u *>(w + fn * 64)[1] = v4u{h[4], h[5], h[6], h[7]};
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses stay in order)
+    const int c = lane & 15, n = n0 + 8 * c;
+    if (n >= a.N) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = i * 4 + (lane >> 4);
+        const v4u v = *reinterpret_cast<const v4u *>(turn + r * kRowPitch + c * 16);
+        if (row0 + r >= row_end) break;
+        uint16_t *dst = a.Y + (row0 + r) * a.ldy + n;
+        if (!RAGGED || n <= a.N - 8) {
+            *reinterpret_cast<v4u *>(dst) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n + e < a.N) dst[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+        }
     }
 }
 
@@ -288,7 +311,8 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
 {
     constexpr int NS = kStages;
     constexpr bool GATED = OUT == Out::Swiglu;
-    __shared__ __align__(16) uint8_t pool[NS * kStageBytes + 2 * kQuadBytes];
+    constexpr int kRing = NS * kStageBytes + 2 * kQuadBytes, kTurn = OUT == Out::Plain ? kWaves * kTurnBytes : 0;
+    __shared__ __align__(16) uint8_t pool[kRing > kTurn ? kRing : kTurn];
     __shared__ __align__(16) float ep[kBN];   // biases
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -429,12 +453,8 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
         const int u = rt.unit0 + wave * 2 + fm;
         if (u >= rt.unit_end) return;
         if constexpr (OUT == Out::Plain) {
-            const int64_t m = (int64_t)u * 32 + (lane & 31);
-            static_for<0, 4>([&](auto fc) {
-                constexpr int fn = decltype(fc)::value;
-                const int c = fn * 32 + h16, n0 = tn * kBN + c;
-                if ((GROUPED || m < a.M) && n0 < a.N) store_plain<RAGGED, BF16>(a, acc[fn][fm], ep + c, m, n0);
-            });
+            const int64_t end = GROUPED ? (int64_t)rt.unit_end * 32 : a.M;
+            store_plain<RAGGED, BF16>(a, acc, fm, ep, pool + wave * kTurnBytes, (int64_t)u * 32, end, tn * kBN, lane);
         } else if constexpr (GATED) {
             float f[2][16];
             static_for<0, 2>([&](auto pc) {
@@ -463,7 +483,7 @@ template <Out OUT, int B, bool GROUPED>
 void launch_kernel(const Args &a, unsigned grid, hipStream_t stream) {
     const dim3 g(grid), b(kThreads);
     if constexpr (OUT == Out::Plain) {
-        const bool ragged = a.N % 16 != 0;
+        const bool ragged = a.N % 8 != 0;
         if (ragged && a.out_bf16) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, true, true>), g, b, 0, stream, a);
         else if (ragged) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, true, false>), g, b, 0, stream, a);
         else if (a.out_bf16) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, false, true>), g, b, 0, stream, a);
