@@ -118,7 +118,7 @@ struct MxGemmArgs {
     int K;
     const int32_t *info;
     int experts;
-    int64_t units, rows_hint;   // plan: row units at most, assignments
+    int64_t units, assignments;   // plan: row units at most, assignments
     // plain output
     void *Y;
     int64_t ldy;

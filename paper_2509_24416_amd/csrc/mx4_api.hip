@@ -116,7 +116,7 @@ clq_status plan_rows(clq::MxGemmArgs &g, const int32_t *tables, int64_t T, int64
     if ((s = check_plan(T, top_k, experts)) != CLQ_OK) return s;
     if (!aligned(tables, 4)) return CLQ_ERR_ALIGN;
     g.info = tables;
-    g.rows_hint = T * top_k;
+    g.assignments = T * top_k;
     g.units = clq::plan_max_units(T * top_k, experts);
     return check_tiles(g.units * 32 + 256 * experts, g.N);
 }

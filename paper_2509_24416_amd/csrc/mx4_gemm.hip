@@ -23,6 +23,7 @@ using tg::lds_addr;
 using tg::read16;
 using tg::static_for;
 using tg::v16f;
+using tg::v4f;
 using tg::v4u;
 using tg::v8i;
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
@@ -125,7 +126,7 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 }
 
 // ---- the tile kernel ---------------------------------------------------------------
-// A workgroup of 4 waves computes 128 channels x 256 tokens, each wave 128 channels x 64
+// A workgroup of NW waves computes 128 channels x 64 NW tokens, each wave 128 channels x 64
 // tokens (4 x 2 fragments of 32 x 32).  A k-stage is 64 codes, one matrix instruction per
 // fragment.  The channel units are shared by the waves: they go global -> LDS without
 // registers through a ring of NS stages, and a wave reads a stage's units back one stage
@@ -141,9 +142,9 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 // free after the barrier of the quad's first iteration and refilled there with quad q + 2,
 // needed at the end of quad q + 1.  Transfers past the end repeat the last stage or quad,
 // so the wait counts stay constant.
-constexpr int kWaves = 4, kThreads = kWaves * 64, kBN = 128, kBM = 256;
+constexpr int kBN = 128;
 constexpr int kStages = 5;                      // ring of channel units
-constexpr int kStageBytes = 4 * kMxUnit;        // one unit transferred by each wave
+constexpr int kStageBytes = 4 * kMxUnit;        // 4 / NW units transferred by each wave
 constexpr int kQuadBytes = 4 * kMxScaleRow;
 constexpr int kDepth = 4;                       // stages of token units in registers
 
@@ -193,17 +194,15 @@ __device__ __forceinline__ int bias_index(int n, int N, bool gated) {
 constexpr int kRowPitch = 272, kTurnBytes = 32 * kRowPitch;
 
 template <bool RAGGED, bool BF16>
-__device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][2], int fm, const float *bias,
-                                            uint8_t *turn, int64_t row0, int64_t row_end, int n0, int lane) {
+__device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][2], int fm, uint8_t *turn, int64_t row0, int64_t row_end, int n0, int lane) {
     const int h16 = (lane >> 5) * 16;
     uint8_t *w = turn + (lane & 31) * kRowPitch + h16 * 2;
 #pragma unroll
     for (int fn = 0; fn < 4; ++fn) {
         const v16f &x = acc[fn][fm];
-        const float *b = bias + fn * 32 + h16;
         uint32_t h[8];
 #pragma unroll
-        for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2<BF16>(x[v] + b[v], x[v + 1] + b[v + 1]);
+        for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2<BF16>(x[v], x[v + 1]);
         reinterpret_cast<v4u *>(w + fn * 64)[0] = v4u{h[0], h[1], h[2], h[3]};
         reinterpret_cast<v4u *>(w + fn * 64)[1] = v4u{h[4], h[5], h[6], h[7]};
     }
@@ -306,12 +305,12 @@ __device__ __forceinline__ void requantize(const Args &a, float (&f)[NF][16], in
     }
 }
 
-template <Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
-__global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
+template <int NW, Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+__global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
 {
-    constexpr int NS = kStages;
+    constexpr int NS = kStages, PPW = 4 / NW;   // transfers per wave and stage
     constexpr bool GATED = OUT == Out::Swiglu;
-    constexpr int kRing = NS * kStageBytes + 2 * kQuadBytes, kTurn = OUT == Out::Plain ? kWaves * kTurnBytes : 0;
+    constexpr int kRing = NS * kStageBytes + 2 * kQuadBytes, kTurn = OUT == Out::Plain ? NW * kTurnBytes : 0;
     __shared__ __align__(16) uint8_t pool[kRing > kTurn ? kRing : kTurn];
     __shared__ __align__(16) float ep[kBN];   // biases
     const int tid = threadIdx.x, lane = tid & 63;
@@ -335,17 +334,21 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
         tg::Args t;
         t.group_m = a.group_m; t.tiles_m = a.tiles_m; t.tiles_n = a.tiles_n;
         tg::tile_coords(t, tg::tile_of_block(), tm, tn);
-        rt.unit0 = tm * (kBM / 32);
+        rt.unit0 = tm * (2 * NW);
         rt.unit_end = a.xunits;
         rt.expert = 0;
     }
     const uint8_t *Wq = a.Wq + rt.expert * a.w_stride, *Ws = a.Ws + rt.expert * a.ws_stride;
 
-    // ---- sources: this wave's channel unit, its two token units, their scales -----------
+    // ---- sources: this wave's channel units, its two token units, their scales ----------
     const uint32_t l16 = (uint32_t)lane * 16, l4 = (uint32_t)lane * 4;
-    const int64_t wu = min(tn * 4 + wave, a.wunits - 1);
-    const Buffer wsrc = buffer_of(Wq + wu * nks * kMxUnit, (uint32_t)(nks * kMxUnit));
-    const Buffer wssrc = buffer_of(Ws + wu * nq * kMxScaleRow, (uint32_t)(nq * kMxScaleRow));
+    Buffer wsrc[PPW], wssrc[PPW];
+    static_for<0, PPW>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        const int64_t wu = min(tn * 4 + wave * PPW + i, a.wunits - 1);
+        wsrc[i] = buffer_of(Wq + wu * nks * kMxUnit, (uint32_t)(nks * kMxUnit));
+        wssrc[i] = buffer_of(Ws + wu * nq * kMxScaleRow, (uint32_t)(nq * kMxScaleRow));
+    });
     const uint8_t *xsrc[2], *xssrc[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
@@ -355,10 +358,18 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
     }
     const uint32_t pool0 = lds_addr(pool), spool = pool0 + NS * kStageBytes;
     auto produce = [&](uint32_t slot, int k) __attribute__((always_inline)) {
-        dma16(wsrc, l16, (uint32_t)min(k, nks - 1) * kMxUnit, pool0 + slot + (uint32_t)wave * kMxUnit);
+        const uint32_t off = (uint32_t)min(k, nks - 1) * kMxUnit;
+        static_for<0, PPW>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            dma16(wsrc[i], l16, off, pool0 + slot + (uint32_t)(wave * PPW + i) * kMxUnit);
+        });
     };
     auto produce_scales = [&](uint32_t slot, int q) __attribute__((always_inline)) {
-        dma4(wssrc, l4, (uint32_t)min(q, nq - 1) * kMxScaleRow, spool + slot + (uint32_t)wave * kMxScaleRow);
+        const uint32_t off = (uint32_t)min(q, nq - 1) * kMxScaleRow;
+        static_for<0, PPW>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            dma4(wssrc[i], l4, off, spool + slot + (uint32_t)(wave * PPW + i) * kMxScaleRow);
+        });
     };
     v4u x[kDepth][2];        // token units of stages k .. k + kDepth - 1
     uint32_t xs[2][2];       // token scales of even and odd quads
@@ -373,12 +384,11 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
         for (int f = 0; f < 2; ++f) xs[decltype(qc)::value][f] = *reinterpret_cast<const uint32_t *>(xssrc[f] + off);
     };
 
-    // the tile's biases, in registers until the ring is done with
-    float bv = 0.0f;
-    if (a.bias && tid < kBN) {
-        const int n = min(tn * kBN + tid, a.N - 1);
-        bv = widen(a.bias[(int64_t)rt.expert * a.N + bias_index(n, a.N, GATED)], a.bias_bf16);
-    }
+    // a channel's bias per thread: every sum starts from it
+    static_assert(NW * 64 >= kBN, "a thread per channel");
+    uint16_t bv = 0;
+    if (a.bias && tid < kBN)
+        bv = a.bias[(int64_t)rt.expert * a.N + bias_index(min(tn * kBN + tid, a.N - 1), a.N, GATED)];
     __builtin_amdgcn_sched_barrier(0);
 
     // ---- k loop ------------------------------------------------------------------------
@@ -389,9 +399,6 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
         constexpr int Q = decltype(qc)::value;
         static_for<0, 4>([&](auto f) { sc[Q].s[f] = read4<Q * kQuadBytes + decltype(f)::value * kMxScaleRow>(sl); });
     };
-    v16f acc[4][2];
-    static_for<0, 4>([&](auto i) { static_for<0, 2>([&](auto j) { acc[decltype(i)::value][decltype(j)::value] = v16f{}; }); });
-
     // prologue: two quads of scales and NS stages in flight, stage 0 and quad 0 landed
     produce_scales(0, 0);
     produce_scales(kQuadBytes, 1);
@@ -402,8 +409,18 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
         if constexpr (Q < kDepth) load_x(qc, Q);
         __builtin_amdgcn_sched_barrier(0);
     });
-    // after stage 0's transfer: at least that of every other stage
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NS - 1 + 2 * (kDepth - 1)) : "memory");
+    if (tid < kBN) ep[tid] = widen(bv, a.bias_bf16);
+    // outstanding: what came after stage 0's transfers and loads
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 1) * PPW + 2 * (kDepth - 1)) : "memory");
+    v16f acc[4][2];
+    const int h16 = (lane >> 5) * 16;
+    static_for<0, 4>([&](auto fc) {
+        constexpr int fn = decltype(fc)::value;
+        const v4f *b = reinterpret_cast<const v4f *>(ep + fn * 32 + h16);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[fn][0][v] = acc[fn][1][v] = b[v >> 2][v & 3];
+    });
+    __builtin_amdgcn_sched_barrier(0);
     op[0].read(wl);
     read_scales(IC<0>{});
     uint32_t cur = 0;
@@ -411,9 +428,9 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
     // position P8 of the eight stages of an even and an odd quad
     auto stage = [&](auto pc) __attribute__((always_inline)) {
         constexpr int P8 = decltype(pc)::value, P = P8 & 3, Q = P8 >> 2, R = P & 1;
-        // Outstanding: the last NS - 2 stages' transfer and two loads, and the three of the
+        // Outstanding: the last NS - 2 stages' transfers and two loads, and as many of the
         // scales if a quad began among them.
-        constexpr int VM = (NS - 2) * 3 + (P >= 1 && P <= NS - 2 ? 3 : 0);
+        constexpr int VM = (NS - 2) * (PPW + 2) + (P >= 1 && P <= NS - 2 ? PPW + 2 : 0);
         if constexpr (P == 0) wait_stage<VM>(op[R], sc[Q]);
         else wait_stage<VM>(op[R]);
         const uint32_t nxt = cur == (uint32_t)((NS - 1) * kStageBytes) ? 0u : cur + kStageBytes;
@@ -443,25 +460,22 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
     // sets are named, so that no register of theirs serves another value meanwhile)
     wait_stage<0>(op[0], sc[0]);
     wait_stage<0>(op[1], sc[1]);
-    if (tid < kBN) ep[tid] = bv;
-    __syncthreads();
 
     // ---- epilogue: lane owns row m and 16 consecutive channels of each fragment ---------
-    const int h16 = (lane >> 5) * 16;
     static_for<0, 2>([&](auto mc) {
         constexpr int fm = decltype(mc)::value;
         const int u = rt.unit0 + wave * 2 + fm;
         if (u >= rt.unit_end) return;
         if constexpr (OUT == Out::Plain) {
             const int64_t end = GROUPED ? (int64_t)rt.unit_end * 32 : a.M;
-            store_plain<RAGGED, BF16>(a, acc, fm, ep, pool + wave * kTurnBytes, (int64_t)u * 32, end, tn * kBN, lane);
+            store_plain<RAGGED, BF16>(a, acc, fm, pool + wave * kTurnBytes, (int64_t)u * 32, end, tn * kBN, lane);
         } else if constexpr (GATED) {
             float f[2][16];
             static_for<0, 2>([&](auto pc) {
                 constexpr int i = decltype(pc)::value;
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    f[i][v] = silu(acc[2 * i][fm][v] + ep[64 * i + h16 + v]) * (acc[2 * i + 1][fm][v] + ep[64 * i + 32 + h16 + v]);
+                    f[i][v] = silu(acc[2 * i][fm][v]) * acc[2 * i + 1][fm][v];
             });
             requantize<B, 2>(a, f, lane, u, tn * 2);
         } else {
@@ -469,43 +483,218 @@ __global__ void __launch_bounds__(kThreads, 2) mx_tile_kernel(Args a)
             static_for<0, 4>([&](auto pc) {
                 constexpr int i = decltype(pc)::value;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const float y = acc[i][fm][v] + ep[32 * i + h16 + v];
-                    f[i][v] = OUT == Out::Gelu ? gelu(y) : y;
-                }
+                for (int v = 0; v < 16; ++v) f[i][v] = OUT == Out::Gelu ? gelu(acc[i][fm][v]) : acc[i][fm][v];
             });
             requantize<B, 4>(a, f, lane, u, tn * 4);
         }
     });
 }
 
+// ---- few rows ----------------------------------------------------------------------------
+// With few tiles of the kernel above most compute units are idle and a launch takes the
+// length of one wave's k loop.  Here a workgroup computes 32 rows x 32 FN channels, its KS
+// waves each a part of the k loop with operands straight from memory (nothing is shared
+// between them), kAhead stages ahead; the partial sums meet in LDS.  A plain result needs no
+// channel but its own (FN = 1: the most workgroups), a requantized one the channels of a
+// rotation block (FN = 4).
+template <int FN, bool MX4>
+struct Split {
+    static constexpr int KS = FN == 1 ? 8 : 4, NT = KS * 64, BN = 32 * FN, kAhead = FN == 1 ? 6 : 3;
+    static constexpr int kPitch = BN + 4;   // floats between rows of a partial tile, for the banks
+};
+template <Out OUT> using SplitOf = Split<OUT == Out::Plain ? 1 : 4, OUT != Out::Plain>;
+
+template <Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+__global__ void __launch_bounds__(SplitOf<OUT>::NT) mx_split_kernel(Args a)
+{
+    constexpr bool MX4 = OUT != Out::Plain, GATED = OUT == Out::Swiglu;
+    constexpr int FN = MX4 ? 4 : 1;
+    using C = SplitOf<OUT>;
+    constexpr int KS = C::KS, D = C::kAhead;
+    __shared__ __align__(16) float part[KS][32 * C::kPitch];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int nks = a.K >> 6, nq = (a.K + 255) >> 8;
+    int tn, u;
+    RowTile rt;
+    if constexpr (GROUPED) {
+        const int total = a.info[plan_table_offset(a.experts, 0) + a.experts] * a.tiles_n;
+        if ((int)blockIdx.x >= total) return;
+        tn = blockIdx.x % a.tiles_n;
+        rt = find_tile(a, blockIdx.x / a.tiles_n, lane);
+        u = rt.unit0;
+    } else {
+        tn = blockIdx.x % a.tiles_n;
+        u = blockIdx.x / a.tiles_n;
+        rt.expert = 0;
+    }
+    // this wave's stages; bytes of a scale row: lane's dword, then the stage's byte
+    const int kb = wave * nks / KS, ke = (wave + 1) * nks / KS;
+    const uint8_t *wsrc[FN], *wssrc[FN];
+#pragma unroll
+    for (int f = 0; f < FN; ++f) {
+        const int64_t wu = min(tn * FN + f, a.wunits - 1);
+        wsrc[f] = a.Wq + rt.expert * a.w_stride + wu * nks * kMxUnit + lane * 16;
+        wssrc[f] = a.Ws + rt.expert * a.ws_stride + wu * nq * kMxScaleRow + lane * 4;
+    }
+    const uint8_t *xsrc = a.Xq + (int64_t)u * nks * kMxUnit + lane * 16;
+    const uint8_t *xssrc = a.Xs + (int64_t)u * nq * kMxScaleRow + lane * 4;
+    v16f acc[FN];
+#pragma unroll
+    for (int f = 0; f < FN; ++f) acc[f] = v16f{};
+    if (kb < ke) {
+        v4u w[D][FN], x[D];
+        uint8_t ws[D][FN], xs[D];
+        auto load = [&](auto dc, int k) __attribute__((always_inline)) {
+            constexpr int d = decltype(dc)::value;
+            const uint32_t off = (uint32_t)k * kMxUnit, soff = (uint32_t)(k >> 2) * kMxScaleRow + (k & 3);
+#pragma unroll
+            for (int f = 0; f < FN; ++f) {
+                w[d][f] = *reinterpret_cast<const v4u *>(wsrc[f] + off);
+                ws[d][f] = wssrc[f][soff];
+            }
+            x[d] = *reinterpret_cast<const v4u *>(xsrc + off);
+            xs[d] = xssrc[soff];
+        };
+        auto mma = [&](auto dc) __attribute__((always_inline)) {
+            constexpr int d = decltype(dc)::value;
+#pragma unroll
+            for (int f = 0; f < FN; ++f) acc[f] = mfma_mx4<0>(w[d][f], x[d], acc[f], ws[d][f], xs[d]);
+        };
+        const int last = ke - 1;   // loads past the end repeat the last stage
+        static_for<0, D>([&](auto dc) {
+            load(dc, min(kb + decltype(dc)::value, last));
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        // whole groups of D stages, then the rest one by one: one loop with one exit, so that
+        // the compiler's waits count only the loads that matter
+        const int groups = (ke - kb) / D, rest = (ke - kb) - groups * D;
+        int k = kb + D;
+        for (int g = 0; g < groups; ++g)
+            static_for<0, D>([&](auto dc) {
+                mma(dc);
+                load(dc, min(k, last));
+                __builtin_amdgcn_sched_barrier(0);
+                ++k;
+            });
+        static_for<0, D - 1>([&](auto dc) {
+            if (rest > decltype(dc)::value) mma(dc);
+        });
+    }
+    // lane's 16 channels of its row
+    const int row = lane & 31, h16 = (lane >> 5) * 16;
+#pragma unroll
+    for (int f = 0; f < FN; ++f) {
+        v4f *dst = reinterpret_cast<v4f *>(&part[wave][row * C::kPitch + f * 32 + h16]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) dst[q] = v4f{acc[f][4 * q], acc[f][4 * q + 1], acc[f][4 * q + 2], acc[f][4 * q + 3]};
+    }
+    __syncthreads();
+    const uint16_t *bias = a.bias ? a.bias + (int64_t)rt.expert * a.N : nullptr;
+    if constexpr (!MX4) {
+        // eight channels of a row per thread
+        const int r = tid >> 2, c = (tid & 3) * 8, n = tn * C::BN + c;
+        const int64_t m = (int64_t)u * 32 + r;
+        if (r >= 32 || n >= a.N || (!GROUPED && m >= a.M)) return;
+        float s[8] = {};
+#pragma unroll
+        for (int w = 0; w < KS; ++w) {
+            const v4f *src = reinterpret_cast<const v4f *>(&part[w][r * C::kPitch + c]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += src[e >> 2][e & 3];
+        }
+        if (bias) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += widen(bias[min(n + e, a.N - 1)], a.bias_bf16);
+        }
+        const v4u v = {narrow2<BF16>(s[0], s[1]), narrow2<BF16>(s[2], s[3]), narrow2<BF16>(s[4], s[5]),
+                       narrow2<BF16>(s[6], s[7])};
+        uint16_t *dst = a.Y + m * a.ldy + n;
+        if (!RAGGED || n <= a.N - 8) {
+            *reinterpret_cast<v4u *>(dst) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n + e < a.N) dst[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+        }
+    } else {
+        // wave 0 .. NW - 1: the fragments of a rotation block each, summed in the products' layout
+        constexpr int NW = GATED || B == 128 ? 1 : 2, NF = FN / NW;
+        if (wave >= NW) return;
+        float s[NF][16];
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+            const int c = (wave * NF + i) * 32 + h16;
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                s[i][v] = bias ? widen(bias[bias_index(min(tn * C::BN + c + v, a.N - 1), a.N, GATED)], a.bias_bf16) : 0.0f;
+#pragma unroll
+            for (int w = 0; w < KS; ++w) {
+                const v4f *src = reinterpret_cast<const v4f *>(&part[w][row * C::kPitch + c]);
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s[i][v] += src[v >> 2][v & 3];
+            }
+        }
+        if constexpr (GATED) {
+            float f[2][16];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) f[i][v] = silu(s[2 * i][v]) * s[2 * i + 1][v];
+            requantize<B, 2>(a, f, lane, u, tn * 2);
+        } else {
+            if constexpr (OUT == Out::Gelu) {
+#pragma unroll
+                for (int i = 0; i < NF; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) s[i][v] = gelu(s[i][v]);
+            }
+            requantize<B, NF>(a, s, lane, u, tn * 4 + wave * NF);
+        }
+    }
+}
+
+// The kernels: 32-row units split over the k loop, tiles of 128 and of 256 rows.
+enum Kernel { kSplit, kTile128, kTile256 };
+
+template <Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
+    const int bn = kernel == kSplit ? SplitOf<OUT>::BN : kBN;
+    a.tiles_n = (a.N + bn - 1) / bn;
+    const dim3 grid((unsigned)(row_tiles * a.tiles_n));
+    if (kernel == kSplit)
+        hipLaunchKernelGGL((mx_split_kernel<OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(SplitOf<OUT>::NT), 0, stream, a);
+    else if (kernel == kTile128)
+        hipLaunchKernelGGL((mx_tile_kernel<2, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(128), 0, stream, a);
+    else hipLaunchKernelGGL((mx_tile_kernel<4, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(256), 0, stream, a);
+}
+
 template <Out OUT, int B, bool GROUPED>
-void launch_kernel(const Args &a, unsigned grid, hipStream_t stream) {
-    const dim3 g(grid), b(kThreads);
+void launch_kernel(const Args &a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
     if constexpr (OUT == Out::Plain) {
         const bool ragged = a.N % 8 != 0;
-        if (ragged && a.out_bf16) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, true, true>), g, b, 0, stream, a);
-        else if (ragged) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, true, false>), g, b, 0, stream, a);
-        else if (a.out_bf16) hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, false, true>), g, b, 0, stream, a);
-        else hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, false, false>), g, b, 0, stream, a);
+        if (ragged && a.out_bf16) launch_one<OUT, B, GROUPED, true, true>(a, kernel, row_tiles, stream);
+        else if (ragged) launch_one<OUT, B, GROUPED, true, false>(a, kernel, row_tiles, stream);
+        else if (a.out_bf16) launch_one<OUT, B, GROUPED, false, true>(a, kernel, row_tiles, stream);
+        else launch_one<OUT, B, GROUPED, false, false>(a, kernel, row_tiles, stream);
     } else {
-        hipLaunchKernelGGL((mx_tile_kernel<OUT, B, GROUPED, false, false>), g, b, 0, stream, a);
+        launch_one<OUT, B, GROUPED, false, false>(a, kernel, row_tiles, stream);
     }
 }
 
 template <bool GROUPED>
-hipError_t launch_out(Args &a, MxAct act, int block, unsigned grid, hipStream_t stream) {
+hipError_t launch_out(const Args &a, MxAct act, int block, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
     if (a.Y) {
-        launch_kernel<Out::Plain, 0, GROUPED>(a, grid, stream);
+        launch_kernel<Out::Plain, 0, GROUPED>(a, kernel, row_tiles, stream);
     } else {
         auto by_block = [&](auto oc) {
             constexpr Out OUT = decltype(oc)::value;
             switch (block) {
-                case 0: launch_kernel<OUT, 0, GROUPED>(a, grid, stream); break;
-                case 32: launch_kernel<OUT, 32, GROUPED>(a, grid, stream); break;
-                case 64: launch_kernel<OUT, 64, GROUPED>(a, grid, stream); break;
+                case 0: launch_kernel<OUT, 0, GROUPED>(a, kernel, row_tiles, stream); break;
+                case 32: launch_kernel<OUT, 32, GROUPED>(a, kernel, row_tiles, stream); break;
+                case 64: launch_kernel<OUT, 64, GROUPED>(a, kernel, row_tiles, stream); break;
                 default:
-                    if constexpr (OUT != Out::Swiglu) launch_kernel<OUT, 128, GROUPED>(a, grid, stream);
+                    if constexpr (OUT != Out::Swiglu) launch_kernel<OUT, 128, GROUPED>(a, kernel, row_tiles, stream);
                     break;
             }
         };
@@ -516,6 +705,35 @@ hipError_t launch_out(Args &a, MxAct act, int block, unsigned grid, hipStream_t 
         }
     }
     return hipGetLastError();
+}
+
+// The kernel of a product, by the workgroups it would be cut into (c compute units; a
+// plan's row units at most, which a few tokens nearly reach).  us, split / 128 / 256 rows:
+//   split   plain results up to 2 c workgroups of 32 channels (256 x 1152 -> 1152, 288 of
+//           them: 6.0 / 6.5 / 7.2; 512 x 1152 -> 2304, 1152: 9.6 / 7.1 / 7.4), long k loops
+//           up to 3 c (777 x 4608 -> 1152, 900: 14.0 / 14.5 / 15.7; 1024, 1152: 16.9 / 14.5 /
+//           15.7; 64 tokens to 2 of 16 experts 13.2 / 14.6 / 16.4, 256 tokens 16.5 / 15.6 /
+//           17.5); requantized ones up to 1.75 c of 128 channels (384 x 1152 -> 4608, 432: 8.8
+//           / 10.7 / 12.8; 512, 576: 12.1 / 10.9 / 11.4), where one wave finishes a tile
+//           whose channels gate each other up to c (8 tokens to 6 of 64 experts, 1152 -> 1536,
+//           588: 14.9 / 10.3 / 11.2);
+//   128     while those tiles are one to a unit (1024 x 4608 -> 1152, 72 of them: 14.5 / 15.7;
+//           1024 x 1152 -> 4608, 288: 9.9 / 8.2), and for experts of under 512 rows on average,
+//           whose last tiles are half empty (384 rows, 1152 -> 1536 gated: 38.5 / 41.8; 512
+//           rows, 1152 -> 4608: 51.6 / 50.2; 5400: 405 / 399);
+//   256     otherwise: the fewest operand bytes (43200 x 1152 -> 4608 189 / 171).
+inline Kernel pick_kernel(const MxGemmArgs &g, int64_t units, int64_t c) {
+    const bool mx4 = g.Y == nullptr;
+    const int64_t split = units * ((g.N + (mx4 ? 127 : 31)) / (mx4 ? 128 : 32));
+    const int64_t most = mx4 ? (g.act == MxAct::Swiglu ? c : c * 7 / 4) : (g.K >= 48 * 64 ? 3 * c : 2 * c);
+    if (split <= most) return kSplit;
+    const int64_t tiles_n = (g.N + kBN - 1) / kBN;
+    if (g.info) {
+        const int64_t nonempty = g.experts < g.assignments ? g.experts : g.assignments;
+        if (g.assignments < 512 * (int64_t)g.experts || (g.assignments / 128 + nonempty) * tiles_n <= c) return kTile128;
+        return kTile256;
+    }
+    return (units + 3) / 4 * tiles_n <= c ? kTile128 : kTile256;
 }
 
 }  // namespace mx
@@ -533,7 +751,6 @@ hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
     a.wunits = (int)(padded_rows(g.N) >> 5);
     a.w_stride = (int64_t)a.wunits * (g.K >> 6) * kMxUnit;
     a.ws_stride = mx_scale_bytes(a.wunits, g.K);
-    a.tiles_n = (int)((g.N + mx::kBN - 1) / mx::kBN);
     a.group_m = 4;
     a.info = g.info;
     a.experts = g.experts;
@@ -542,15 +759,17 @@ hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
     a.Oq = g.Oq;
     a.Os = g.Os;
     a.oK = (int)(g.act == MxAct::Swiglu ? g.N / 2 : g.N);
+    a.xunits = (int)(g.info ? g.units : padded_act_rows(g.M) >> 5);
+    const mx::Kernel kernel = mx::pick_kernel(g, a.xunits, compute_units());
+    a.log_units = kernel == mx::kSplit ? 0 : kernel == mx::kTile128 ? 2 : 3;
+    const int64_t per = 1 << a.log_units;
     if (g.info) {
-        a.log_units = 3;
-        a.xunits = (int)g.units;
-        const int64_t most = g.units / 8 + (g.experts < g.units ? g.experts : g.units);
-        return mx::launch_out<true>(a, g.act, g.block, (unsigned)(most * a.tiles_n), stream);
+        // every expert's last tile may be a part of one
+        const int64_t most = per == 1 ? g.units : g.units / per + (g.experts < g.units ? g.experts : g.units);
+        return mx::launch_out<true>(a, g.act, g.block, kernel, most, stream);
     }
-    a.xunits = (int)(padded_act_rows(g.M) >> 5);
-    a.tiles_m = (int)((g.M + mx::kBM - 1) / mx::kBM);
-    return mx::launch_out<false>(a, g.act, g.block, (unsigned)((int64_t)a.tiles_m * a.tiles_n), stream);
+    a.tiles_m = (int)((a.xunits + per - 1) / per);
+    return mx::launch_out<false>(a, g.act, g.block, kernel, a.tiles_m, stream);
 }
 
 }  // namespace clq

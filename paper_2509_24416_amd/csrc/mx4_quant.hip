@@ -26,6 +26,8 @@ namespace {
 
 constexpr int kTileCols = 256, kChunkLanes = kTileCols / 8, kRowGroups = 8;
 constexpr int kThreads = kChunkLanes * kRowGroups;   // 32 rows x 256 columns
+constexpr int kGatherThreads = 256;
+constexpr int kGatherLds = 160 * 1024;               // four rows of up to 20480 columns
 
 // the larger of two magnitudes, a NaN if either is one
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -66,38 +68,82 @@ struct QuantParams {
     uint8_t *codes, *scales;
 };
 
+// Source row of W or X of output row r of unit u; negative: zeros.
+__device__ __forceinline__ int64_t source_row(const QuantParams &p, int64_t u, int r) {
+    if (p.source) {
+        const int64_t src = p.source[u * 32 + r];
+        return src < p.rows ? src : -1;
+    }
+    const int64_t mat = u / p.mat_units, n = (u - mat * p.mat_units) * 32 + r;
+    if (n >= p.rows) return -1;
+    return (p.gated ? gated_row(n, p.rows) : n) + mat * p.rows;
+}
+__device__ __forceinline__ int64_t used_units(const QuantParams &p) {
+    return p.total_units ? min((int64_t)*p.total_units, p.units) : p.units;
+}
+
+// Stage h = 1 of a lane's pair of columns (the values themselves without a rotation).
+template <int B>
+__device__ __forceinline__ void pair_in(float lo, float hi, float &a, float &b) {
+    a = B ? lo + hi : lo;
+    b = B ? lo - hi : hi;
+}
+
+// The rest of the rotation, the codes and the stores of four rows' chunk of 8 columns,
+// x[row][column] after stage h = 1; rho0: the first row's fragment row.
+template <int B>
+__device__ __forceinline__ void quantize_chunk(const QuantParams &p, float (&x)[4][8], int chunk, const CrossSigns &cs,
+                                               int64_t u, int rho0) {
+    if constexpr (B != 0) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) fwht8_rest(x[r]);
+        cross_stages<B, 4>(x, cs);
+    }
+    const uint32_t flip = B && cs.sign < 0.0f ? 0x88888888u : 0u;
+    uint32_t codes[4];
+    int byte[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float m0 = 0.0f, m1 = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+            m0 = max_nan(max_nan(m0, fabsf(x[r][e])), fabsf(x[r][e + 1]));
+            m1 = max_nan(max_nan(m1, fabsf(x[r][e + 2])), fabsf(x[r][e + 3]));
+        }
+        float m = max_nan(m0, m1);
+        m = max_nan(m, lane_xchg<kLaneXor1>(m));
+        m = max_nan(m, lane_xchg<kLaneXor2>(m));
+        byte[r] = mx_scale_byte(__float_as_uint(m) & 0x7fffffffu, p.log_div);
+        codes[r] = mx_pack8(x[r], mx_scale_value(byte[r], p.log_div)) ^ flip;
+    }
+    quad_transpose(codes, chunk & 1, chunk & 2);
+    const int k4 = chunk & 3, c32 = chunk >> 2;   // the row of the four that this lane stores
+    if (8 * chunk < p.K) {
+        *reinterpret_cast<uint4 *>(p.codes + mx_code_offset(u, rho0 + k4, c32, p.K)) =
+            make_uint4(codes[0], codes[1], codes[2], codes[3]);
+        const int sb = k4 == 0 ? byte[0] : k4 == 1 ? byte[1] : k4 == 2 ? byte[2] : byte[3];
+        p.scales[mx_scale_offset(u, rho0 + k4, c32, p.K)] = (uint8_t)sb;
+    }
+}
+
+// A workgroup takes 32 rows x 256 columns.  Gathered inputs (PERM): from memory.
 template <int B, bool BF16, bool PERM>
 __global__ void __launch_bounds__(kThreads) mx_quant_kernel(QuantParams p)
 {
     const int t = threadIdx.x;
     const int lc = t & (kChunkLanes - 1), rg = t / kChunkLanes;
     // chunk order over lanes: see rq_device.h
-    const int chunk = (lc & ~7) | logical_lane(lc & 7);
-    const bool b0 = chunk & 1, b1 = chunk & 2;
-    const CrossSigns cs = cross_signs<B ? B : 32>(chunk);
-    const uint32_t flip = B && cs.sign < 0.0f ? 0x88888888u : 0u;
-    int64_t units = p.units;
-    if (p.total_units) units = min((int64_t)*p.total_units, units);
-    const int64_t work = units * p.tiles;
+    const int lane_chunk = (lc & ~7) | logical_lane(lc & 7);
+    const CrossSigns cs = cross_signs<B ? B : 32>(lane_chunk);
+    const int64_t work = used_units(p) * p.tiles;
     for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
         const int64_t u = w / p.tiles;
-        const int ct = (int)(w - u * p.tiles);
-        const int col = ct * kTileCols + 8 * chunk;
-        const int64_t mat = u / p.mat_units, um = u - mat * p.mat_units;
-        // four consecutive rows; in the weights' fragment order four rows aligned to
-        // four stay together
-        const int64_t r0 = um * 32 + rg * 4;
-        const int rho0 = p.weights ? wq_rho(rg * 4) : rg * 4;
+        const int chunk = (int)(w - u * p.tiles) * kChunkLanes + lane_chunk, col = 8 * chunk;
         const bool in = col < p.K;   // (whole octets and, for B = 128, whole 16 lanes)
         float x[4][8];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int64_t n = r0 + r;
-            int64_t src = n < p.rows ? (p.gated ? gated_row(n, p.rows) : n) + mat * p.rows : -1;
-            if (p.source) {
-                src = p.source[u * 32 + rg * 4 + r];
-                if (src >= p.rows) src = -1;
-            }
+            const int64_t src = source_row(p, u, rg * 4 + r);
             uint32_t d[4] = {0u, 0u, 0u, 0u};
             if (in && src >= 0) {
                 const uint16_t *row = p.X + src * p.ldx;
@@ -111,75 +157,111 @@ __global__ void __launch_bounds__(kThreads) mx_quant_kernel(QuantParams p)
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float lo = widen((uint16_t)d[e], BF16), hi = widen((uint16_t)(d[e] >> 16), BF16);
-                x[r][2 * e] = B ? lo + hi : lo;
-                x[r][2 * e + 1] = B ? lo - hi : hi;
-            }
-            if constexpr (B != 0) fwht8_rest(x[r]);
+            for (int e = 0; e < 4; ++e)
+                pair_in<B>(widen((uint16_t)d[e], BF16), widen((uint16_t)(d[e] >> 16), BF16), x[r][2 * e], x[r][2 * e + 1]);
         }
-        if constexpr (B != 0) cross_stages<B, 4>(x, cs);
-        uint32_t codes[4];
-        int byte[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float m = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(x[r][e]));
-            m = max_nan(m, lane_xchg<kLaneXor1>(m));
-            m = max_nan(m, lane_xchg<kLaneXor2>(m));
-            byte[r] = mx_scale_byte(__float_as_uint(m) & 0x7fffffffu, p.log_div);
-            codes[r] = mx_pack8(x[r], mx_scale_value(byte[r], p.log_div)) ^ flip;
-        }
-        quad_transpose(codes, b0, b1);
-        const int k4 = chunk & 3;   // the row of the four that this lane stores
-        if (in) {
-            const int c32 = col >> 5;
-            *reinterpret_cast<uint4 *>(p.codes + mx_code_offset(u, rho0 + k4, c32, p.K)) =
-                make_uint4(codes[0], codes[1], codes[2], codes[3]);
-            const int sb = k4 == 0 ? byte[0] : k4 == 1 ? byte[1] : k4 == 2 ? byte[2] : byte[3];
-            p.scales[mx_scale_offset(u, rho0 + k4, c32, p.K)] = (uint8_t)sb;
-        }
+        // (in the weights' fragment order four rows aligned to four stay together)
+        quantize_chunk<B>(p, x, chunk, cs, u, p.weights ? wq_rho(rg * 4) : rg * 4);
     }
 }
 
-// 8 codes of a row per thread, 16 neighbouring threads on 128 columns
+// Gathered inputs whose four rows fit LDS: a workgroup takes four rows, staged with the
+// rows' values of a column side by side, so that one 8-byte read gathers a column of all
+// four.  From memory, column by column, 2777 x 4608 took 45 us.
+template <int B, bool BF16>
+__global__ void __launch_bounds__(kGatherThreads) mx_gather_kernel(QuantParams p)
+{
+    extern __shared__ __align__(16) uint8_t staged[];
+    const int t = threadIdx.x, chunks = p.K >> 3, padded = (chunks + 15) & ~15;
+    const int64_t work = used_units(p) * 8;
+    for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
+        const int64_t u = w >> 3;
+        const int rg = (int)(w & 7);
+        const uint16_t *row[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t src = source_row(p, u, rg * 4 + r);
+            row[r] = src < 0 ? nullptr : p.X + src * p.ldx;
+        }
+        for (int c = t; c < chunks; c += kGatherThreads) {
+            uint4 v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                v[r] = row[r] ? reinterpret_cast<const uint4 *>(row[r])[c] : make_uint4(0u, 0u, 0u, 0u);
+            uint32_t q[16];
+            interleave_rows(v, q);
+            uint4 *dst = reinterpret_cast<uint4 *>(staged) + c * 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[i] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+        }
+        __syncthreads();
+        for (int c0 = t; c0 < padded; c0 += kGatherThreads) {   // (whole 16-lane rows)
+            const int chunk = (c0 & ~7) | logical_lane(c0 & 7);
+            const CrossSigns cs = cross_signs<B ? B : 32>(chunk);
+            float x[4][8];
+            const bool in = chunk < chunks;
+            int s[8] = {};
+            if (in) {
+                const int4 s0 = reinterpret_cast<const int4 *>(p.perm)[2 * chunk];
+                const int4 s1 = reinterpret_cast<const int4 *>(p.perm)[2 * chunk + 1];
+                s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w;
+                s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const uint2 lo = reinterpret_cast<const uint2 *>(staged)[s[e]];
+                const uint2 hi = reinterpret_cast<const uint2 *>(staged)[s[e + 1]];
+                const uint32_t l[2] = {lo.x, lo.y}, h[2] = {hi.x, hi.y};
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    pair_in<B>(widen((uint16_t)(l[r >> 1] >> (16 * (r & 1))), BF16),
+                               widen((uint16_t)(h[r >> 1] >> (16 * (r & 1))), BF16), x[r][e], x[r][e + 1]);
+            }
+            quantize_chunk<B>(p, x, chunk, cs, u, p.weights ? wq_rho(rg * 4) : rg * 4);
+        }
+        __syncthreads();
+    }
+}
+
+// The inverse.  A workgroup takes 32 rows x 128 columns, a thread 8 codes of one row twice
+// over: 16 neighbouring threads store 256 bytes of a row (16-bit types), and the 4-byte
+// pieces of codes that they read are all of the tile's two units between them.
 template <class T>
 __global__ void __launch_bounds__(256) mx_dequant_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows,
                                                          int K, bool weights, bool gated, int64_t mats, T *out,
                                                          int64_t ldo)
 {
-    const int tiles = (K + 127) / 128;
-    const int64_t mat_units = weights ? padded_rows(rows) >> 5 : padded_act_rows(rows) >> 5;
-    const int64_t total = mats * mat_units * 32 * tiles * 16;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t ur = i / (512 * tiles);   // unit
-        const int in_unit = (int)(i - ur * 512 * tiles);
-        const int tile = in_unit / 512, q = in_unit & 511;
-        const int row = q >> 4, col = tile * 128 + (q & 15) * 8;
-        const int64_t mat = ur / mat_units, n = (ur - mat * mat_units) * 32 + row;
-        if (n >= rows || col >= K) continue;
-        const int rho = weights ? wq_rho(row) : row;
-        const uint32_t d = *reinterpret_cast<const uint32_t *>(codes + mx_code_offset(ur, rho, col >> 5, K) +
-                                                               (col & 31) / 2);
-        const int byte = scales[mx_scale_offset(ur, rho, col >> 5, K)];
-        const float s = __uint_as_float(byte == 255 ? 0x7fc00000u : byte == 0 ? 0x00400000u : (uint32_t)byte << 23);
-        const int64_t dst = mat * rows + (gated ? gated_row(n, rows) : n);
-        T v[8];
+    const int tiles = (K + 127) / 128, t = threadIdx.x;
+    const int64_t mat_units = (weights ? padded_rows(rows) : padded_act_rows(rows)) >> 5;
+    const int64_t work = mats * mat_units * tiles;
+    for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
+        const int64_t u = w / tiles, mat = u / mat_units;
+        const int col = (int)(w - u * tiles) * 128 + (t & 15) * 8, c = col >> 5;
+        if (col >= K) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int c = (int)(d >> (4 * e)) & 15, ex = (c >> 1) & 3, m = c & 1;
-            const float a = ex ? __uint_as_float((uint32_t)(126 + ex) << 23 | (uint32_t)m << 22) : 0.5f * (float)m;
-            const float f = (c & 8 ? -a : a) * s;
-            if constexpr (sizeof(T) == 4) v[e] = f;
-            else v[e] = (T)f;
-        }
-        T *o = out + dst * ldo + col;
-        if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<float4 *>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            *reinterpret_cast<uint4 *>(o) = *reinterpret_cast<uint4 *>(v);
+        for (int half = 0; half < 2; ++half) {
+            const int row = half * 16 + (t >> 4), rho = weights ? wq_rho(row) : row;
+            const int64_t n = (u - mat * mat_units) * 32 + row;
+            if (n >= rows) continue;
+            const uint32_t d = *reinterpret_cast<const uint32_t *>(codes + mx_code_offset(u, rho, c, K) + (col & 31) / 2);
+            const int byte = scales[mx_scale_offset(u, rho, c, K)];
+            // (byte 255: NaN; byte 0, 2^-127, is fp32's subnormal)
+            const float s = __uint_as_float(byte == 255 ? 0x7fc00000u : byte == 0 ? 0x00400000u : (uint32_t)byte << 23);
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            const f2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(d, 1.0f, 0),
+                             __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(d, 1.0f, 1),
+                             __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(d, 1.0f, 2),
+                             __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(d, 1.0f, 3)};
+            T v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (T)(p[e >> 1][e & 1] * s);
+            T *o = out + (mat * rows + (gated ? gated_row(n, rows) : n)) * ldo + col;
+            if constexpr (sizeof(T) == 4) {
+                reinterpret_cast<float4 *>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                reinterpret_cast<float4 *>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+                *reinterpret_cast<uint4 *>(o) = *reinterpret_cast<uint4 *>(v);
+            }
         }
     }
 }
@@ -208,20 +290,35 @@ __global__ void __launch_bounds__(256) mx_pack_kernel(const uint8_t *codes, cons
     }
 }
 
+constexpr int64_t kMaxGrid = 1 << 20;   // workgroups of a launch; the rest by a loop
+
 template <int B, bool BF16>
-void launch_quant(const QuantParams &p, unsigned grid, hipStream_t stream) {
-    if (p.perm) hipLaunchKernelGGL((mx_quant_kernel<B, BF16, true>), dim3(grid), dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((mx_quant_kernel<B, BF16, false>), dim3(grid), dim3(kThreads), 0, stream, p);
+hipError_t launch_quant(const QuantParams &p, hipStream_t stream) {
+    const size_t lds = (size_t)p.K * 8;
+    // (the vector loads of the indices need 16 bytes of alignment)
+    if (p.perm && lds <= (size_t)kGatherLds && (reinterpret_cast<uintptr_t>(p.perm) & 15) == 0) {
+        if (lds > 64 * 1024) {
+            const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void *>(&mx_gather_kernel<B, BF16>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kGatherLds);
+            if (set != hipSuccess) return set;
+        }
+        const int64_t work = p.units * 8;
+        hipLaunchKernelGGL((mx_gather_kernel<B, BF16>), dim3((unsigned)(work < kMaxGrid ? work : kMaxGrid)),
+                           dim3(kGatherThreads), lds, stream, p);
+        return hipGetLastError();
+    }
+    const int64_t work = p.units * p.tiles;
+    const dim3 grid((unsigned)(work < kMaxGrid ? work : kMaxGrid));
+    if (p.perm) hipLaunchKernelGGL((mx_quant_kernel<B, BF16, true>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((mx_quant_kernel<B, BF16, false>), grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
 }
 template <int B>
-void launch_quant(const QuantParams &p, bool bf16, unsigned grid, hipStream_t stream) {
-    if (bf16) launch_quant<B, true>(p, grid, stream);
-    else launch_quant<B, false>(p, grid, stream);
+hipError_t launch_quant(const QuantParams &p, bool bf16, hipStream_t stream) {
+    return bf16 ? launch_quant<B, true>(p, stream) : launch_quant<B, false>(p, stream);
 }
 
 }  // namespace
-
-constexpr int64_t kMaxGrid = 1 << 20;   // workgroups of a launch; the rest by a loop
 
 hipError_t launch_mx_quantize(const MxQuantArgs &a, hipStream_t stream) {
     QuantParams p;
@@ -240,22 +337,19 @@ hipError_t launch_mx_quantize(const MxQuantArgs &a, hipStream_t stream) {
     p.total_units = a.total_units;
     p.codes = a.codes;
     p.scales = a.scales;
-    const int64_t work = p.units * p.tiles;
-    const unsigned grid = (unsigned)(work < kMaxGrid ? work : kMaxGrid);
     const bool bf16 = a.type == MxType::BF16;
     switch (a.block) {
-        case 0: launch_quant<0>(p, bf16, grid, stream); break;
-        case 32: launch_quant<32>(p, bf16, grid, stream); break;
-        case 64: launch_quant<64>(p, bf16, grid, stream); break;
-        default: launch_quant<128>(p, bf16, grid, stream); break;
+        case 0: return launch_quant<0>(p, bf16, stream);
+        case 32: return launch_quant<32>(p, bf16, stream);
+        case 64: return launch_quant<64>(p, bf16, stream);
+        default: return launch_quant<128>(p, bf16, stream);
     }
-    return hipGetLastError();
 }
 
 hipError_t launch_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int K, bool weights,
                                 bool gated, int mats, MxType type, void *out, int64_t ldo, hipStream_t stream) {
     const int64_t units = (weights ? padded_rows(rows) : padded_act_rows(rows)) / 32 * mats;
-    const int64_t want = units * ((K + 127) / 128) * 2;
+    const int64_t want = units * ((K + 127) / 128);
     const dim3 grid((unsigned)(want < kMaxGrid ? want : kMaxGrid)), block(256);
     switch (type) {
         case MxType::F16:

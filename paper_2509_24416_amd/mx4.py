@@ -58,14 +58,25 @@ _ACTS = {None: 0, "none": 0, "gelu": 1, "swiglu": 2}
 _SCORES = {"softmax": 0, "sigmoid": 1}
 
 
-@dataclass(slots=True)
 class MX4:
-    """Activations quantized to MX4: `rows` rows of `K` values (opaque layouts)."""
-    codes: torch.Tensor     # uint8
-    scales: torch.Tensor    # uint8
-    rows: int
-    K: int
-    block: int = 0
+    """Activations quantized to MX4: `rows` rows of `K` values, rotated by blocks of `block`.
+    One uint8 buffer holds the codes, then the scales (opaque layouts)."""
+    __slots__ = ("data", "rows", "K", "block")
+
+    def __init__(self, data, rows, K, block=0):
+        self.data, self.rows, self.K, self.block = data, rows, K, block
+
+    @property
+    def codes(self):
+        return self.data[:_code_bytes(self.rows, self.K)]
+
+    @property
+    def scales(self):
+        c = _code_bytes(self.rows, self.K)
+        return self.data[c:c + _scale_bytes(self.rows, self.K)]
+
+    def __repr__(self):
+        return f"MX4(rows={self.rows}, K={self.K}, block={self.block})"
 
 
 @dataclass(slots=True)
@@ -81,25 +92,34 @@ class MX4Weight:
     gated: bool = False
 
 
-@dataclass(slots=True)
 class ExpertPlan:
-    """Assignments sorted by expert.  Expert e's rows start at offsets()[e], a multiple of 32."""
-    tokens: int
-    top_k: int
-    experts: int
-    plan_rows: int          # rows that buffers of a plan of this size have
-    tables: torch.Tensor    # int32
-    rows: torch.Tensor      # int32 [tokens, top_k], -1: no row
-    source: torch.Tensor    # int32 [plan_rows], the rows' tokens
+    """Assignments sorted by expert: `tokens` x `top_k` of them to `experts` experts, in buffers
+    of `plan_rows` rows.  One int32 buffer holds the tables, the rows and the sources."""
+    __slots__ = ("data", "tokens", "top_k", "experts", "plan_rows", "at_rows", "at_source")
+
+    def __init__(self, data, tokens, top_k, experts, plan_rows, ints):
+        self.data, self.tokens, self.top_k, self.experts, self.plan_rows = data, tokens, top_k, experts, plan_rows
+        self.at_rows, self.at_source = ints, ints + tokens * top_k
 
     @property
     def counts(self):
         """int32 [experts]: assignments of each expert."""
-        return self.tables[:self.experts]
+        return self.data[:self.experts]
+
+    @property
+    def rows(self):
+        """int32 [tokens, top_k]: the row of each assignment, -1 for none."""
+        return self.data[self.at_rows:self.at_source].view(self.tokens, self.top_k)
+
+    @property
+    def source(self):
+        """int32 [plan_rows]: the token of each row in use, -1 on padding."""
+        return self.data[self.at_source:]
 
     def offsets(self):
-        """int32 [experts + 1]: each expert's first row, and the end of the last one's."""
-        return 32 * self.tables[self.experts:2 * self.experts + 1]
+        """int32 [experts + 1]: each expert's first row, a multiple of 32, and the end of the last
+        one's."""
+        return 32 * self.data[self.experts:2 * self.experts + 1]
 
 
 def _dev(t, name, dtypes):
@@ -113,41 +133,44 @@ def _dev(t, name, dtypes):
 _HALF = (torch.float16, torch.bfloat16)
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+def _together(device, name, t):
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
 
 
 def _rows2d(X, name, dtypes=_HALF):
+    """Rows, columns, row stride of a matrix."""
     _dev(X, name, dtypes)
-    if X.dim() != 2 or X.stride(1) != 1:
+    if X.dim() != 2:
+        raise ValueError(f"{name} must be 2-D with unit column stride")
+    (M, K), (ld, step) = X.shape, X.stride()
+    if step != 1:
         raise ValueError(f"{name} must be 2-D with unit column stride")
     # (a single row has no stride of its own; torch gives such a view any)
-    return X.shape[0], X.shape[1], X.stride(0) if X.shape[0] > 1 else max(X.stride(0), -(-X.shape[1] // 8) * 8)
+    return M, K, ld if M > 1 else max(ld, -(-K // 8) * 8)
 
 
-class _On:
-    """The raw stream of a call; allocations inside belong to it."""
-    __slots__ = ("guard", "device", "given")
+def _gather(perm, K, device):
+    _together(device, "perm", _perm(perm, K))
+    return perm.data_ptr()
 
-    def __init__(self, device, stream):
-        self.device, self.given = device, stream
-        self.guard = None
 
-    def __enter__(self):
-        if self.given is None:
-            if torch.cuda.current_device() != self.device.index:
-                self.guard = torch.cuda.device(self.device)
-                self.guard.__enter__()
-            return _raw_stream(self.device.index)
-        self.guard = torch.cuda.stream(self.given)
-        self.guard.__enter__()
-        return self.given.cuda_stream
+# Every call runs on the current stream of its tensors' device.  One given a stream, or
+# tensors of another device, calls itself again with that made current, so that what it
+# allocates belongs there too.
+_current_device = torch.cuda.current_device
 
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+
+def _elsewhere(device, stream):
+    return torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
+
+
+def _code_bytes(rows, K):
+    return (rows + 31) // 32 * 32 * (K // 2)
+
+
+def _scale_bytes(rows, K):
+    return (rows + 31) // 32 * ((K + 255) // 256) * 256
 
 
 def clq_mx4_code_bytes(rows, K, weights=False):
@@ -158,18 +181,16 @@ def clq_mx4_scale_bytes(rows, K, weights=False):
     return _lib.clq_mx4_scale_bytes(rows, K, int(weights))
 
 
-def _buffers(out, rows, K, device, where, block=0):
+def _buffer(out, rows, K, block, device, where):
     """An MX4 of that shape: the caller's, checked, or a new one."""
-    cb, sb = _lib.clq_mx4_code_bytes(rows, K, 0), _lib.clq_mx4_scale_bytes(rows, K, 0)
-    if cb == 0:
+    if not 0 < rows < 2 ** 31 or not 64 <= K <= 32768 or K % 64:
         raise ClqError(CLQ_ERR_SHAPE, where)
+    n = _code_bytes(rows, K) + _scale_bytes(rows, K)
     if out is None:
-        return MX4(torch.empty(cb, dtype=torch.uint8, device=device),
-                   torch.empty(sb, dtype=torch.uint8, device=device), rows, K, block)
-    for t, n in ((out.codes, cb), (out.scales, sb)):
-        if _dev(t, "out", (torch.uint8,)).numel() < n or not t.is_contiguous():
-            raise ValueError("the output's buffers are too small")
-    _same_device(device, out=out.codes)
+        return MX4(torch.empty(n, dtype=torch.uint8, device=device), rows, K, block)
+    if _dev(out.data, "out", (torch.uint8,)).numel() < n or not out.data.is_contiguous():
+        raise ValueError("the output's buffer is too small")
+    _together(device, "out", out.data)
     out.rows, out.K, out.block = rows, K, block
     return out
 
@@ -177,14 +198,17 @@ def _buffers(out, rows, K, device, where, block=0):
 def clq_mx4_quantize(X, block=0, perm=None, out=None, stream=None):
     """Rotates each row by blocks of `block` (0: none), after gathering its columns by
     `perm`, and quantizes it to MX4.  X: fp16 or bf16 [M, K], any row stride that is a
-    multiple of 8.  out: an MX4 whose buffers are reused."""
+    multiple of 8.  out: an MX4 whose buffer is reused."""
     M, K, ldx = _rows2d(X, "X")
-    perm = _perm(perm, K)
-    _same_device(X.device, perm=perm)
-    with _On(X.device, stream) as s:
-        q = _buffers(out, M, K, X.device, "clq_mx4_quantize", block)
-        _check(_lib.clq_mx4_quantize(X.data_ptr(), _TYPES[X.dtype], ldx, _ptr(perm), M, K, block,
-                                     q.codes.data_ptr(), q.scales.data_ptr(), s), "clq_mx4_quantize")
+    device = X.device
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_mx4_quantize(X, block, perm, out)
+    q = _buffer(out, M, K, block, device, "clq_mx4_quantize")
+    p = q.data.data_ptr()
+    _check(_lib.clq_mx4_quantize(X.data_ptr(), _TYPES[X.dtype], ldx, None if perm is None else _gather(perm, K, device),
+                                 M, K, block, p, p + _code_bytes(M, K), _raw_stream(i)), "clq_mx4_quantize")
     return q
 
 
@@ -209,13 +233,15 @@ def clq_mx4_quantize_weights(W, block=0, perm=None, gated=False, stream=None):
     act="swiglu")."""
     _dev(W, "W", _HALF)
     experts, N, K = _weight_shape(W, "W")
-    perm = _perm(perm, K)
-    _same_device(W.device, perm=perm)
-    with _On(W.device, stream) as s:
-        qw = _weight(experts, N, K, block, perm, gated, W.device, "clq_mx4_quantize_weights")
-        _check(_lib.clq_mx4_quantize_weights(W.data_ptr(), _TYPES[W.dtype], _ptr(perm), experts or 1, N, K, block,
-                                             int(gated), qw.codes.data_ptr(), qw.scales.data_ptr(), s),
-               "clq_mx4_quantize_weights")
+    device = W.device
+    if stream is not None or _current_device() != device.index:
+        with _elsewhere(device, stream):
+            return clq_mx4_quantize_weights(W, block, perm, gated)
+    p = None if perm is None else _gather(perm, K, device)
+    qw = _weight(experts, N, K, block, perm, gated, device, "clq_mx4_quantize_weights")
+    _check(_lib.clq_mx4_quantize_weights(W.data_ptr(), _TYPES[W.dtype], p, experts or 1, N, K, block, int(gated),
+                                         qw.codes.data_ptr(), qw.scales.data_ptr(), _raw_stream(device.index)),
+           "clq_mx4_quantize_weights")
     return qw
 
 
@@ -225,15 +251,19 @@ def clq_mx4_pack_weights(codes, scales, block=0, perm=None, gated=False, stream=
     _dev(codes, "codes", (torch.uint8,))
     _dev(scales, "scales", (torch.uint8,))
     experts, N, half = _weight_shape(codes, "codes")
-    K = 2 * half
-    perm = _perm(perm, K)
+    K, device = 2 * half, codes.device
     if scales.shape != (*codes.shape[:-1], K // 32) or not scales.is_contiguous():
         raise ValueError("scales must be contiguous, one byte for 32 codes of each row")
-    _same_device(codes.device, scales=scales, perm=perm)
-    with _On(codes.device, stream) as s:
-        qw = _weight(experts, N, K, block, perm, gated, codes.device, "clq_mx4_pack_weights")
-        _check(_lib.clq_mx4_pack_weights(codes.data_ptr(), scales.data_ptr(), experts or 1, N, K, int(gated),
-                                         qw.codes.data_ptr(), qw.scales.data_ptr(), s), "clq_mx4_pack_weights")
+    _together(device, "scales", scales)
+    if perm is not None:
+        _gather(perm, K, device)
+    if stream is not None or _current_device() != device.index:
+        with _elsewhere(device, stream):
+            return clq_mx4_pack_weights(codes, scales, block, perm, gated)
+    qw = _weight(experts, N, K, block, perm, gated, device, "clq_mx4_pack_weights")
+    _check(_lib.clq_mx4_pack_weights(codes.data_ptr(), scales.data_ptr(), experts or 1, N, K, int(gated),
+                                     qw.codes.data_ptr(), qw.scales.data_ptr(), _raw_stream(device.index)),
+           "clq_mx4_pack_weights")
     return qw
 
 
@@ -242,23 +272,32 @@ def clq_mx4_dequantize(q, dtype=torch.float16, out=None, stream=None):
     [experts, N, K] of fp16, bf16 or fp32."""
     if dtype not in _TYPES:
         raise TypeError(f"dtype must be fp16, bf16 or fp32, got {dtype}")
-    w = isinstance(q, MX4Weight)
-    rows = q.N if w else q.rows
-    mats = (q.experts or 1) if w else 1
-    shape = (mats, rows, q.K) if w and q.experts else (rows, q.K)
-    with _On(q.codes.device, stream) as s:
-        if out is None:
-            out = torch.empty(shape, dtype=dtype, device=q.codes.device)
-        elif _dev(out, "out", (dtype,)).shape != shape or not out.is_contiguous():
+    K = q.K
+    if isinstance(q, MX4Weight):
+        w, gated, rows, mats = 1, int(q.gated), q.N, q.experts or 1
+        shape = (mats, rows, K) if q.experts else (rows, K)
+        device, c, s = q.codes.device, q.codes.data_ptr(), q.scales.data_ptr()
+    else:
+        w, gated, rows, mats, shape, device = 0, 0, q.rows, 1, (q.rows, K), q.data.device
+        c = q.data.data_ptr()
+        s = c + _code_bytes(rows, K)
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_mx4_dequantize(q, dtype, out)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    else:
+        if _dev(out, "out", (dtype,)).shape != shape or not out.is_contiguous():
             raise ValueError(f"out must be a contiguous {shape} tensor")
-        _same_device(q.codes.device, out=out)
-        _check(_lib.clq_mx4_dequantize(q.codes.data_ptr(), q.scales.data_ptr(), int(w), int(w and q.gated), mats, rows,
-                                       q.K, _TYPES[dtype], out.data_ptr(), q.K, s), "clq_mx4_dequantize")
+        _together(device, "out", out)
+    _check(_lib.clq_mx4_dequantize(c, s, w, gated, mats, rows, K, _TYPES[dtype], out.data_ptr(), K, _raw_stream(i)),
+           "clq_mx4_dequantize")
     return out
 
 
 def _product(q, qw, bias, experts):
-    """Checks the operands of a product; the bias's type."""
+    """Checks the operands of a product; their device, and the bias's pointer and type."""
     if not isinstance(q, MX4) or not isinstance(qw, MX4Weight):
         raise TypeError("the operands must be an MX4 and an MX4Weight")
     if q.K != qw.K:
@@ -267,13 +306,15 @@ def _product(q, qw, bias, experts):
         raise ValueError(f"inputs are rotated by blocks of {q.block}, weights by {qw.block}")
     if qw.experts != experts:
         raise ValueError(f"weights hold {qw.experts} experts, not {experts}")
-    _same_device(q.codes.device, weights=qw.codes, bias=bias)
+    device = q.data.device
+    _together(device, "weights", qw.codes)
     if bias is None:
-        return 0
+        return device, None, 0
     _dev(bias, "bias", _HALF)
     if bias.shape != ((qw.N,) if experts is None else (experts, qw.N)) or not bias.is_contiguous():
         raise ValueError("bias must be a contiguous [N] or [experts, N] tensor")
-    return _TYPES[bias.dtype]
+    _together(device, "bias", bias)
+    return device, bias.data_ptr(), _TYPES[bias.dtype]
 
 
 def _output(out, rows, N, dtype, device):
@@ -286,7 +327,7 @@ def _output(out, rows, N, dtype, device):
     r, n, ld = _rows2d(out, "out", (dtype,))
     if r < rows or n != N:
         raise ValueError(f"out must be [{rows}, {N}]")
-    _same_device(device, out=out)
+    _together(device, "out", out)
     return out, ld
 
 
@@ -304,14 +345,18 @@ def _columns(qw, act):
 
 def clq_mx4_linear(q, qw, bias=None, dtype=torch.float16, out=None, stream=None):
     """Y = X . W^T + bias, fp16 or bf16 [M, N]."""
-    bt = _product(q, qw, bias, None)
+    device, b, bt = _product(q, qw, bias, None)
     if qw.gated:
         raise ValueError("gated weights go with clq_mx4_linear_mx4(act='swiglu')")
-    with _On(q.codes.device, stream) as s:
-        Y, ld = _output(out, q.rows, qw.N, dtype, q.codes.device)
-        _check(_lib.clq_mx4_linear(q.codes.data_ptr(), q.scales.data_ptr(), qw.codes.data_ptr(), qw.scales.data_ptr(),
-                                   _ptr(bias), bt, q.rows, qw.N, qw.K, _TYPES[dtype], Y.data_ptr(), ld, s),
-               "clq_mx4_linear")
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_mx4_linear(q, qw, bias, dtype, out)
+    M, K, N = q.rows, q.K, qw.N
+    Y, ld = _output(out, M, N, dtype, device)
+    p = q.data.data_ptr()
+    _check(_lib.clq_mx4_linear(p, p + _code_bytes(M, K), qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, M, N, K,
+                               _TYPES[dtype], Y.data_ptr(), ld, _raw_stream(i)), "clq_mx4_linear")
     return Y
 
 
@@ -320,12 +365,16 @@ def clq_mx4_linear_mx4(q, qw, bias=None, act=None, block=0, out=None, stream=Non
     fp32 in between: the input of the next product.  act: None, "gelu" (tanh form) or "swiglu"
     (gated weights, N / 2 columns)."""
     a = _act(act)
-    bt = _product(q, qw, bias, None)
-    with _On(q.codes.device, stream) as s:
-        o = _buffers(out, q.rows, _columns(qw, a), q.codes.device, "clq_mx4_linear_mx4", block)
-        _check(_lib.clq_mx4_linear_mx4(q.codes.data_ptr(), q.scales.data_ptr(), qw.codes.data_ptr(),
-                                       qw.scales.data_ptr(), _ptr(bias), bt, q.rows, qw.N, qw.K, a, block,
-                                       o.codes.data_ptr(), o.scales.data_ptr(), s), "clq_mx4_linear_mx4")
+    device, b, bt = _product(q, qw, bias, None)
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_mx4_linear_mx4(q, qw, bias, act, block, out)
+    M, K, C = q.rows, q.K, _columns(qw, a)
+    o = _buffer(out, M, C, block, device, "clq_mx4_linear_mx4")
+    p, r = q.data.data_ptr(), o.data.data_ptr()
+    _check(_lib.clq_mx4_linear_mx4(p, p + _code_bytes(M, K), qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, M, qw.N,
+                                   K, a, block, r, r + _code_bytes(M, C), _raw_stream(i)), "clq_mx4_linear_mx4")
     return o
 
 
@@ -335,23 +384,31 @@ def clq_expert_route(logits, top_k, score="softmax", bias=None, groups=1, top_gr
     logits: fp32, fp16 or bf16 [T, experts].  score: "softmax" or "sigmoid".  bias: fp32
     [experts], added for the ranking alone.  groups, top_groups: only the experts of the best
     top_groups of `groups` groups take part.  scale multiplies the weights."""
-    _dev(logits, "logits", tuple(_TYPES))
-    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] != 1:
+    _dev(logits, "logits", _TYPES)
+    if logits.dim() != 2:
+        raise ValueError("logits must be 2-D with unit column stride")
+    (T, E), (ld, step) = logits.shape, logits.stride()
+    if step != 1 and E != 1:
         raise ValueError("logits must be 2-D with unit column stride")
     if score not in _SCORES:
         raise ValueError(f"score must be 'softmax' or 'sigmoid', not {score!r}")
-    T, E = logits.shape
+    device = logits.device
+    i = device.index
+    b = None
     if bias is not None:
         _dev(bias, "bias", (torch.float32,))
         if bias.shape != (E,) or not bias.is_contiguous():
             raise ValueError(f"bias must be a contiguous fp32 [{E}] tensor")
-        _same_device(logits.device, bias=bias)
-    with _On(logits.device, stream) as s:
-        ids = torch.empty((T, top_k), dtype=torch.int32, device=logits.device)
-        weights = torch.empty((T, top_k), dtype=torch.float32, device=logits.device)
-        _check(_lib.clq_expert_route(logits.data_ptr(), _TYPES[logits.dtype], max(logits.stride(0), E), T, E, top_k,
-                                     _SCORES[score], _ptr(bias), groups, top_groups, int(renormalize), scale,
-                                     ids.data_ptr(), weights.data_ptr(), s), "clq_expert_route")
+        _together(device, "bias", bias)
+        b = bias.data_ptr()
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_expert_route(logits, top_k, score, bias, groups, top_groups, renormalize, scale)
+    ids = torch.empty((T, top_k), dtype=torch.int32, device=device)
+    weights = torch.empty((T, top_k), dtype=torch.float32, device=device)
+    _check(_lib.clq_expert_route(logits.data_ptr(), _TYPES[logits.dtype], max(ld, E), T, E, top_k, _SCORES[score], b,
+                                 groups, top_groups, int(renormalize), scale, ids.data_ptr(), weights.data_ptr(),
+                                 _raw_stream(i)), "clq_expert_route")
     return ids, weights
 
 
@@ -374,20 +431,21 @@ def clq_expert_plan(ids, experts, stream=None):
     if ids.dim() != 2 or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous int32 [tokens, top_k] tensor")
     T, k = ids.shape
+    device = ids.device
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_expert_plan(ids, experts)
     n = _lib.clq_expert_plan_rows(T, k, experts)
     if n == 0:
         raise ClqError(CLQ_ERR_SHAPE, "clq_expert_plan")
     nt, nw = _lib.clq_expert_plan_ints(experts), _lib.clq_expert_plan_workspace_bytes(T, k, experts)
-    with _On(ids.device, stream) as s:
-        # the tables, the rows and the sources in one buffer
-        buf = torch.empty(nt + T * k + n, dtype=torch.int32, device=ids.device)
-        tables, rows, source = buf.split_with_sizes((nt, T * k, n))
-        ws = torch.empty(nw, dtype=torch.uint8, device=ids.device) if nw else None
-        plan = ExpertPlan(T, k, experts, n, tables, rows.view(T, k), source)
-        p = buf.data_ptr()
-        _check(_lib.clq_expert_plan(ids.data_ptr(), T, k, experts, p, p + 4 * nt, p + 4 * (nt + T * k), _ptr(ws), nw,
-                                    s), "clq_expert_plan")
-    return plan
+    data = torch.empty(nt + T * k + n, dtype=torch.int32, device=device)
+    ws = torch.empty(nw, dtype=torch.uint8, device=device) if nw else None
+    p = data.data_ptr()
+    _check(_lib.clq_expert_plan(ids.data_ptr(), T, k, experts, p, p + 4 * nt, p + 4 * (nt + T * k), _ptr(ws), nw,
+                                _raw_stream(i)), "clq_expert_plan")
+    return ExpertPlan(data, T, k, experts, n, nt)
 
 
 def clq_mx4_dispatch(X, plan, block=0, perm=None, out=None, stream=None):
@@ -395,49 +453,64 @@ def clq_mx4_dispatch(X, plan, block=0, perm=None, out=None, stream=None):
     T, K, ldx = _rows2d(X, "X")
     if T != plan.tokens:
         raise ValueError(f"X has {T} tokens, the plan {plan.tokens}")
-    perm = _perm(perm, K)
-    _same_device(X.device, perm=perm, plan=plan.tables)
-    with _On(X.device, stream) as s:
-        q = _buffers(out, plan.plan_rows, K, X.device, "clq_mx4_dispatch", block)
-        _check(_lib.clq_mx4_dispatch(X.data_ptr(), _TYPES[X.dtype], ldx, _ptr(perm), T, plan.top_k, plan.experts, K,
-                                     block, plan.tables.data_ptr(), plan.source.data_ptr(), q.codes.data_ptr(),
-                                     q.scales.data_ptr(), s), "clq_mx4_dispatch")
+    device = X.device
+    i = device.index
+    _together(device, "plan", plan.data)
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_mx4_dispatch(X, plan, block, perm, out)
+    g = None if perm is None else _gather(perm, K, device)
+    n = plan.plan_rows
+    q = _buffer(out, n, K, block, device, "clq_mx4_dispatch")
+    p, t = q.data.data_ptr(), plan.data.data_ptr()
+    _check(_lib.clq_mx4_dispatch(X.data_ptr(), _TYPES[X.dtype], ldx, g, T, plan.top_k, plan.experts, K, block, t,
+                                 t + 4 * plan.at_source, p, p + _code_bytes(n, K), _raw_stream(i)), "clq_mx4_dispatch")
     return q
 
 
-def _plan_operands(q, plan):
+def _plan_operands(q, plan, qw, bias):
+    r = _product(q, qw, bias, plan.experts)
     if q.rows != plan.plan_rows:
         raise ValueError(f"inputs have {q.rows} rows, the plan {plan.plan_rows}")
-    _same_device(q.codes.device, plan=plan.tables)
+    _together(r[0], "plan", plan.data)
+    return r
 
 
 def clq_mx4_experts(q, plan, qw, bias=None, dtype=None, out=None, stream=None):
     """Each row of the plan times its expert's weights: Y [plan.plan_rows, N], fp16 or bf16 (default:
     the bias's type, or fp16); rows past the last expert's are left as they were."""
-    bt = _product(q, qw, bias, plan.experts)
-    _plan_operands(q, plan)
+    device, b, bt = _plan_operands(q, plan, qw, bias)
     if qw.gated:
         raise ValueError("gated weights go with clq_mx4_experts_mx4(act='swiglu')")
-    dtype = dtype or (torch.float16 if bias is None else bias.dtype)
-    with _On(q.codes.device, stream) as s:
-        Y, ld = _output(out, q.rows, qw.N, dtype, q.codes.device)
-        _check(_lib.clq_mx4_experts(q.codes.data_ptr(), q.scales.data_ptr(), plan.tables.data_ptr(), plan.tokens,
-                                    plan.top_k, plan.experts, qw.codes.data_ptr(), qw.scales.data_ptr(), _ptr(bias),
-                                    bt, qw.N, qw.K, _TYPES[dtype], Y.data_ptr(), ld, s), "clq_mx4_experts")
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_mx4_experts(q, plan, qw, bias, dtype, out)
+    if dtype is None:
+        dtype = torch.float16 if bias is None else bias.dtype
+    M, K, N = q.rows, q.K, qw.N
+    Y, ld = _output(out, M, N, dtype, device)
+    p = q.data.data_ptr()
+    _check(_lib.clq_mx4_experts(p, p + _code_bytes(M, K), plan.data.data_ptr(), plan.tokens, plan.top_k, plan.experts,
+                                qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, N, K, _TYPES[dtype], Y.data_ptr(),
+                                ld, _raw_stream(i)), "clq_mx4_experts")
     return Y
 
 
 def clq_mx4_experts_mx4(q, plan, qw, bias=None, act=None, block=0, out=None, stream=None):
     """clq_mx4_linear_mx4 with each row times its expert's weights."""
     a = _act(act)
-    bt = _product(q, qw, bias, plan.experts)
-    _plan_operands(q, plan)
-    with _On(q.codes.device, stream) as s:
-        o = _buffers(out, q.rows, _columns(qw, a), q.codes.device, "clq_mx4_experts_mx4", block)
-        _check(_lib.clq_mx4_experts_mx4(q.codes.data_ptr(), q.scales.data_ptr(), plan.tables.data_ptr(), plan.tokens,
-                                        plan.top_k, plan.experts, qw.codes.data_ptr(), qw.scales.data_ptr(),
-                                        _ptr(bias), bt, qw.N, qw.K, a, block, o.codes.data_ptr(),
-                                        o.scales.data_ptr(), s), "clq_mx4_experts_mx4")
+    device, b, bt = _plan_operands(q, plan, qw, bias)
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_mx4_experts_mx4(q, plan, qw, bias, act, block, out)
+    M, K, C = q.rows, q.K, _columns(qw, a)
+    o = _buffer(out, M, C, block, device, "clq_mx4_experts_mx4")
+    p, r = q.data.data_ptr(), o.data.data_ptr()
+    _check(_lib.clq_mx4_experts_mx4(p, p + _code_bytes(M, K), plan.data.data_ptr(), plan.tokens, plan.top_k,
+                                    plan.experts, qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, qw.N, K, a, block,
+                                    r, r + _code_bytes(M, C), _raw_stream(i)), "clq_mx4_experts_mx4")
     return o
 
 
@@ -445,12 +518,18 @@ def clq_expert_combine(Y, plan, weights, out=None, stream=None):
     """out[t] = sum over the slots of weights[t, j] * Y[plan.rows[t, j]], in fp32, of Y's type."""
     r, N, ldy = _rows2d(Y, "Y")
     _dev(weights, "weights", (torch.float32,))
-    if r < plan.plan_rows or weights.shape != plan.rows.shape or not weights.is_contiguous():
+    T, k = plan.tokens, plan.top_k
+    if r < plan.plan_rows or weights.shape != (T, k) or not weights.is_contiguous():
         raise ValueError("Y and weights must have the plan's rows and slots")
-    _same_device(Y.device, weights=weights, plan=plan.tables)
-    with _On(Y.device, stream) as s:
-        o, ld = _output(out, plan.tokens, N, Y.dtype, Y.device)
-        _check(_lib.clq_expert_combine(Y.data_ptr(), _TYPES[Y.dtype], ldy, plan.rows.data_ptr(), weights.data_ptr(),
-                                       plan.tokens, plan.top_k, plan.experts, N, o.data_ptr(), ld, s),
-               "clq_expert_combine")
+    device = Y.device
+    i = device.index
+    _together(device, "weights", weights)
+    _together(device, "plan", plan.data)
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_expert_combine(Y, plan, weights, out)
+    o, ld = _output(out, T, N, Y.dtype, device)
+    _check(_lib.clq_expert_combine(Y.data_ptr(), _TYPES[Y.dtype], ldy, plan.data.data_ptr() + 4 * plan.at_rows,
+                                   weights.data_ptr(), T, k, plan.experts, N, o.data_ptr(), ld, _raw_stream(i)),
+           "clq_expert_combine")
     return o

@@ -160,7 +160,7 @@ def test_binding_refuses_host_tensors_and_wrong_kinds():
                  lambda: clq.clq_mx4_linear(x, x), lambda: clq.clq_mx4_dequantize(None, torch.int8)):
         with pytest.raises(TypeError):
             call()
-    a, w = clq.MX4(x, x, 4, 64, 64), clq.MX4Weight(x, x, 64, 64, 32)
+    a, w = clq.MX4(x, 4, 64, 64), clq.MX4Weight(x, x, 64, 64, 32)
     with pytest.raises(ValueError, match="rotated"):
         clq.clq_mx4_linear(a, w)
     w.block, w.K = 64, 128
