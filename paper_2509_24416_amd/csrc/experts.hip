@@ -105,9 +105,19 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
     // lanes of a group: the largest power of two that gives every group as many
     int per_group = 64;
     while (per_group * a.groups > 64) per_group >>= 1;
-    for (int64_t t = (int64_t)blockIdx.x * kRouteWaves + wave; t < a.T; t += (int64_t)gridDim.x * kRouteWaves) {
+    const bool by_logit = a.bias == nullptr && a.groups == 1;
+    float balance[VPL];
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) balance[v] = a.bias && lane * VPL + v < a.E ? a.bias[lane * VPL + v] : 0.0f;
+    const int64_t step = (int64_t)gridDim.x * kRouteWaves;
+    int64_t t = (int64_t)blockIdx.x * kRouteWaves + wave;
+    float next[VPL];
+    if (t < a.T) load_logits<VPL>(a, t, lane, next);
+    for (; t < a.T; t += step) {
         float x[VPL], score[VPL];
-        load_logits<VPL>(a, t, lane, x);
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) x[v] = next[v];
+        if (t + step < a.T) load_logits<VPL>(a, t + step, lane, next);
         bool nan = false;
 #pragma unroll
         for (int v = 0; v < VPL; ++v) nan |= x[v] != x[v];
@@ -133,15 +143,13 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
 #pragma unroll
             for (int v = 0; v < VPL; ++v) score[v] = score[v] / sum;
         }
-        const bool by_logit = a.bias == nullptr && a.groups == 1;
         uint32_t key[VPL];
-        int id[VPL];
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-            id[v] = lane * VPL + v;
-            const bool in = id[v] < a.E;
+            const int e = lane * VPL + v;
+            const bool in = e < a.E;
             float r = by_logit ? x[v] : score[v];
-            if (a.bias) r = score[v] + (in ? a.bias[id[v]] : 0.0f);
+            if (a.bias) r = score[v] + balance[v];
             key[v] = in ? order_of(r == r ? r : kNone) : 0u;
         }
 #pragma unroll
@@ -176,40 +184,48 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
             }
             const uint64_t kept = __ballot(g < a.groups && before < a.top_groups);
 #pragma unroll
-            for (int v = 0; v < VPL; ++v)
-                if (id[v] < a.E && !((kept >> (id[v] / gs * per_group)) & 1)) key[v] = 0;
+            for (int v = 0; v < VPL; ++v) {
+                const int e = min(lane * VPL + v, a.E - 1);
+                key[v] = (kept >> (e / gs * per_group)) & 1 ? key[v] : 0u;
+            }
         }
-        // the lane's experts, best first (an equal one stays behind: its index is higher)
+        // the lane's experts, best first (an equal one stays behind: its index is higher);
+        // their places, four bits each, go along
+        uint32_t place[VPL];
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) place[v] = (uint32_t)v;
 #pragma unroll
         for (int i = 1; i < VPL; ++i)
 #pragma unroll
             for (int j = i; j > 0; --j) {
-                const bool swap = key[j] > key[j - 1];
-                const uint32_t hi = swap ? key[j] : key[j - 1], lo = swap ? key[j - 1] : key[j];
-                const int hid = swap ? id[j] : id[j - 1], lid = swap ? id[j - 1] : id[j];
-                key[j - 1] = hi; key[j] = lo;
-                id[j - 1] = hid; id[j] = lid;
+                const uint32_t d = key[j] > key[j - 1] ? place[j] ^ place[j - 1] : 0u;
+                const uint32_t hi = max(key[j], key[j - 1]), lo = min(key[j], key[j - 1]);
+                key[j - 1] = hi;
+                key[j] = lo;
+                place[j - 1] ^= d;
+                place[j] ^= d;
             }
+        uint32_t order = 0;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) order |= place[v] << (4 * v);
         int my_id = 0;
         for (int j = 0; j < a.k; ++j) {
             const uint32_t top = wave_max(key[0]);
             const int from = __ffsll((unsigned long long)__ballot(key[0] == top)) - 1;
-            const int got = __builtin_amdgcn_readlane(id[0], from);
+            const int got = from * VPL + (__builtin_amdgcn_readlane((int)order, from) & 15);
             my_id = lane == j ? got : my_id;
-            const bool pop = lane == from;
+            // the winner's lane moves its experts up
+            const uint32_t pop = lane == from ? ~0u : 0u;
 #pragma unroll
-            for (int v = 0; v + 1 < VPL; ++v) {
-                key[v] = pop ? key[v + 1] : key[v];
-                id[v] = pop ? id[v + 1] : id[v];
-            }
-            key[VPL - 1] = pop ? 0u : key[VPL - 1];
+            for (int v = 0; v + 1 < VPL; ++v) key[v] = (key[v + 1] & pop) | (key[v] & ~pop);
+            key[VPL - 1] &= ~pop;
+            order = ((order >> 4) & pop) | (order & ~pop);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         float w = lane < a.k ? scores[my_id] : 0.0f;
         if (a.renormalize) {
             float total = w;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) total += __shfl_xor(total, o);   // (k is 32 at most)
+            for (int o = 1; o < a.k; o <<= 1) total += __shfl_xor(total, o);   // (0 past the k-th lane)
             // (a total of 0, where every score is, leaves weights of 0)
             w = total > 0.0f ? w / total : total == 0.0f ? 0.0f : total;
         }
@@ -279,6 +295,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
             const int line = tid / width, e = e0 + tid - line * width;
             if (line < lines) {
                 int sum = 0, before = 0;
+#pragma unroll 8
                 for (int r = line; r < runs; r += lines) {
                     const int c = hist[(int64_t)r * E + e];
                     sum += c;
@@ -411,8 +428,9 @@ hipError_t launch_expert_route(const void *logits, MxType type, int64_t ld, int6
                                const float *bias, int groups, int top_groups, bool renormalize, float scale,
                                int32_t *ids, float *weights, hipStream_t stream) {
     const RouteArgs a = {logits, type, ld, T, E, k, groups, top_groups, sigmoid, renormalize, bias, scale, ids, weights};
-    const int64_t want = (T + kRouteWaves - 1) / kRouteWaves;
-    const dim3 grid((unsigned)(want < (1 << 20) ? want : 1 << 20)), block(64 * kRouteWaves);
+    // as many waves as the chip holds, each with every so-many-th token
+    const int64_t want = (T + kRouteWaves - 1) / kRouteWaves, most = (int64_t)compute_units() * 8;
+    const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kRouteWaves);
     if (E <= 64) hipLaunchKernelGGL((route_kernel<1>), grid, block, 0, stream, a);
     else if (E <= 128) hipLaunchKernelGGL((route_kernel<2>), grid, block, 0, stream, a);
     else if (E <= 256) hipLaunchKernelGGL((route_kernel<4>), grid, block, 0, stream, a);

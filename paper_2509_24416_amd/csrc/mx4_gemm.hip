@@ -87,12 +87,12 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b) {
     return __builtin_bit_cast(uint32_t, v);
 }
 
-// The tanh form of GELU: 0.5 h (1 + tanh u) = h / (1 + exp(-2u)).  The hardware's exp2
-// and reciprocal (1 ulp each) keep the relative error near 3e-7, under that of the
-// sum it is applied to.
+// The tanh form of GELU: 0.5 h (1 + tanh u) = h / (1 + exp(-2u)), the exponent's constants
+// times log2 e.  The hardware's exp2 and reciprocal (1 ulp each) keep the relative error near
+// 3e-7, under that of the sum it is applied to.
 __device__ __forceinline__ float gelu(float h) {
-    const float u2 = h * (1.5957691216057308f + 0.07135481282553575f * h * h);   // 2u
-    return h * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u2));
+    const float t = h * __builtin_fmaf(-0.10294324f, h * h, -2.3022082f);   // -2u log2 e
+    return h * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
 }
 __device__ __forceinline__ float silu(float g) {
     return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g));
@@ -143,7 +143,7 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 // needed at the end of quad q + 1.  Transfers past the end repeat the last stage or quad,
 // so the wait counts stay constant.
 constexpr int kBN = 128;
-constexpr int kStages = 5;                      // ring of channel units
+constexpr int kStages = 8;                      // ring of channel units
 constexpr int kStageBytes = 4 * kMxUnit;        // 4 / NW units transferred by each wave
 constexpr int kQuadBytes = 4 * kMxScaleRow;
 constexpr int kDepth = 4;                       // stages of token units in registers

@@ -158,7 +158,7 @@ def _gather(perm, K, device):
 # Every call runs on the current stream of its tensors' device.  One given a stream, or
 # tensors of another device, calls itself again with that made current, so that what it
 # allocates belongs there too.
-_current_device = torch.cuda.current_device
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _elsewhere(device, stream):
@@ -286,7 +286,7 @@ def clq_mx4_dequantize(q, dtype=torch.float16, out=None, stream=None):
         with _elsewhere(device, stream):
             return clq_mx4_dequantize(q, dtype, out)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
+        out = torch.empty(*shape, dtype=dtype, device=device)
     else:
         if _dev(out, "out", (dtype,)).shape != shape or not out.is_contiguous():
             raise ValueError(f"out must be a contiguous {shape} tensor")
@@ -322,7 +322,7 @@ def _output(out, rows, N, dtype, device):
         raise TypeError(f"dtype must be fp16 or bf16, got {dtype}")
     if out is None:   # rows on 16-byte boundaries
         ld = (N + 7) // 8 * 8
-        out = torch.empty((rows, ld), dtype=dtype, device=device)
+        out = torch.empty(rows, ld, dtype=dtype, device=device)
         return (out if ld == N else out[:, :N]), ld
     r, n, ld = _rows2d(out, "out", (dtype,))
     if r < rows or n != N:
@@ -404,8 +404,8 @@ def clq_expert_route(logits, top_k, score="softmax", bias=None, groups=1, top_gr
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
             return clq_expert_route(logits, top_k, score, bias, groups, top_groups, renormalize, scale)
-    ids = torch.empty((T, top_k), dtype=torch.int32, device=device)
-    weights = torch.empty((T, top_k), dtype=torch.float32, device=device)
+    ids = torch.empty(T, top_k, dtype=torch.int32, device=device)
+    weights = torch.empty(T, top_k, dtype=torch.float32, device=device)
     _check(_lib.clq_expert_route(logits.data_ptr(), _TYPES[logits.dtype], max(ld, E), T, E, top_k, _SCORES[score], b,
                                  groups, top_groups, int(renormalize), scale, ids.data_ptr(), weights.data_ptr(),
                                  _raw_stream(i)), "clq_expert_route")
