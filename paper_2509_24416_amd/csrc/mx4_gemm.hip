@@ -143,10 +143,12 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 // needed at the end of quad q + 1.  Transfers past the end repeat the last stage or quad,
 // so the wait counts stay constant.
 constexpr int kBN = 128;
-constexpr int kStages = 8;                      // ring of channel units
 constexpr int kStageBytes = 4 * kMxUnit;        // 4 / NW units transferred by each wave
 constexpr int kQuadBytes = 4 * kMxScaleRow;
 constexpr int kDepth = 4;                       // stages of token units in registers
+// Ring of channel units: one more than kDepth, so that the stages that the prologue leaves in
+// flight are as many transfers and loads as the loop's wait counts take them for.
+constexpr int kStages = kDepth + 1;
 
 struct Operands {
     v4u w[4];
@@ -406,6 +408,7 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
     static_for<0, NS>([&](auto qc) {
         constexpr int Q = decltype(qc)::value;
         produce(Q * kStageBytes, Q);
+        __builtin_amdgcn_sched_barrier(0);   // (the loop's first wait counts rely on this order)
         if constexpr (Q < kDepth) load_x(qc, Q);
         __builtin_amdgcn_sched_barrier(0);
     });
@@ -492,42 +495,44 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
 
 // ---- few rows ----------------------------------------------------------------------------
 // With few tiles of the kernel above most compute units are idle and a launch takes the
-// length of one wave's k loop.  Here a workgroup computes 32 rows x 32 FN channels, its KS
+// length of one wave's k loop.  Here a workgroup computes 32 FM rows x 32 FN channels, its KS
 // waves each a part of the k loop with operands straight from memory (nothing is shared
 // between them), kAhead stages ahead; the partial sums meet in LDS.  A plain result needs no
-// channel but its own (FN = 1: the most workgroups), a requantized one the channels of a
-// rotation block (FN = 4).
-template <int FN, bool MX4>
+// channel but its own: 1 x 1 fragments make the most workgroups, 2 x 2 read half the operand
+// bytes an instruction.  A requantized one needs the channels of a rotation block (FN = 4).
+template <int FN_, int FM_, int KS_, int AHEAD>
 struct Split {
-    static constexpr int KS = FN == 1 ? 8 : 4, NT = KS * 64, BN = 32 * FN, kAhead = FN == 1 ? 6 : 3;
+    static constexpr int FN = FN_, FM = FM_, KS = KS_, kAhead = AHEAD, NT = KS * 64, BN = 32 * FN, BM = 32 * FM;
     static constexpr int kPitch = BN + 4;   // floats between rows of a partial tile, for the banks
 };
-template <Out OUT> using SplitOf = Split<OUT == Out::Plain ? 1 : 4, OUT != Out::Plain>;
+using Split1 = Split<1, 1, 8, 6>;
+using Split2 = Split<2, 2, 4, 4>;
+using SplitMx = Split<4, 1, 4, 3>;
 
-template <Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
-__global__ void __launch_bounds__(SplitOf<OUT>::NT) mx_split_kernel(Args a)
+template <class C, Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+__global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
 {
     constexpr bool MX4 = OUT != Out::Plain, GATED = OUT == Out::Swiglu;
-    constexpr int FN = MX4 ? 4 : 1;
-    using C = SplitOf<OUT>;
-    constexpr int KS = C::KS, D = C::kAhead;
-    __shared__ __align__(16) float part[KS][32 * C::kPitch];
+    constexpr int FN = C::FN, FM = C::FM, KS = C::KS, D = C::kAhead;
+    static_assert(!MX4 || (FN == 4 && FM == 1), "a requantized tile");
+    __shared__ __align__(16) float part[KS][C::BM * C::kPitch];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nks = a.K >> 6, nq = (a.K + 255) >> 8;
-    int tn, u;
+    int tn;
     RowTile rt;
     if constexpr (GROUPED) {
-        const int total = a.info[plan_table_offset(a.experts, 0) + a.experts] * a.tiles_n;
+        const int total = a.info[plan_table_offset(a.experts, a.log_units) + a.experts] * a.tiles_n;
         if ((int)blockIdx.x >= total) return;
         tn = blockIdx.x % a.tiles_n;
         rt = find_tile(a, blockIdx.x / a.tiles_n, lane);
-        u = rt.unit0;
     } else {
         tn = blockIdx.x % a.tiles_n;
-        u = blockIdx.x / a.tiles_n;
+        rt.unit0 = blockIdx.x / a.tiles_n * FM;
+        rt.unit_end = a.xunits;
         rt.expert = 0;
     }
+    const int u = rt.unit0;
     // this wave's stages; bytes of a scale row: lane's dword, then the stage's byte
     const int kb = wave * nks / KS, ke = (wave + 1) * nks / KS;
     const uint8_t *wsrc[FN], *wssrc[FN];
@@ -537,14 +542,21 @@ __global__ void __launch_bounds__(SplitOf<OUT>::NT) mx_split_kernel(Args a)
         wsrc[f] = a.Wq + rt.expert * a.w_stride + wu * nks * kMxUnit + lane * 16;
         wssrc[f] = a.Ws + rt.expert * a.ws_stride + wu * nq * kMxScaleRow + lane * 4;
     }
-    const uint8_t *xsrc = a.Xq + (int64_t)u * nks * kMxUnit + lane * 16;
-    const uint8_t *xssrc = a.Xs + (int64_t)u * nq * kMxScaleRow + lane * 4;
-    v16f acc[FN];
+    const uint8_t *xsrc[FM], *xssrc[FM];
 #pragma unroll
-    for (int f = 0; f < FN; ++f) acc[f] = v16f{};
+    for (int f = 0; f < FM; ++f) {
+        const int64_t xu = min(u + f, rt.unit_end - 1);
+        xsrc[f] = a.Xq + xu * nks * kMxUnit + lane * 16;
+        xssrc[f] = a.Xs + xu * nq * kMxScaleRow + lane * 4;
+    }
+    v16f acc[FN][FM];
+#pragma unroll
+    for (int f = 0; f < FN; ++f)
+#pragma unroll
+        for (int g = 0; g < FM; ++g) acc[f][g] = v16f{};
     if (kb < ke) {
-        v4u w[D][FN], x[D];
-        uint8_t ws[D][FN], xs[D];
+        v4u w[D][FN], x[D][FM];
+        uint8_t ws[D][FN], xs[D][FM];
         auto load = [&](auto dc, int k) __attribute__((always_inline)) {
             constexpr int d = decltype(dc)::value;
             const uint32_t off = (uint32_t)k * kMxUnit, soff = (uint32_t)(k >> 2) * kMxScaleRow + (k & 3);
@@ -553,13 +565,18 @@ __global__ void __launch_bounds__(SplitOf<OUT>::NT) mx_split_kernel(Args a)
                 w[d][f] = *reinterpret_cast<const v4u *>(wsrc[f] + off);
                 ws[d][f] = wssrc[f][soff];
             }
-            x[d] = *reinterpret_cast<const v4u *>(xsrc + off);
-            xs[d] = xssrc[soff];
+#pragma unroll
+            for (int f = 0; f < FM; ++f) {
+                x[d][f] = *reinterpret_cast<const v4u *>(xsrc[f] + off);
+                xs[d][f] = xssrc[f][soff];
+            }
         };
         auto mma = [&](auto dc) __attribute__((always_inline)) {
             constexpr int d = decltype(dc)::value;
 #pragma unroll
-            for (int f = 0; f < FN; ++f) acc[f] = mfma_mx4<0>(w[d][f], x[d], acc[f], ws[d][f], xs[d]);
+            for (int f = 0; f < FN; ++f)
+#pragma unroll
+                for (int g = 0; g < FM; ++g) acc[f][g] = mfma_mx4<0>(w[d][f], x[d][g], acc[f][g], ws[d][f], xs[d][g]);
         };
         const int last = ke - 1;   // loads past the end repeat the last stage
         static_for<0, D>([&](auto dc) {
@@ -584,38 +601,44 @@ __global__ void __launch_bounds__(SplitOf<OUT>::NT) mx_split_kernel(Args a)
     // lane's 16 channels of its row
     const int row = lane & 31, h16 = (lane >> 5) * 16;
 #pragma unroll
-    for (int f = 0; f < FN; ++f) {
-        v4f *dst = reinterpret_cast<v4f *>(&part[wave][row * C::kPitch + f * 32 + h16]);
+    for (int f = 0; f < FN; ++f)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) dst[q] = v4f{acc[f][4 * q], acc[f][4 * q + 1], acc[f][4 * q + 2], acc[f][4 * q + 3]};
-    }
+        for (int g = 0; g < FM; ++g) {
+            v4f *dst = reinterpret_cast<v4f *>(&part[wave][(g * 32 + row) * C::kPitch + f * 32 + h16]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                dst[q] = v4f{acc[f][g][4 * q], acc[f][g][4 * q + 1], acc[f][g][4 * q + 2], acc[f][g][4 * q + 3]};
+        }
     __syncthreads();
     const uint16_t *bias = a.bias ? a.bias + (int64_t)rt.expert * a.N : nullptr;
     if constexpr (!MX4) {
-        // eight channels of a row per thread
-        const int r = tid >> 2, c = (tid & 3) * 8, n = tn * C::BN + c;
-        const int64_t m = (int64_t)u * 32 + r;
-        if (r >= 32 || n >= a.N || (!GROUPED && m >= a.M)) return;
-        float s[8] = {};
+        // eight channels of a row at a time
+        constexpr int kPieces = C::BN / 8;
+        for (int p = tid; p < C::BM * kPieces; p += C::NT) {
+            const int r = p / kPieces, c = (p % kPieces) * 8, n = tn * C::BN + c;
+            const int64_t m = (int64_t)u * 32 + r;
+            if (n >= a.N || m >= (GROUPED ? (int64_t)rt.unit_end * 32 : (int64_t)a.M)) continue;
+            float s[8] = {};
 #pragma unroll
-        for (int w = 0; w < KS; ++w) {
-            const v4f *src = reinterpret_cast<const v4f *>(&part[w][r * C::kPitch + c]);
+            for (int w = 0; w < KS; ++w) {
+                const v4f *src = reinterpret_cast<const v4f *>(&part[w][r * C::kPitch + c]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += src[e >> 2][e & 3];
-        }
-        if (bias) {
+                for (int e = 0; e < 8; ++e) s[e] += src[e >> 2][e & 3];
+            }
+            if (bias) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += widen(bias[min(n + e, a.N - 1)], a.bias_bf16);
-        }
-        const v4u v = {narrow2<BF16>(s[0], s[1]), narrow2<BF16>(s[2], s[3]), narrow2<BF16>(s[4], s[5]),
-                       narrow2<BF16>(s[6], s[7])};
-        uint16_t *dst = a.Y + m * a.ldy + n;
-        if (!RAGGED || n <= a.N - 8) {
-            *reinterpret_cast<v4u *>(dst) = v;
-        } else {
+                for (int e = 0; e < 8; ++e) s[e] += widen(bias[min(n + e, a.N - 1)], a.bias_bf16);
+            }
+            const v4u v = {narrow2<BF16>(s[0], s[1]), narrow2<BF16>(s[2], s[3]), narrow2<BF16>(s[4], s[5]),
+                           narrow2<BF16>(s[6], s[7])};
+            uint16_t *dst = a.Y + m * a.ldy + n;
+            if (!RAGGED || n <= a.N - 8) {
+                *reinterpret_cast<v4u *>(dst) = v;
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (n + e < a.N) dst[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                for (int e = 0; e < 8; ++e)
+                    if (n + e < a.N) dst[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+            }
         }
     } else {
         // wave 0 .. NW - 1: the fragments of a rotation block each, summed in the products' layout
@@ -654,19 +677,31 @@ __global__ void __launch_bounds__(SplitOf<OUT>::NT) mx_split_kernel(Args a)
     }
 }
 
-// The kernels: 32-row units split over the k loop, tiles of 128 and of 256 rows.
-enum Kernel { kSplit, kTile128, kTile256 };
+// The kernels: tiles of 32 and 64 rows split over the k loop, of 128 and of 256 rows.
+enum Kernel { kSplit1, kSplit2, kTile128, kTile256 };
+constexpr int kLogUnits[] = {0, 1, 2, 3};   // row units of a tile
 
 template <Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
 void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
-    const int bn = kernel == kSplit ? SplitOf<OUT>::BN : kBN;
+    using S1 = std::conditional_t<OUT == Out::Plain, Split1, SplitMx>;
+    using S2 = std::conditional_t<OUT == Out::Plain && !GROUPED, Split2, S1>;
+    const int bn = kernel == kSplit1 ? S1::BN : kernel == kSplit2 ? S2::BN : kBN;
     a.tiles_n = (a.N + bn - 1) / bn;
     const dim3 grid((unsigned)(row_tiles * a.tiles_n));
-    if (kernel == kSplit)
-        hipLaunchKernelGGL((mx_split_kernel<OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(SplitOf<OUT>::NT), 0, stream, a);
-    else if (kernel == kTile128)
-        hipLaunchKernelGGL((mx_tile_kernel<2, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(128), 0, stream, a);
-    else hipLaunchKernelGGL((mx_tile_kernel<4, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(256), 0, stream, a);
+    switch (kernel) {
+        case kSplit1:
+            hipLaunchKernelGGL((mx_split_kernel<S1, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(S1::NT), 0, stream, a);
+            break;
+        case kSplit2:
+            hipLaunchKernelGGL((mx_split_kernel<S2, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(S2::NT), 0, stream, a);
+            break;
+        case kTile128:
+            hipLaunchKernelGGL((mx_tile_kernel<2, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(128), 0, stream, a);
+            break;
+        case kTile256:
+            hipLaunchKernelGGL((mx_tile_kernel<4, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(256), 0, stream, a);
+            break;
+    }
 }
 
 template <Out OUT, int B, bool GROUPED>
@@ -707,26 +742,37 @@ hipError_t launch_out(const Args &a, MxAct act, int block, Kernel kernel, int64_
     return hipGetLastError();
 }
 
-// The kernel of a product, by the workgroups it would be cut into (c compute units; a
-// plan's row units at most, which a few tokens nearly reach).  us, split / 128 / 256 rows:
-//   split   plain results up to 2 c workgroups of 32 channels (256 x 1152 -> 1152, 288 of
-//           them: 6.0 / 6.5 / 7.2; 512 x 1152 -> 2304, 1152: 9.6 / 7.1 / 7.4), long k loops
-//           up to 3 c (777 x 4608 -> 1152, 900: 14.0 / 14.5 / 15.7; 1024, 1152: 16.9 / 14.5 /
-//           15.7; 64 tokens to 2 of 16 experts 13.2 / 14.6 / 16.4, 256 tokens 16.5 / 15.6 /
-//           17.5); requantized ones up to 1.75 c of 128 channels (384 x 1152 -> 4608, 432: 8.8
-//           / 10.7 / 12.8; 512, 576: 12.1 / 10.9 / 11.4), where one wave finishes a tile
-//           whose channels gate each other up to c (8 tokens to 6 of 64 experts, 1152 -> 1536,
-//           588: 14.9 / 10.3 / 11.2);
-//   128     while those tiles are one to a unit (1024 x 4608 -> 1152, 72 of them: 14.5 / 15.7;
-//           1024 x 1152 -> 4608, 288: 9.9 / 8.2), and for experts of under 512 rows on average,
-//           whose last tiles are half empty (384 rows, 1152 -> 1536 gated: 38.5 / 41.8; 512
-//           rows, 1152 -> 4608: 51.6 / 50.2; 5400: 405 / 399);
-//   256     otherwise: the fewest operand bytes (43200 x 1152 -> 4608 189 / 171).
+// The kernel of a product, by the workgroups it would be cut into (c compute units; of a
+// plan the row units it can have at most, which a few tokens nearly reach).  us, measured
+// on tiles of 32 / 64 (both split) / 128 / 256 rows:
+//   32   one row unit, plain, up to 2 c workgroups (3 c on long k loops): 1 x 4608 -> 1152
+//        6.2 / - / 12.9 / 14.3; experts, 2 tokens to 2 of 16, 4608 -> 1152, 144 workgroups:
+//        7.5 / - / 13.5 / 14.7, 64 tokens, 720: 13.1 / - / 14.8 / 16.4, 256, 1152: 16.4 / - /
+//        15.7 / 17.5.  Requantized, up to 1.75 c: 384 x 1152 -> 4608, 432: 8.8 / - / 10.7 /
+//        12.8; 512, 576: 12.1 / - / 10.9 / 11.4; where one wave finishes a tile whose
+//        channels gate each other, up to c: 8 tokens to 6 of 64 experts, 1152 -> 1536, 588:
+//        14.9 / - / 10.3 / 11.2.
+//   64   more units, plain, while every workgroup has a unit to itself: 777 x 4608 -> 1152,
+//        234: 13.4 / 8.5 / 13.8 / 15.5; 512 x 1152 -> 1152, 144: 7.1 / 6.3 / 6.6 / 7.3; 512 x
+//        1152 -> 2304, 288: 9.8 / 7.7 / 6.9 / 7.3; on long k loops up to 1.75 c: 1536 x 4608 ->
+//        1152, 432: 22.1 / 13.8 / 14.4 / 15.8, 2048, 576: 27.5 / 18.7 / 14.8 / 16.1.
+//   128  while those tiles are one to a unit (3072 x 4608 -> 1152, 216: 40.9 / 23.8 / 15.8 /
+//        17.2; 4096, 288: 51.4 / 28.6 / 24.2 / 18.0), and for experts of under 512 rows on
+//        average, whose last tiles are half empty (384 rows, 1152 -> 1536 gated: 38.5 of 128 /
+//        41.8 of 256; 512 rows, 1152 -> 4608: 51.6 / 50.2; 5400: 405 / 399);
+//   256  otherwise: the fewest operand bytes (43200 x 1152 -> 4608: 189 of 128 / 171 of 256).
 inline Kernel pick_kernel(const MxGemmArgs &g, int64_t units, int64_t c) {
-    const bool mx4 = g.Y == nullptr;
-    const int64_t split = units * ((g.N + (mx4 ? 127 : 31)) / (mx4 ? 128 : 32));
-    const int64_t most = mx4 ? (g.act == MxAct::Swiglu ? c : c * 7 / 4) : (g.K >= 48 * 64 ? 3 * c : 2 * c);
-    if (split <= most) return kSplit;
+    const bool mx4 = g.Y == nullptr, longk = g.K >= 48 * 64;
+    if (mx4) {
+        const int64_t split = units * ((g.N + SplitMx::BN - 1) / SplitMx::BN);
+        if (split <= (g.act == MxAct::Swiglu ? c : c * 7 / 4)) return kSplit1;
+    } else if (g.info || units == 1) {
+        const int64_t split = units * ((g.N + Split1::BN - 1) / Split1::BN);
+        if (split <= (longk ? 3 * c : 2 * c)) return kSplit1;
+    } else {
+        const int64_t split = (units + 1) / 2 * ((g.N + Split2::BN - 1) / Split2::BN);
+        if (split <= (longk ? c * 7 / 4 : c)) return kSplit2;
+    }
     const int64_t tiles_n = (g.N + kBN - 1) / kBN;
     if (g.info) {
         const int64_t nonempty = g.experts < g.assignments ? g.experts : g.assignments;
@@ -761,7 +807,7 @@ hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
     a.oK = (int)(g.act == MxAct::Swiglu ? g.N / 2 : g.N);
     a.xunits = (int)(g.info ? g.units : padded_act_rows(g.M) >> 5);
     const mx::Kernel kernel = mx::pick_kernel(g, a.xunits, compute_units());
-    a.log_units = kernel == mx::kSplit ? 0 : kernel == mx::kTile128 ? 2 : 3;
+    a.log_units = mx::kLogUnits[kernel];
     const int64_t per = 1 << a.log_units;
     if (g.info) {
         // every expert's last tile may be a part of one

@@ -143,11 +143,12 @@ def _rows2d(X, name, dtypes=_HALF):
     _dev(X, name, dtypes)
     if X.dim() != 2:
         raise ValueError(f"{name} must be 2-D with unit column stride")
-    (M, K), (ld, step) = X.shape, X.stride()
+    M, K = X.shape
+    ld, step = X.stride()
     if step != 1:
         raise ValueError(f"{name} must be 2-D with unit column stride")
     # (a single row has no stride of its own; torch gives such a view any)
-    return M, K, ld if M > 1 else max(ld, -(-K // 8) * 8)
+    return M, K, ld if M > 1 else (K + 7) & ~7
 
 
 def _gather(perm, K, device):
@@ -182,17 +183,24 @@ def clq_mx4_scale_bytes(rows, K, weights=False):
 
 
 def _buffer(out, rows, K, block, device, where):
-    """An MX4 of that shape: the caller's, checked, or a new one."""
-    if not 0 < rows < 2 ** 31 or not 64 <= K <= 32768 or K % 64:
+    """An MX4 of that shape, the caller's, checked, or a new one; its codes' and scales'
+    pointers."""
+    if not 0 < rows < 2147483648 or not 64 <= K <= 32768 or K & 63:
         raise ClqError(CLQ_ERR_SHAPE, where)
-    n = _code_bytes(rows, K) + _scale_bytes(rows, K)
+    units = (rows + 31) >> 5
+    codes = units * K << 4
+    n = codes + (units * ((K + 255) >> 8) << 8)
     if out is None:
-        return MX4(torch.empty(n, dtype=torch.uint8, device=device), rows, K, block)
-    if _dev(out.data, "out", (torch.uint8,)).numel() < n or not out.data.is_contiguous():
-        raise ValueError("the output's buffer is too small")
-    _together(device, "out", out.data)
-    out.rows, out.K, out.block = rows, K, block
-    return out
+        data = torch.empty(n, dtype=torch.uint8, device=device)
+        out = MX4(data, rows, K, block)
+    else:
+        data = _dev(out.data, "out", (torch.uint8,))
+        if data.numel() < n or not data.is_contiguous():
+            raise ValueError("the output's buffer is too small")
+        _together(device, "out", data)
+        out.rows, out.K, out.block = rows, K, block
+    p = data.data_ptr()
+    return out, p, p + codes
 
 
 def clq_mx4_quantize(X, block=0, perm=None, out=None, stream=None):
@@ -205,10 +213,9 @@ def clq_mx4_quantize(X, block=0, perm=None, out=None, stream=None):
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
             return clq_mx4_quantize(X, block, perm, out)
-    q = _buffer(out, M, K, block, device, "clq_mx4_quantize")
-    p = q.data.data_ptr()
+    q, codes, scales = _buffer(out, M, K, block, device, "clq_mx4_quantize")
     _check(_lib.clq_mx4_quantize(X.data_ptr(), _TYPES[X.dtype], ldx, None if perm is None else _gather(perm, K, device),
-                                 M, K, block, p, p + _code_bytes(M, K), _raw_stream(i)), "clq_mx4_quantize")
+                                 M, K, block, codes, scales, _raw_stream(i)), "clq_mx4_quantize")
     return q
 
 
@@ -371,10 +378,10 @@ def clq_mx4_linear_mx4(q, qw, bias=None, act=None, block=0, out=None, stream=Non
         with _elsewhere(device, stream):
             return clq_mx4_linear_mx4(q, qw, bias, act, block, out)
     M, K, C = q.rows, q.K, _columns(qw, a)
-    o = _buffer(out, M, C, block, device, "clq_mx4_linear_mx4")
-    p, r = q.data.data_ptr(), o.data.data_ptr()
+    o, codes, scales = _buffer(out, M, C, block, device, "clq_mx4_linear_mx4")
+    p = q.data.data_ptr()
     _check(_lib.clq_mx4_linear_mx4(p, p + _code_bytes(M, K), qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, M, qw.N,
-                                   K, a, block, r, r + _code_bytes(M, C), _raw_stream(i)), "clq_mx4_linear_mx4")
+                                   K, a, block, codes, scales, _raw_stream(i)), "clq_mx4_linear_mx4")
     return o
 
 
@@ -461,10 +468,10 @@ def clq_mx4_dispatch(X, plan, block=0, perm=None, out=None, stream=None):
             return clq_mx4_dispatch(X, plan, block, perm, out)
     g = None if perm is None else _gather(perm, K, device)
     n = plan.plan_rows
-    q = _buffer(out, n, K, block, device, "clq_mx4_dispatch")
-    p, t = q.data.data_ptr(), plan.data.data_ptr()
+    q, codes, scales = _buffer(out, n, K, block, device, "clq_mx4_dispatch")
+    t = plan.data.data_ptr()
     _check(_lib.clq_mx4_dispatch(X.data_ptr(), _TYPES[X.dtype], ldx, g, T, plan.top_k, plan.experts, K, block, t,
-                                 t + 4 * plan.at_source, p, p + _code_bytes(n, K), _raw_stream(i)), "clq_mx4_dispatch")
+                                 t + 4 * plan.at_source, codes, scales, _raw_stream(i)), "clq_mx4_dispatch")
     return q
 
 
@@ -506,11 +513,11 @@ def clq_mx4_experts_mx4(q, plan, qw, bias=None, act=None, block=0, out=None, str
         with _elsewhere(device, stream):
             return clq_mx4_experts_mx4(q, plan, qw, bias, act, block, out)
     M, K, C = q.rows, q.K, _columns(qw, a)
-    o = _buffer(out, M, C, block, device, "clq_mx4_experts_mx4")
-    p, r = q.data.data_ptr(), o.data.data_ptr()
+    o, codes, scales = _buffer(out, M, C, block, device, "clq_mx4_experts_mx4")
+    p = q.data.data_ptr()
     _check(_lib.clq_mx4_experts_mx4(p, p + _code_bytes(M, K), plan.data.data_ptr(), plan.tokens, plan.top_k,
                                     plan.experts, qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, qw.N, K, a, block,
-                                    r, r + _code_bytes(M, C), _raw_stream(i)), "clq_mx4_experts_mx4")
+                                    codes, scales, _raw_stream(i)), "clq_mx4_experts_mx4")
     return o
 
 

@@ -169,6 +169,21 @@ def test_linear_large(clq, M, N, K):
     _check_product(got, (xv @ wv.T).numpy(), (xv.abs() @ wv.abs().T).numpy(), K, F16)
 
 
+@pytest.mark.parametrize("M,N,K", [(43200, 4608, 1152), (20000, 1152, 4608), (30000, 3456, 192)])
+def test_linear_many_tiles(clq, M, N, K):
+    """Many rounds of workgroups under full memory load, several times over: a transfer that was
+    not waited for shows here and not in a launch of a few tiles.  Against fp64 on the GPU."""
+    x, w = torch.randn(M, K, device="cuda", dtype=F16), torch.randn(N, K, device="cuda", dtype=F16) * K ** -0.5
+    q, qw = clq.clq_mx4_quantize(x, 64), clq.clq_mx4_quantize_weights(w, 64)
+    xv, wv = clq.clq_mx4_dequantize(q, torch.float32), clq.clq_mx4_dequantize(qw, torch.float32)
+    want = xv.double() @ wv.double().t().contiguous()
+    mass = xv.abs() @ wv.abs().t().contiguous()
+    tol = UNIT[F16] * want.abs() + K * 2.0 ** -24 * mass + 2.0 ** -25
+    for i in range(5):
+        got = clq.clq_mx4_linear(q, qw).double()
+        assert ((got - want).abs() <= tol).all(), i
+
+
 def test_linear_of_rotated_is_the_linear(clq):
     """The rotation is absorbed: the product approximates x . w^T."""
     x, w = _rand(1, 64, 1152), _rand(2, 256, 1152, scale=1152 ** -0.5)
