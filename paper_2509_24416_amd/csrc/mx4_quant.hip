@@ -58,28 +58,37 @@ __device__ __forceinline__ int64_t gated_row(int64_t n, int64_t rows) {
     return t < 32 ? 32 * j + t : rows / 2 + 32 * j + (t - 32);
 }
 
+// A launch covers row units first .. first + units - 1 (fewer than 2^31 tiles, so that the
+// index arithmetic is 32-bit).
 struct QuantParams {
     const uint16_t *X;
-    int64_t ldx, rows, units, mat_units;   // mat_units: units of each matrix
+    int64_t ldx, rows;
+    int first, units, mat_units;   // mat_units: units of each matrix
     const int32_t *perm;
-    int K, log_div, tiles;                 // tiles: 256-column tiles of a unit
+    int K, log_div, tiles;         // tiles: 256-column tiles of a unit
     bool weights, gated;
     const int32_t *source, *total_units;
     uint8_t *codes, *scales;
 };
 
-// Source row of W or X of output row r of unit u; negative: zeros.
-__device__ __forceinline__ int64_t source_row(const QuantParams &p, int64_t u, int r) {
+// Source rows of W or X of output rows r .. r + 3 of unit u; negative: zeros.
+__device__ __forceinline__ void source_rows(const QuantParams &p, int u, int r, int64_t (&src)[4]) {
     if (p.source) {
-        const int64_t src = p.source[u * 32 + r];
-        return src < p.rows ? src : -1;
+        int v[4];
+        __builtin_memcpy(v, p.source + (int64_t)u * 32 + r, sizeof v);   // (4-byte aligned)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) src[i] = v[i] < p.rows ? v[i] : -1;
+        return;
     }
-    const int64_t mat = u / p.mat_units, n = (u - mat * p.mat_units) * 32 + r;
-    if (n >= p.rows) return -1;
-    return (p.gated ? gated_row(n, p.rows) : n) + mat * p.rows;
+    const int mat = u < p.mat_units ? 0 : u / p.mat_units;
+    const int64_t n = (int64_t)(u - mat * p.mat_units) * 32 + r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        src[i] = n + i < p.rows ? (p.gated ? gated_row(n + i, p.rows) : n + i) + mat * p.rows : -1;
 }
-__device__ __forceinline__ int64_t used_units(const QuantParams &p) {
-    return p.total_units ? min((int64_t)*p.total_units, p.units) : p.units;
+// the launch's share of the row units in use
+__device__ __forceinline__ int used_units(const QuantParams &p) {
+    return p.total_units ? max(min(*p.total_units - p.first, p.units), 0) : p.units;
 }
 
 // Stage h = 1 of a lane's pair of columns (the values themselves without a rotation).
@@ -93,7 +102,7 @@ __device__ __forceinline__ void pair_in(float lo, float hi, float &a, float &b) 
 // x[row][column] after stage h = 1; rho0: the first row's fragment row.
 template <int B>
 __device__ __forceinline__ void quantize_chunk(const QuantParams &p, float (&x)[4][8], int chunk, const CrossSigns &cs,
-                                               int64_t u, int rho0) {
+                                               int u, int rho0) {
     if constexpr (B != 0) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) fwht8_rest(x[r]);
@@ -135,34 +144,34 @@ __global__ void __launch_bounds__(kThreads) mx_quant_kernel(QuantParams p)
     // chunk order over lanes: see rq_device.h
     const int lane_chunk = (lc & ~7) | logical_lane(lc & 7);
     const CrossSigns cs = cross_signs<B ? B : 32>(lane_chunk);
-    const int64_t work = used_units(p) * p.tiles;
-    for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
-        const int64_t u = w / p.tiles;
-        const int chunk = (int)(w - u * p.tiles) * kChunkLanes + lane_chunk, col = 8 * chunk;
-        const bool in = col < p.K;   // (whole octets and, for B = 128, whole 16 lanes)
-        float x[4][8];
+    const int w = (int)(blockIdx.x / (unsigned)p.tiles);
+    if (w >= used_units(p)) return;
+    const int u = p.first + w, chunk = ((int)blockIdx.x - w * p.tiles) * kChunkLanes + lane_chunk, col = 8 * chunk;
+    const bool in = col < p.K;   // (whole octets and, for B = 128, whole 16 lanes)
+    int64_t src[4];
+    source_rows(p, u, rg * 4, src);
+    uint32_t d[4][4] = {};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t src = source_row(p, u, rg * 4 + r);
-            uint32_t d[4] = {0u, 0u, 0u, 0u};
-            if (in && src >= 0) {
-                const uint16_t *row = p.X + src * p.ldx;
-                if constexpr (PERM) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        d[e] = (uint32_t)row[p.perm[col + 2 * e]] | (uint32_t)row[p.perm[col + 2 * e + 1]] << 16;
-                } else {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(row + col);
-                    d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
-                }
-            }
+    for (int r = 0; r < 4; ++r) {
+        if (!in || src[r] < 0) continue;
+        const uint16_t *row = p.X + src[r] * p.ldx;
+        if constexpr (PERM) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                pair_in<B>(widen((uint16_t)d[e], BF16), widen((uint16_t)(d[e] >> 16), BF16), x[r][2 * e], x[r][2 * e + 1]);
+                d[r][e] = (uint32_t)row[p.perm[col + 2 * e]] | (uint32_t)row[p.perm[col + 2 * e + 1]] << 16;
+        } else {
+            const uint4 v = *reinterpret_cast<const uint4 *>(row + col);
+            d[r][0] = v.x; d[r][1] = v.y; d[r][2] = v.z; d[r][3] = v.w;
         }
-        // (in the weights' fragment order four rows aligned to four stay together)
-        quantize_chunk<B>(p, x, chunk, cs, u, p.weights ? wq_rho(rg * 4) : rg * 4);
     }
+    float x[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            pair_in<B>(widen((uint16_t)d[r][e], BF16), widen((uint16_t)(d[r][e] >> 16), BF16), x[r][2 * e], x[r][2 * e + 1]);
+    // (in the weights' fragment order four rows aligned to four stay together)
+    quantize_chunk<B>(p, x, chunk, cs, u, p.weights ? wq_rho(rg * 4) : rg * 4);
 }
 
 // Gathered inputs whose four rows fit LDS: a workgroup takes four rows, staged with the
@@ -173,16 +182,14 @@ __global__ void __launch_bounds__(kGatherThreads) mx_gather_kernel(QuantParams p
 {
     extern __shared__ __align__(16) uint8_t staged[];
     const int t = threadIdx.x, chunks = p.K >> 3, padded = (chunks + 15) & ~15;
-    const int64_t work = used_units(p) * 8;
-    for (int64_t w = blockIdx.x; w < work; w += gridDim.x) {
-        const int64_t u = w >> 3;
-        const int rg = (int)(w & 7);
+    const int u = p.first + (int)(blockIdx.x >> 3), rg = blockIdx.x & 7;
+    if (u - p.first >= used_units(p)) return;
+    int64_t src[4];
+    source_rows(p, u, rg * 4, src);
+    {
         const uint16_t *row[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t src = source_row(p, u, rg * 4 + r);
-            row[r] = src < 0 ? nullptr : p.X + src * p.ldx;
-        }
+        for (int r = 0; r < 4; ++r) row[r] = src[r] < 0 ? nullptr : p.X + src[r] * p.ldx;
         for (int c = t; c < chunks; c += kGatherThreads) {
             uint4 v[4];
 #pragma unroll
@@ -219,7 +226,6 @@ __global__ void __launch_bounds__(kGatherThreads) mx_gather_kernel(QuantParams p
             }
             quantize_chunk<B>(p, x, chunk, cs, u, p.weights ? wq_rho(rg * 4) : rg * 4);
         }
-        __syncthreads();
     }
 }
 
@@ -290,27 +296,29 @@ __global__ void __launch_bounds__(256) mx_pack_kernel(const uint8_t *codes, cons
     }
 }
 
-constexpr int64_t kMaxGrid = 1 << 20;   // workgroups of a launch; the rest by a loop
+constexpr int64_t kMaxGrid = 1 << 23;   // workgroups of a launch
 
 template <int B, bool BF16>
-hipError_t launch_quant(const QuantParams &p, hipStream_t stream) {
+hipError_t launch_quant(QuantParams p, hipStream_t stream) {
     const size_t lds = (size_t)p.K * 8;
     // (the vector loads of the indices need 16 bytes of alignment)
-    if (p.perm && lds <= (size_t)kGatherLds && (reinterpret_cast<uintptr_t>(p.perm) & 15) == 0) {
-        if (lds > 64 * 1024) {
-            const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void *>(&mx_gather_kernel<B, BF16>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kGatherLds);
-            if (set != hipSuccess) return set;
-        }
-        const int64_t work = p.units * 8;
-        hipLaunchKernelGGL((mx_gather_kernel<B, BF16>), dim3((unsigned)(work < kMaxGrid ? work : kMaxGrid)),
-                           dim3(kGatherThreads), lds, stream, p);
-        return hipGetLastError();
+    const bool staged = p.perm && lds <= (size_t)kGatherLds && (reinterpret_cast<uintptr_t>(p.perm) & 15) == 0;
+    if (staged && lds > 64 * 1024) {
+        const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void *>(&mx_gather_kernel<B, BF16>),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, kGatherLds);
+        if (set != hipSuccess) return set;
     }
-    const int64_t work = p.units * p.tiles;
-    const dim3 grid((unsigned)(work < kMaxGrid ? work : kMaxGrid));
-    if (p.perm) hipLaunchKernelGGL((mx_quant_kernel<B, BF16, true>), grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((mx_quant_kernel<B, BF16, false>), grid, dim3(kThreads), 0, stream, p);
+    const int per = staged ? 8 : p.tiles, all = p.units;
+    for (int left = all, first = 0; left > 0;) {
+        p.first = first;
+        p.units = left < kMaxGrid / per ? left : (int)(kMaxGrid / per);
+        const dim3 grid((unsigned)(p.units * per));
+        if (staged) hipLaunchKernelGGL((mx_gather_kernel<B, BF16>), grid, dim3(kGatherThreads), lds, stream, p);
+        else if (p.perm) hipLaunchKernelGGL((mx_quant_kernel<B, BF16, true>), grid, dim3(kThreads), 0, stream, p);
+        else hipLaunchKernelGGL((mx_quant_kernel<B, BF16, false>), grid, dim3(kThreads), 0, stream, p);
+        first += p.units;
+        left -= p.units;
+    }
     return hipGetLastError();
 }
 template <int B>
@@ -325,8 +333,9 @@ hipError_t launch_mx_quantize(const MxQuantArgs &a, hipStream_t stream) {
     p.X = static_cast<const uint16_t *>(a.X);
     p.ldx = a.ldx;
     p.rows = a.rows;
-    p.mat_units = a.units;
-    p.units = a.units * a.mats;
+    p.mat_units = (int)a.units;
+    p.units = (int)(a.units * a.mats);   // (under 2^26)
+    p.first = 0;
     p.perm = a.perm;
     p.K = a.K;
     p.log_div = a.log_div;
