@@ -15,7 +15,7 @@
  *
  * Conventions are those of clq.h: device pointers, caller-owned buffers, checks on the
  * host before anything is enqueued, no synchronisation, CLQ_ERR_* statuses.  Values
- * are fp16 or bf16 (clq_type); sums are fp32.
+ * are fp16 or bf16 (clq_type), results fp32 too; sums are fp32.
  *   - Shapes: 1 <= M, N, T; 64 <= K <= 32768 with K % 64 == 0 and K % block == 0;
  *     1 <= experts <= 512; rows of a matrix (experts * padded rows) below 2^31;
  *     products of fewer than 2^24 tiles of 256 rows x 128 channels.  Row strides
@@ -80,7 +80,7 @@ clq_status clq_mx4_pack_weights(const void *row_codes, const void *row_scales, i
 clq_status clq_mx4_dequantize(const void *codes, const void *scales, int32_t weights, int32_t gated, int64_t matrices,
                               int64_t rows, int64_t K, clq_type type, void *out, int64_t ldo, hipStream_t stream);
 
-/* Y = X . W^T + bias, summed in fp32 and rounded once to fp16 or bf16.
+/* Y = X . W^T + bias, summed in fp32 and rounded once to `type` (fp16, bf16, or fp32: not rounded).
  *   bias    fp16 or bf16 [N] (bias_type), or NULL.
  *   Y       out, [M][N], row stride ldy. */
 clq_status clq_mx4_linear(const void *Xq, const void *Xs, const void *Wq, const void *Ws, const void *bias,
@@ -156,11 +156,11 @@ clq_status clq_mx4_experts_mx4(const void *Xq, const void *Xs, const int32_t *ta
                                hipStream_t stream);
 
 /* out[t] = sum over j of weights[t][j] * Y[rows[t][j]], in the order of the slots, in fp32,
- * rounded once; rows of -1 add nothing.  Y [plan rows][N] and out [T][N] of `type` (fp16 or
- * bf16), row strides ldy and ldo. */
+ * rounded once; rows of -1 add nothing.  Y [plan rows][N] of `type`, out [T][N] of `out_type`,
+ * row strides ldy and ldo. */
 clq_status clq_expert_combine(const void *Y, clq_type type, int64_t ldy, const int32_t *rows, const float *weights,
-                              int64_t T, int64_t top_k, int64_t experts, int64_t N, void *out, int64_t ldo,
-                              hipStream_t stream);
+                              int64_t T, int64_t top_k, int64_t experts, int64_t N, void *out, clq_type out_type,
+                              int64_t ldo, hipStream_t stream);
 
 #ifdef __cplusplus
 }

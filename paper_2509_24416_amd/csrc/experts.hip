@@ -391,14 +391,20 @@ struct CombineArgs {
     int64_t first;         // token of the launch's first thread
     int tokens, k, per;    // per: pieces of W columns in a row
 };
+// (W consecutive values)
 template <class T, int W>
+struct __align__(W * sizeof(T) < 16 ? W * sizeof(T) : 16) Piece {
+    T v[W];
+};
+
+template <class TI, class TO, int W>
 __global__ void __launch_bounds__(256) combine_kernel(CombineArgs a)
 {
     const unsigned i = blockIdx.x * 256 + threadIdx.x, tl = i / (unsigned)a.per;
     if (tl >= (unsigned)a.tokens) return;
     const int64_t t = a.first + tl;
     const int c = (int)(i - tl * a.per) * W;
-    const T *Y = static_cast<const T *>(a.Y) + c;
+    const TI *Y = static_cast<const TI *>(a.Y) + c;
     const int32_t *rows = a.rows + t * a.k;
     const float *weights = a.weights + t * a.k;
     float s[W] = {};
@@ -411,38 +417,48 @@ __global__ void __launch_bounds__(256) combine_kernel(CombineArgs a)
             w[q] = j + q < a.k ? weights[j + q] : 0.0f;
             if (r[q] >= a.plan_rows) r[q] = -1;
         }
-        T v[4][W];
+        Piece<TI, W> v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (r[q] >= 0) v[q] = *reinterpret_cast<const Piece<TI, W> *>(Y + r[q] * a.ldy);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             if (r[q] < 0) continue;
-            if constexpr (W == 8) *reinterpret_cast<uint4 *>(v[q]) = *reinterpret_cast<const uint4 *>(Y + r[q] * a.ldy);
-            else v[q][0] = Y[r[q] * a.ldy];
-        }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (r[q] < 0) continue;
-#pragma unroll
-            for (int e = 0; e < W; ++e) s[e] = __builtin_fmaf(w[q], (float)v[q][e], s[e]);
+            for (int e = 0; e < W; ++e) s[e] = __builtin_fmaf(w[q], (float)v[q].v[e], s[e]);
         }
     }
-    T o[W];
+    Piece<TO, W> o;
 #pragma unroll
-    for (int e = 0; e < W; ++e) o[e] = (T)s[e];
-    T *out = static_cast<T *>(a.out) + t * a.ldo + c;
-    if constexpr (W == 8) *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<uint4 *>(o);
-    else out[0] = o[0];
+    for (int e = 0; e < W; ++e) o.v[e] = (TO)s[e];
+    *reinterpret_cast<Piece<TO, W> *>(static_cast<TO *>(a.out) + t * a.ldo + c) = o;
 }
 
-template <class T, int W>
+template <class TI, class TO, int W>
 hipError_t launch_combine(CombineArgs a, int64_t tokens, hipStream_t stream) {
     // (a launch's threads stay under 2^31)
     const int64_t most = ((int64_t)1 << 30) / a.per;
     for (a.first = 0; a.first < tokens; a.first += a.tokens) {
         a.tokens = (int)(tokens - a.first < most ? tokens - a.first : most);
         const dim3 grid((unsigned)(((int64_t)a.tokens * a.per + 255) / 256));
-        hipLaunchKernelGGL((combine_kernel<T, W>), grid, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((combine_kernel<TI, TO, W>), grid, dim3(256), 0, stream, a);
     }
     return hipGetLastError();
+}
+template <class TI, class TO>
+hipError_t launch_combine(CombineArgs a, int64_t tokens, int64_t N, hipStream_t stream) {
+    const bool vec = N % 8 == 0;
+    a.per = (int)(vec ? N / 8 : N);
+    return vec ? launch_combine<TI, TO, 8>(a, tokens, stream) : launch_combine<TI, TO, 1>(a, tokens, stream);
+}
+template <class TI>
+hipError_t launch_combine(const CombineArgs &a, MxType out, int64_t tokens, int64_t N, hipStream_t stream) {
+    switch (out) {
+        case MxType::F16: return launch_combine<TI, _Float16>(a, tokens, N, stream);
+        case MxType::BF16: return launch_combine<TI, __bf16>(a, tokens, N, stream);
+        case MxType::F32: return launch_combine<TI, float>(a, tokens, N, stream);
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -483,12 +499,15 @@ hipError_t launch_expert_plan(const int32_t *ids, int64_t n, int k, int E, int32
 }
 
 hipError_t launch_expert_combine(const void *Y, MxType type, int64_t ldy, const int32_t *rows, const float *weights,
-                                 int64_t T, int k, int64_t N, int64_t plan_rows, void *out, int64_t ldo,
+                                 int64_t T, int k, int64_t N, int64_t plan_rows, void *out, MxType out_type, int64_t ldo,
                                  hipStream_t stream) {
-    const bool vec = N % 8 == 0;
-    const CombineArgs a = {Y, rows, weights, out, ldy, ldo, plan_rows, 0, 0, k, (int)(vec ? N / 8 : N)};
-    if (type == MxType::BF16) return vec ? launch_combine<__bf16, 8>(a, T, stream) : launch_combine<__bf16, 1>(a, T, stream);
-    return vec ? launch_combine<_Float16, 8>(a, T, stream) : launch_combine<_Float16, 1>(a, T, stream);
+    const CombineArgs a = {Y, rows, weights, out, ldy, ldo, plan_rows, 0, 0, k, 0};
+    switch (type) {
+        case MxType::F16: return launch_combine<_Float16>(a, out_type, T, N, stream);
+        case MxType::BF16: return launch_combine<__bf16>(a, out_type, T, N, stream);
+        case MxType::F32: return launch_combine<float>(a, out_type, T, N, stream);
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace clq

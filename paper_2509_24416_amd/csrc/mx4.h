@@ -138,7 +138,7 @@ size_t expert_plan_workspace_bytes(int64_t n, int64_t E);
 hipError_t launch_expert_plan(const int32_t *ids, int64_t n, int k, int E, int32_t *info, int32_t *rows,
                               int32_t *source, void *workspace, hipStream_t stream);
 hipError_t launch_expert_combine(const void *Y, MxType type, int64_t ldy, const int32_t *rows, const float *weights,
-                                 int64_t T, int k, int64_t N, int64_t plan_rows, void *out, int64_t ldo,
+                                 int64_t T, int k, int64_t N, int64_t plan_rows, void *out, MxType out_type, int64_t ldo,
                                  hipStream_t stream);
 
 }  // namespace clq

@@ -16,6 +16,7 @@ namespace {
 constexpr int64_t kMaxExperts = 512, kMaxTopK = 32, kMaxGroups = 64;
 
 bool is_16bit(clq_type t) { return t == CLQ_F16 || t == CLQ_BF16; }
+bool is_type(clq_type t) { return is_16bit(t) || t == CLQ_F32; }
 clq::MxType mx_type(clq_type t) { return t == CLQ_F16 ? clq::MxType::F16 : t == CLQ_BF16 ? clq::MxType::BF16 : clq::MxType::F32; }
 
 clq_status check_mx_block(int64_t K, int32_t block) { return block == 0 ? CLQ_OK : check_block(K, block); }
@@ -88,7 +89,7 @@ clq_status check_tiles(int64_t rows, int64_t N) {
     return ((rows + 255) / 256) * ((N + 127) / 128) < (int64_t)1 << 24 ? CLQ_OK : CLQ_ERR_SHAPE;
 }
 clq_status plain_output(clq::MxGemmArgs &g, clq_type type, void *Y, int64_t ldy) {
-    if (!is_16bit(type)) return CLQ_ERR_ARG;
+    if (!is_type(type)) return CLQ_ERR_ARG;
     if (ldy < g.N || ldy % 8 != 0) return CLQ_ERR_SHAPE;
     if (!aligned(Y, 16)) return CLQ_ERR_ALIGN;
     g.out_type = mx_type(type);
@@ -188,7 +189,7 @@ clq_status clq_mx4_dequantize(const void *codes, const void *scales, int32_t wei
     if (!codes || !scales || !out) return CLQ_ERR_NULL;
     clq_status s;
     if ((weights != 0 && weights != 1) || (gated != 0 && gated != 1)) return CLQ_ERR_ARG;
-    if (!is_16bit(type) && type != CLQ_F32) return CLQ_ERR_ARG;
+    if (!is_type(type)) return CLQ_ERR_ARG;
     if (!weights && (gated || matrices != 1)) return CLQ_ERR_ARG;
     if (weights) s = check_matrices(matrices, rows, K);
     else s = check_rows(rows) != CLQ_OK ? CLQ_ERR_SHAPE : check_k(K);
@@ -233,7 +234,7 @@ clq_status clq_expert_route(const void *logits, clq_type type, int64_t ld, int64
                             int32_t renormalize, float scale, int32_t *ids, float *weights, hipStream_t stream) {
     if (!logits || !ids || !weights) return CLQ_ERR_NULL;
     clq_status s;
-    if ((!is_16bit(type) && type != CLQ_F32) || (score != CLQ_SOFTMAX && score != CLQ_SIGMOID)) return CLQ_ERR_ARG;
+    if ((!is_type(type)) || (score != CLQ_SOFTMAX && score != CLQ_SIGMOID)) return CLQ_ERR_ARG;
     if ((renormalize != 0 && renormalize != 1) || !isfinite(scale)) return CLQ_ERR_ARG;
     if ((s = check_plan(T, top_k, experts)) != CLQ_OK) return s;
     if (ld < experts) return CLQ_ERR_SHAPE;
@@ -317,16 +318,17 @@ clq_status clq_mx4_experts_mx4(const void *Xq, const void *Xs, const int32_t *ta
 }
 
 clq_status clq_expert_combine(const void *Y, clq_type type, int64_t ldy, const int32_t *rows, const float *weights,
-                              int64_t T, int64_t top_k, int64_t experts, int64_t N, void *out, int64_t ldo,
-                              hipStream_t stream) {
+                              int64_t T, int64_t top_k, int64_t experts, int64_t N, void *out, clq_type out_type,
+                              int64_t ldo, hipStream_t stream) {
     if (!Y || !rows || !weights || !out) return CLQ_ERR_NULL;
     clq_status s;
-    if (!is_16bit(type)) return CLQ_ERR_ARG;
+    if (!is_type(type) || !is_type(out_type)) return CLQ_ERR_ARG;
     if ((s = check_plan(T, top_k, experts)) != CLQ_OK || (s = check_rows(N)) != CLQ_OK) return s;
     if (ldy < N || ldo < N || ldy % 8 != 0 || ldo % 8 != 0) return CLQ_ERR_SHAPE;
     if (!aligned(Y, 16) || !aligned(out, 16) || !aligned(rows, 4) || !aligned(weights, 4)) return CLQ_ERR_ALIGN;
     return done(stream, clq::launch_expert_combine(Y, mx_type(type), ldy, rows, weights, T, (int)top_k, N,
-                                                   clq_expert_plan_rows(T, top_k, experts), out, ldo, stream));
+                                                   clq_expert_plan_rows(T, top_k, experts), out, mx_type(out_type), ldo,
+                                                   stream));
 }
 
 }  // extern "C"

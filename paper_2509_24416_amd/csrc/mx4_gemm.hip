@@ -1,5 +1,5 @@
 // MX4 products: Y = dequant(Xq) . dequant(Wq)^T + bias on the fp4 matrix cores of
-// gfx950, dense and grouped by expert, with the result either stored as fp16 / bf16
+// gfx950, dense and grouped by expert, with the result either stored (fp16, bf16, fp32)
 // or activated, rotated (CLQ, arXiv 2509.24416, Sec. 3.3) and requantized to MX4 for
 // the next product without leaving the registers.
 //
@@ -36,9 +36,10 @@ struct Args {
     int xunits, wunits;
     const int32_t *info;
     int experts, log_units;   // of a tile
-    uint16_t *Y;
+    void *Y;
     int64_t ldy;
-    bool bias_bf16, out_bf16;
+    bool bias_bf16;
+    MxType out_type;
     uint8_t *Oq, *Os;
     int oK;   // channels of the MX4 output
 };
@@ -74,10 +75,10 @@ __device__ __forceinline__ v16f mfma_mx4(v4u a, v4u b, v16f c, uint32_t sa, uint
 __device__ __forceinline__ float widen(uint16_t h, bool bf16) {
     return bf16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
 }
-// two outputs, rounded to nearest even
-template <bool BF16>
+// two 16-bit outputs, rounded to nearest even
+template <MxType T>
 __device__ __forceinline__ uint32_t narrow2(float a, float b) {
-    if constexpr (BF16) {
+    if constexpr (T == MxType::BF16) {
         typedef __bf16 b2 __attribute__((ext_vector_type(2)));
         const b2 v = {(__bf16)a, (__bf16)b};
         return __builtin_bit_cast(uint32_t, v);
@@ -189,22 +190,66 @@ __device__ __forceinline__ int bias_index(int n, int N, bool gated) {
     return t < 32 ? 32 * j + t : N / 2 + 32 * j + (t - 32);
 }
 
-// Stores the plain outputs of one 32-row unit (row0 ..), 128 channels from n0.  A lane's
+// Eight outputs of a row from channel n on, s in fp32.
+template <bool RAGGED, MxType T>
+__device__ __forceinline__ void store8(const Args &a, const float *s, int64_t m, int n) {
+    const bool whole = !RAGGED || n <= a.N - 8;
+    if constexpr (T == MxType::F32) {
+        float *dst = static_cast<float *>(a.Y) + m * a.ldy + n;
+        if (whole) {
+            reinterpret_cast<v4f *>(dst)[0] = v4f{s[0], s[1], s[2], s[3]};
+            reinterpret_cast<v4f *>(dst)[1] = v4f{s[4], s[5], s[6], s[7]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n + e < a.N) dst[e] = s[e];
+        }
+    } else {
+        const v4u v = {narrow2<T>(s[0], s[1]), narrow2<T>(s[2], s[3]), narrow2<T>(s[4], s[5]), narrow2<T>(s[6], s[7])};
+        uint16_t *dst = static_cast<uint16_t *>(a.Y) + m * a.ldy + n;
+        if (whole) {
+            *reinterpret_cast<v4u *>(dst) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n + e < a.N) dst[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+        }
+    }
+}
+
+// Stores the 16-bit outputs of one 32-row unit (row0 ..), 128 channels from n0.  A lane's
 // 16 channels of a row are 32 bytes of 32 different rows to a store, and the L2 takes a
 // request for each; so the wave turns the unit in its own part of LDS (rows kRowPitch bytes
-// apart, for the banks) and stores four whole 256-byte row pieces at a time.
+// apart, for the banks) and stores four whole 256-byte row pieces at a time.  (fp32 outputs
+// are 64 bytes a lane, whole requests as they are.)
 constexpr int kRowPitch = 272, kTurnBytes = 32 * kRowPitch;
 
-template <bool RAGGED, bool BF16>
-__device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][2], int fm, uint8_t *turn, int64_t row0, int64_t row_end, int n0, int lane) {
+template <bool RAGGED, MxType T>
+__device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][2], int fm, uint8_t *turn, int64_t row0,
+                                            int64_t row_end, int n0, int lane) {
     const int h16 = (lane >> 5) * 16;
+    if constexpr (T == MxType::F32) {
+        const int64_t m = row0 + (lane & 31);
+        if (m >= row_end) return;
+#pragma unroll
+        for (int fn = 0; fn < 4; ++fn)
+#pragma unroll
+            for (int q = 0; q < 16; q += 8) {
+                const int n = n0 + fn * 32 + h16 + q;
+                float s[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] = acc[fn][fm][q + e];
+                if (n < a.N) store8<RAGGED, T>(a, s, m, n);
+            }
+        return;
+    }
     uint8_t *w = turn + (lane & 31) * kRowPitch + h16 * 2;
 #pragma unroll
     for (int fn = 0; fn < 4; ++fn) {
         const v16f &x = acc[fn][fm];
         uint32_t h[8];
 #pragma unroll
-        for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2<BF16>(x[v], x[v + 1]);
+        for (int v = 0; v < 16; v += 2) h[v / 2] = narrow2<T>(x[v], x[v + 1]);
         reinterpret_cast<v4u *>(w + fn * 64)[0] = v4u{h[0], h[1], h[2], h[3]};
         reinterpret_cast<v4u *>(w + fn * 64)[1] = v4u{h[4], h[5], h[6], h[7]};
     }
@@ -216,7 +261,7 @@ __device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][
         const int r = i * 4 + (lane >> 4);
         const v4u v = *reinterpret_cast<const v4u *>(turn + r * kRowPitch + c * 16);
         if (row0 + r >= row_end) break;
-        uint16_t *dst = a.Y + (row0 + r) * a.ldy + n;
+        uint16_t *dst = static_cast<uint16_t *>(a.Y) + (row0 + r) * a.ldy + n;
         if (!RAGGED || n <= a.N - 8) {
             *reinterpret_cast<v4u *>(dst) = v;
         } else {
@@ -307,12 +352,12 @@ __device__ __forceinline__ void requantize(const Args &a, float (&f)[NF][16], in
     }
 }
 
-template <int NW, Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+template <int NW, Out OUT, int B, bool GROUPED, bool RAGGED, MxType T>
 __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
 {
     constexpr int NS = kStages, PPW = 4 / NW;   // transfers per wave and stage
     constexpr bool GATED = OUT == Out::Swiglu;
-    constexpr int kRing = NS * kStageBytes + 2 * kQuadBytes, kTurn = OUT == Out::Plain ? NW * kTurnBytes : 0;
+    constexpr int kRing = NS * kStageBytes + 2 * kQuadBytes, kTurn = OUT == Out::Plain && T != MxType::F32 ? NW * kTurnBytes : 0;
     __shared__ __align__(16) uint8_t pool[kRing > kTurn ? kRing : kTurn];
     __shared__ __align__(16) float ep[kBN];   // biases
     const int tid = threadIdx.x, lane = tid & 63;
@@ -471,7 +516,7 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
         if (u >= rt.unit_end) return;
         if constexpr (OUT == Out::Plain) {
             const int64_t end = GROUPED ? (int64_t)rt.unit_end * 32 : a.M;
-            store_plain<RAGGED, BF16>(a, acc, fm, pool + wave * kTurnBytes, (int64_t)u * 32, end, tn * kBN, lane);
+            store_plain<RAGGED, T>(a, acc, fm, pool + wave * kTurnBytes, (int64_t)u * 32, end, tn * kBN, lane);
         } else if constexpr (GATED) {
             float f[2][16];
             static_for<0, 2>([&](auto pc) {
@@ -509,13 +554,14 @@ using Split1 = Split<1, 1, 8, 6>;
 using Split2 = Split<2, 2, 4, 4>;
 using SplitMx = Split<4, 1, 4, 3>;
 
-template <class C, Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+template <class C, Out OUT, int B, bool GROUPED, bool RAGGED, MxType T>
 __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
 {
     constexpr bool MX4 = OUT != Out::Plain, GATED = OUT == Out::Swiglu;
     constexpr int FN = C::FN, FM = C::FM, KS = C::KS, D = C::kAhead;
     static_assert(!MX4 || (FN == 4 && FM == 1), "a requantized tile");
     __shared__ __align__(16) float part[KS][C::BM * C::kPitch];
+    __shared__ __align__(16) float ep[C::BN];   // biases
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nks = a.K >> 6, nq = (a.K + 255) >> 8;
@@ -542,6 +588,11 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
         wsrc[f] = a.Wq + rt.expert * a.w_stride + wu * nks * kMxUnit + lane * 16;
         wssrc[f] = a.Ws + rt.expert * a.ws_stride + wu * nq * kMxScaleRow + lane * 4;
     }
+    // a channel's bias per thread, on its way while the k loop runs
+    static_assert(C::NT >= C::BN, "a thread per channel");
+    uint16_t bv = 0;
+    if (a.bias && tid < C::BN)
+        bv = a.bias[(int64_t)rt.expert * a.N + bias_index(min(tn * C::BN + tid, a.N - 1), a.N, GATED)];
     const uint8_t *xsrc[FM], *xssrc[FM];
 #pragma unroll
     for (int f = 0; f < FM; ++f) {
@@ -598,6 +649,7 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
             if (rest > decltype(dc)::value) mma(dc);
         });
     }
+    if (tid < C::BN) ep[tid] = widen(bv, a.bias_bf16);
     // lane's 16 channels of its row
     const int row = lane & 31, h16 = (lane >> 5) * 16;
 #pragma unroll
@@ -610,7 +662,6 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
                 dst[q] = v4f{acc[f][g][4 * q], acc[f][g][4 * q + 1], acc[f][g][4 * q + 2], acc[f][g][4 * q + 3]};
         }
     __syncthreads();
-    const uint16_t *bias = a.bias ? a.bias + (int64_t)rt.expert * a.N : nullptr;
     if constexpr (!MX4) {
         // eight channels of a row at a time
         constexpr int kPieces = C::BN / 8;
@@ -618,27 +669,16 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
             const int r = p / kPieces, c = (p % kPieces) * 8, n = tn * C::BN + c;
             const int64_t m = (int64_t)u * 32 + r;
             if (n >= a.N || m >= (GROUPED ? (int64_t)rt.unit_end * 32 : (int64_t)a.M)) continue;
-            float s[8] = {};
+            float s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] = ep[c + e];
 #pragma unroll
             for (int w = 0; w < KS; ++w) {
                 const v4f *src = reinterpret_cast<const v4f *>(&part[w][r * C::kPitch + c]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[e] += src[e >> 2][e & 3];
             }
-            if (bias) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[e] += widen(bias[min(n + e, a.N - 1)], a.bias_bf16);
-            }
-            const v4u v = {narrow2<BF16>(s[0], s[1]), narrow2<BF16>(s[2], s[3]), narrow2<BF16>(s[4], s[5]),
-                           narrow2<BF16>(s[6], s[7])};
-            uint16_t *dst = a.Y + m * a.ldy + n;
-            if (!RAGGED || n <= a.N - 8) {
-                *reinterpret_cast<v4u *>(dst) = v;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < a.N) dst[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
-            }
+            store8<RAGGED, T>(a, s, m, n);
         }
     } else {
         // wave 0 .. NW - 1: the fragments of a rotation block each, summed in the products' layout
@@ -649,8 +689,7 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
         for (int i = 0; i < NF; ++i) {
             const int c = (wave * NF + i) * 32 + h16;
 #pragma unroll
-            for (int v = 0; v < 16; ++v)
-                s[i][v] = bias ? widen(bias[bias_index(min(tn * C::BN + c + v, a.N - 1), a.N, GATED)], a.bias_bf16) : 0.0f;
+            for (int v = 0; v < 16; ++v) s[i][v] = ep[c + v];
 #pragma unroll
             for (int w = 0; w < KS; ++w) {
                 const v4f *src = reinterpret_cast<const v4f *>(&part[w][row * C::kPitch + c]);
@@ -681,7 +720,7 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
 enum Kernel { kSplit1, kSplit2, kTile128, kTile256 };
 constexpr int kLogUnits[] = {0, 1, 2, 3};   // row units of a tile
 
-template <Out OUT, int B, bool GROUPED, bool RAGGED, bool BF16>
+template <Out OUT, int B, bool GROUPED, bool RAGGED, MxType T>
 void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
     using S1 = std::conditional_t<OUT == Out::Plain, Split1, SplitMx>;
     using S2 = std::conditional_t<OUT == Out::Plain && !GROUPED, Split2, S1>;
@@ -690,16 +729,16 @@ void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
     const dim3 grid((unsigned)(row_tiles * a.tiles_n));
     switch (kernel) {
         case kSplit1:
-            hipLaunchKernelGGL((mx_split_kernel<S1, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(S1::NT), 0, stream, a);
+            hipLaunchKernelGGL((mx_split_kernel<S1, OUT, B, GROUPED, RAGGED, T>), grid, dim3(S1::NT), 0, stream, a);
             break;
         case kSplit2:
-            hipLaunchKernelGGL((mx_split_kernel<S2, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(S2::NT), 0, stream, a);
+            hipLaunchKernelGGL((mx_split_kernel<S2, OUT, B, GROUPED, RAGGED, T>), grid, dim3(S2::NT), 0, stream, a);
             break;
         case kTile128:
-            hipLaunchKernelGGL((mx_tile_kernel<2, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(128), 0, stream, a);
+            hipLaunchKernelGGL((mx_tile_kernel<2, OUT, B, GROUPED, RAGGED, T>), grid, dim3(128), 0, stream, a);
             break;
         case kTile256:
-            hipLaunchKernelGGL((mx_tile_kernel<4, OUT, B, GROUPED, RAGGED, BF16>), grid, dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((mx_tile_kernel<4, OUT, B, GROUPED, RAGGED, T>), grid, dim3(256), 0, stream, a);
             break;
     }
 }
@@ -707,13 +746,18 @@ void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
 template <Out OUT, int B, bool GROUPED>
 void launch_kernel(const Args &a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
     if constexpr (OUT == Out::Plain) {
-        const bool ragged = a.N % 8 != 0;
-        if (ragged && a.out_bf16) launch_one<OUT, B, GROUPED, true, true>(a, kernel, row_tiles, stream);
-        else if (ragged) launch_one<OUT, B, GROUPED, true, false>(a, kernel, row_tiles, stream);
-        else if (a.out_bf16) launch_one<OUT, B, GROUPED, false, true>(a, kernel, row_tiles, stream);
-        else launch_one<OUT, B, GROUPED, false, false>(a, kernel, row_tiles, stream);
+        auto by_type = [&](auto rc) {
+            constexpr bool RAGGED = decltype(rc)::value;
+            switch (a.out_type) {
+                case MxType::F16: launch_one<OUT, B, GROUPED, RAGGED, MxType::F16>(a, kernel, row_tiles, stream); break;
+                case MxType::BF16: launch_one<OUT, B, GROUPED, RAGGED, MxType::BF16>(a, kernel, row_tiles, stream); break;
+                case MxType::F32: launch_one<OUT, B, GROUPED, RAGGED, MxType::F32>(a, kernel, row_tiles, stream); break;
+            }
+        };
+        if (a.N % 8 != 0) by_type(std::true_type{});
+        else by_type(std::false_type{});
     } else {
-        launch_one<OUT, B, GROUPED, false, false>(a, kernel, row_tiles, stream);
+        launch_one<OUT, B, GROUPED, false, MxType::F16>(a, kernel, row_tiles, stream);
     }
 }
 
@@ -790,7 +834,7 @@ hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
     a.Xq = g.Xq; a.Xs = g.Xs; a.Wq = g.Wq; a.Ws = g.Ws;
     a.bias = static_cast<const uint16_t *>(g.bias);
     a.bias_bf16 = g.bias_type == MxType::BF16;
-    a.out_bf16 = g.out_type == MxType::BF16;
+    a.out_type = g.out_type;
     a.M = (int)g.M;
     a.N = (int)g.N;
     a.K = g.K;
@@ -800,7 +844,7 @@ hipError_t launch_mx_gemm(const MxGemmArgs &g, hipStream_t stream) {
     a.group_m = 4;
     a.info = g.info;
     a.experts = g.experts;
-    a.Y = static_cast<uint16_t *>(g.Y);
+    a.Y = g.Y;
     a.ldy = g.ldy;
     a.Oq = g.Oq;
     a.Os = g.Os;

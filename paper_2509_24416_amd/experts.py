@@ -38,8 +38,8 @@ class ExpertMLP:
         plan = clq_expert_plan(ids, self.experts)
         q = clq_mx4_dispatch(x, plan, self.block)
         h = clq_mx4_experts_mx4(q, plan, self.w1, self.b1, act=self.act, block=self.block)
-        y = clq_mx4_experts(h, plan, self.w2, self.b2, dtype=x.dtype)
-        return clq_expert_combine(y, plan, weights)
+        y = clq_mx4_experts(h, plan, self.w2, self.b2)
+        return clq_expert_combine(y, plan, weights, dtype=x.dtype)
 
     def capture(self, tokens, dtype=torch.float16):
         """Captures forward for `tokens` tokens as one graph."""

@@ -44,7 +44,7 @@ _SIGNATURES = {
     "clq_mx4_experts": (_i32, [_p, _p, _p, _i64, _i64, _i64, _p, _p, _p, _i32, _i64, _i64, _i32, _p, _i64, _p]),
     "clq_mx4_experts_mx4": (_i32, [_p, _p, _p, _i64, _i64, _i64, _p, _p, _p, _i32, _i64, _i64, _i32, _i32, _p, _p,
                                    _p]),
-    "clq_expert_combine": (_i32, [_p, _i32, _i64, _p, _p, _i64, _i64, _i64, _i64, _p, _i64, _p]),
+    "clq_expert_combine": (_i32, [_p, _i32, _i64, _p, _p, _i64, _i64, _i64, _i64, _p, _i32, _i64, _p]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
     getattr(_lib, _name).restype = _res
@@ -94,12 +94,13 @@ class MX4Weight:
 
 class ExpertPlan:
     """Assignments sorted by expert: `tokens` x `top_k` of them to `experts` experts, in buffers
-    of `plan_rows` rows.  One int32 buffer holds the tables, the rows and the sources."""
-    __slots__ = ("data", "tokens", "top_k", "experts", "plan_rows", "at_rows", "at_source")
+    of `plan_rows` rows.  One int32 buffer holds the tables, the rows and the sources; `dtype` is
+    the type of the tokens last dispatched."""
+    __slots__ = ("data", "tokens", "top_k", "experts", "plan_rows", "at_rows", "at_source", "dtype")
 
     def __init__(self, data, tokens, top_k, experts, plan_rows, ints):
         self.data, self.tokens, self.top_k, self.experts, self.plan_rows = data, tokens, top_k, experts, plan_rows
-        self.at_rows, self.at_source = ints, ints + tokens * top_k
+        self.at_rows, self.at_source, self.dtype = ints, ints + tokens * top_k, None
 
     @property
     def counts(self):
@@ -325,8 +326,8 @@ def _product(q, qw, bias, experts):
 
 
 def _output(out, rows, N, dtype, device):
-    if dtype not in _HALF:
-        raise TypeError(f"dtype must be fp16 or bf16, got {dtype}")
+    if dtype not in _TYPES:
+        raise TypeError(f"dtype must be fp16, bf16 or fp32, got {dtype}")
     if out is None:   # rows on 16-byte boundaries
         ld = (N + 7) // 8 * 8
         out = torch.empty(rows, ld, dtype=dtype, device=device)
@@ -351,7 +352,7 @@ def _columns(qw, act):
 
 
 def clq_mx4_linear(q, qw, bias=None, dtype=torch.float16, out=None, stream=None):
-    """Y = X . W^T + bias, fp16 or bf16 [M, N]."""
+    """Y = X . W^T + bias, fp16, bf16 or fp32 [M, N]."""
     device, b, bt = _product(q, qw, bias, None)
     if qw.gated:
         raise ValueError("gated weights go with clq_mx4_linear_mx4(act='swiglu')")
@@ -472,6 +473,7 @@ def clq_mx4_dispatch(X, plan, block=0, perm=None, out=None, stream=None):
     t = plan.data.data_ptr()
     _check(_lib.clq_mx4_dispatch(X.data_ptr(), _TYPES[X.dtype], ldx, g, T, plan.top_k, plan.experts, K, block, t,
                                  t + 4 * plan.at_source, codes, scales, _raw_stream(i)), "clq_mx4_dispatch")
+    plan.dtype = X.dtype
     return q
 
 
@@ -483,9 +485,18 @@ def _plan_operands(q, plan, qw, bias):
     return r
 
 
+# Results that are summed afterwards keep fp32 while they are this small: a rounding to 16 bits
+# and the one of the sum make 1.4 times the error of one.  Past it the bytes count, and the default
+# is the tokens' type (whole layers, us, 16 bits / fp32: 512 tokens to 2 of 16 experts of width
+# 1152, 7 MB of fp32, 49 / 50; 4096, 38 MB, 103 / 114; 43200, 382 MB, 704 / 823; 4096 to 6 of 64,
+# 117 MB, 102 / 137).
+_FP32_RESULTS = 8 << 20
+
+
 def clq_mx4_experts(q, plan, qw, bias=None, dtype=None, out=None, stream=None):
-    """Each row of the plan times its expert's weights: Y [plan.plan_rows, N], fp16 or bf16 (default:
-    the bias's type, or fp16); rows past the last expert's are left as they were."""
+    """Each row of the plan times its expert's weights: Y [plan.plan_rows, N] of fp16, bf16 or fp32;
+    rows past the last expert's are left as they were.  dtype: by default that of `out`, or fp32
+    for results of up to 8 MB and the tokens' type for larger ones."""
     device, b, bt = _plan_operands(q, plan, qw, bias)
     if qw.gated:
         raise ValueError("gated weights go with clq_mx4_experts_mx4(act='swiglu')")
@@ -493,9 +504,10 @@ def clq_mx4_experts(q, plan, qw, bias=None, dtype=None, out=None, stream=None):
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
             return clq_mx4_experts(q, plan, qw, bias, dtype, out)
-    if dtype is None:
-        dtype = torch.float16 if bias is None else bias.dtype
     M, K, N = q.rows, q.K, qw.N
+    if dtype is None:
+        dtype = (out.dtype if out is not None else torch.float32 if 4 * M * N <= _FP32_RESULTS else
+                 plan.dtype or (torch.float16 if bias is None else bias.dtype))
     Y, ld = _output(out, M, N, dtype, device)
     p = q.data.data_ptr()
     _check(_lib.clq_mx4_experts(p, p + _code_bytes(M, K), plan.data.data_ptr(), plan.tokens, plan.top_k, plan.experts,
@@ -521,9 +533,10 @@ def clq_mx4_experts_mx4(q, plan, qw, bias=None, act=None, block=0, out=None, str
     return o
 
 
-def clq_expert_combine(Y, plan, weights, out=None, stream=None):
-    """out[t] = sum over the slots of weights[t, j] * Y[plan.rows[t, j]], in fp32, of Y's type."""
-    r, N, ldy = _rows2d(Y, "Y")
+def clq_expert_combine(Y, plan, weights, dtype=None, out=None, stream=None):
+    """out[t] = sum over the slots of weights[t, j] * Y[plan.rows[t, j]], in fp32.  dtype: by default
+    that of `out`, or of the tokens that the plan dispatched (none: Y's)."""
+    r, N, ldy = _rows2d(Y, "Y", _TYPES)
     _dev(weights, "weights", (torch.float32,))
     T, k = plan.tokens, plan.top_k
     if r < plan.plan_rows or weights.shape != (T, k) or not weights.is_contiguous():
@@ -534,9 +547,11 @@ def clq_expert_combine(Y, plan, weights, out=None, stream=None):
     _together(device, "plan", plan.data)
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
-            return clq_expert_combine(Y, plan, weights, out)
-    o, ld = _output(out, T, N, Y.dtype, device)
+            return clq_expert_combine(Y, plan, weights, dtype, out)
+    if dtype is None:
+        dtype = out.dtype if out is not None else plan.dtype or Y.dtype
+    o, ld = _output(out, T, N, dtype, device)
     _check(_lib.clq_expert_combine(Y.data_ptr(), _TYPES[Y.dtype], ldy, plan.data.data_ptr() + 4 * plan.at_rows,
-                                   weights.data_ptr(), T, k, plan.experts, N, o.data_ptr(), ld, _raw_stream(i)),
-           "clq_expert_combine")
+                                   weights.data_ptr(), T, k, plan.experts, N, o.data_ptr(), _TYPES[dtype], ld,
+                                   _raw_stream(i)), "clq_expert_combine")
     return o

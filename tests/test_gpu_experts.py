@@ -207,6 +207,47 @@ def test_combine(clq, N):
     assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + k * 2.0 ** -23 * mass).all()
 
 
+@pytest.mark.parametrize("ydt", [F16, BF16, F32])
+@pytest.mark.parametrize("odt", [F16, BF16, F32])
+def test_combine_types(clq, ydt, odt):
+    T, k, E, N = 20, 3, 4, 24
+    plan = clq.clq_expert_plan(torch.randint(0, E, (T, k), dtype=torch.int32).cuda(), E)
+    y, w = torch.randn(plan.plan_rows, N).to(ydt).cuda(), torch.rand(T, k).cuda()
+    got = clq.clq_expert_combine(y, plan, w, dtype=odt)
+    assert got.dtype == odt
+    rows = plan.rows.cpu().numpy()
+    want = (_np(w)[:, :, None] * _np(y)[rows]).sum(1)
+    unit = {F16: 2.0 ** -11, BF16: 2.0 ** -8, F32: 2.0 ** -24}[odt]
+    mass = (np.abs(_np(w))[:, :, None] * np.abs(_np(y)[rows])).sum(1)
+    assert (np.abs(_np(got) - want) <= unit * np.abs(want) + k * 2.0 ** -24 * mass + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_results_that_are_summed_keep_fp32_while_they_are_small(clq, dtype):
+    """One rounding: half a unit of the layer's output, beside the fp32 sums'."""
+    T, K, F, E, k = 33, 128, 128, 4, 3
+    x, w1, b1, w2, b2, gates = _layer(2, T, K, F, E, k, None, dtype)
+    ids = torch.randint(0, E, (T, k), dtype=torch.int32)
+    plan = clq.clq_expert_plan(ids.cuda(), E)
+    q1, q2 = clq.clq_mx4_quantize_weights(w1.cuda()), clq.clq_mx4_quantize_weights(w2.cuda())
+    h = clq.clq_mx4_experts_mx4(clq.clq_mx4_dispatch(x.cuda(), plan), plan, q1, b1.cuda())
+    y = clq.clq_mx4_experts(h, plan, q2, b2.cuda())
+    out = clq.clq_expert_combine(y, plan, gates.cuda())
+    assert y.dtype == F32 and out.dtype == dtype
+    hv, rows = _np(clq.clq_mx4_dequantize(h, F32)), plan.rows.cpu().numpy()
+    wv = _np(clq.clq_mx4_dequantize(q2, F32))
+    want, mass = np.zeros((T, K)), np.zeros((T, K))
+    for j in range(k):
+        e = ids[:, j].numpy()
+        v = hv[rows[:, j]]
+        g = _np(gates)[:, j:j + 1]
+        want += g * (np.einsum("tf,tnf->tn", v, wv[e]) + _np(b2)[e])
+        mass += g * (np.einsum("tf,tnf->tn", np.abs(v), np.abs(wv[e])) + np.abs(_np(b2)[e]))
+    unit = {F16: 2.0 ** -11, BF16: 2.0 ** -8}[dtype]
+    assert (np.abs(_np(out) - want) <= unit * np.abs(want) + (F + k) * 2.0 ** -24 * mass + 2.0 ** -25).all()
+    assert clq.clq_mx4_experts(h, plan, q2, b2.cuda(), dtype=F16).dtype == F16
+
+
 def test_layer_graph_replays(clq):
     T, K, F, E, k = 40, 128, 256, 8, 2
     x, w1, b1, w2, b2, _ = (t.cuda() for t in _layer(3, T, K, F, E, k, "gelu", F16))

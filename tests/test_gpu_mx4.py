@@ -159,6 +159,18 @@ def test_linear(clq, M, N, K, block, bias, dtype):
     _check_product(got, want, np.abs(xv) @ np.abs(wv).T + (0.0 if b is None else np.abs(_np(b))), K, dtype)
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 40, 128), (100, 131, 192), (70, 1152, 4608), (3000, 1000, 256)])
+def test_linear_fp32_result(clq, M, N, K):
+    """The sums as they are, on every kernel, ragged or not."""
+    x, w, b = _rand(M, M, K), _rand(N, N, K, scale=K ** -0.5), _rand(5, N)
+    q, qw = clq.clq_mx4_quantize(x.cuda(), 64), clq.clq_mx4_quantize_weights(w.cuda(), 64)
+    y = clq.clq_mx4_linear(q, qw, b.cuda(), dtype=torch.float32)
+    assert y.dtype == torch.float32 and y.shape == (M, N)
+    xv, wv = ref.quantize(_np(x), 64), ref.quantize(_np(w), 64, divide=64)
+    err = np.abs(_np(y) - (xv @ wv.T + _np(b)))
+    assert (err <= K * 2.0 ** -24 * (np.abs(xv) @ np.abs(wv).T + np.abs(_np(b)))).all()
+
+
 @pytest.mark.parametrize("M,N,K", [(64, 256, 256), (700, 3456, 1152), (2050, 1152, 4608), (4096, 4608, 320)])
 def test_linear_large(clq, M, N, K):
     x, w = _rand(M, M, K), _rand(N, N, K, scale=K ** -0.5)

@@ -95,7 +95,7 @@ def lin(Xq=A, Xs=A, Wq=A, Ws=A, b=None, bt=0, M=4, N=64, K=256, t=0, Y=A, ldy=64
 
 @pytest.mark.parametrize("kw,want", [
     (dict(Xq=None), NULL), (dict(Ws=None), NULL), (dict(Y=None), NULL), (dict(M=0), SHAPE), (dict(N=0), SHAPE),
-    (dict(K=32), SHAPE), (dict(t=2), ARG), (dict(b=A, bt=2), ARG), (dict(ldy=56), SHAPE), (dict(ldy=68), SHAPE),
+    (dict(K=32), SHAPE), (dict(t=3), ARG), (dict(b=A, bt=2), ARG), (dict(ldy=56), SHAPE), (dict(ldy=68), SHAPE),
     (dict(Xs=MIS), ALIGN), (dict(Y=MIS), ALIGN), (dict(b=0x10001), ALIGN), (dict(M=2 ** 31 - 1, N=2 ** 16, ldy=2 ** 16), SHAPE)])
 def test_linear_refusals(kw, want):
     assert lin(**kw) == want
@@ -139,17 +139,17 @@ def test_plan_and_layer_refusals():
     def exp4(tables=A, T=8, k=2, E=4, N=64, act=0, block=0, co=A):
         return L.clq_mx4_experts_mx4(A, A, tables, T, k, E, A, A, None, 0, N, 64, act, block, co, A, None)
 
-    def comb(Y=A, t=0, ldy=64, rows=A, w=A, T=8, k=2, E=4, N=64, out=A, ldo=64):
-        return L.clq_expert_combine(Y, t, ldy, rows, w, T, k, E, N, out, ldo, None)
+    def comb(Y=A, t=0, ldy=64, rows=A, w=A, T=8, k=2, E=4, N=64, out=A, to=0, ldo=64):
+        return L.clq_expert_combine(Y, t, ldy, rows, w, T, k, E, N, out, to, ldo, None)
 
     assert plan(ids=None) == plan(source=None) == NULL and plan(E=0) == plan(k=33) == SHAPE
     assert plan(T=43200, k=8) == NULL and plan(T=43200, k=8, ws=A, wb=16) == WORKSPACE and plan(rows=MIS) == ALIGN
     assert disp(tables=None) == NULL and disp(t=2) == ARG and disp(E=513) == SHAPE and disp(source=MIS) == ALIGN
     assert disp(ldx=60) == SHAPE and disp(block=128) == BLOCK
-    assert exp(tables=None) == exp(Y=None) == NULL and exp(T=0) == SHAPE and exp(ldy=60) == SHAPE and exp(t=2) == ARG
+    assert exp(tables=None) == exp(Y=None) == NULL and exp(T=0) == SHAPE and exp(ldy=60) == SHAPE and exp(t=3) == ARG
     assert exp(tables=MIS) == ALIGN
     assert exp4(co=None) == NULL and exp4(act=2) == SHAPE and exp4(block=128) == BLOCK and exp4(E=600) == SHAPE
-    assert comb(w=None) == NULL and comb(t=2) == ARG and comb(N=0) == SHAPE and comb(ldo=60) == SHAPE
+    assert comb(w=None) == NULL and comb(t=3) == ARG and comb(to=3) == ARG and comb(N=0) == SHAPE and comb(ldo=60) == SHAPE
     assert comb(out=MIS) == ALIGN and comb(k=40) == SHAPE
 
 
