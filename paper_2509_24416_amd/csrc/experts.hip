@@ -26,8 +26,9 @@ namespace {
 // among equal ranks the lowest lane's first one is the lowest index.  Ranks are compared as
 // whole numbers in the floats' order, 0 for an expert that cannot be chosen.  A lane sorts
 // its own experts once; each of the top_k rounds then is a wave maximum of the lanes' heads
-// (six lane permutes) and a pop.  What bounds it are these vector instructions: reading the
-// logits is a tenth of the time at 256 experts.
+// (six lane permutes) and a pop.  What bounds it are these vector instructions, some 600 a token
+// at 256 experts: 43200 tokens to 8 of them in 4 of 8 groups take 47 us, reading the logits 9
+// (one LDS read after another by a lane a group, and shuffles instead of permutes: 89).
 constexpr int kRouteWaves = 4;
 
 template <int CTRL, int ROWS>
@@ -381,7 +382,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
 // ---- combination ------------------------------------------------------------------------------
 // out[t] = sum over the slots, in order and in fp32, of weight * Y[row]; a slot without
 // a row adds nothing.  W columns per thread; the rows and weights of four slots are read
-// ahead of their values, whose loads are then in flight together.  Bound by memory.
+// ahead of their values, whose loads are then in flight together.  Bound by memory (43200 x 1152 of
+// two slots, fp16: 51 us, 5.9 TB/s with the memory-side cache).
 struct CombineArgs {
     const void *Y;
     const int32_t *rows;

@@ -143,6 +143,13 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 // free after the barrier of the quad's first iteration and refilled there with quad q + 2,
 // needed at the end of quad q + 1.  Transfers past the end repeat the last stage or quad,
 // so the wait counts stay constant.
+//
+// What bounds it: the matrix instructions (8 per wave and stage of 32 cycles) and the vector
+// instructions of the epilogue, which do not overlap on a SIMD, and on large products the power
+// limit (the clock falls from 2.4 to 1.6 .. 2.0 GHz).  8192^3 244 us, 4.5 PFLOP/s, matrix cores
+// 68% busy; 43200 x 4608 -> 1152 116 us, 4.0 PFLOP/s; 43200 x 1152 -> 4608 140 to 186 us (2.8
+// TB/s of fp16 results at best; 78 with two stages of k loop), with GELU and requantization 185;
+// 8192 x 1152 -> 4608 the same 41 us.
 constexpr int kBN = 128;
 constexpr int kStageBytes = 4 * kMxUnit;        // 4 / NW units transferred by each wave
 constexpr int kQuadBytes = 4 * kMxScaleRow;

@@ -7,7 +7,8 @@
 // per-token scale needs the whole row), so a workgroup takes a 32-row x 256-column
 // tile and nothing passes through LDS.
 //
-// What bounds it is memory: 2 bytes in and 17/32 out per element.  A lane owns one
+// What bounds it is memory: 2 bytes in and 17/32 out per element (43200 x 4608, b = 64: 97
+// to 118 us, 4.3 to 5.2 TB/s; 8192 x 1152 7 us).  A lane owns one
 // 16-byte chunk (8 columns) of four rows, so that a wave's loads are whole 256-byte
 // pieces, four in flight per lane; stages h = 1, 2, 4 run inside the lane, 8 .. 64
 // across lanes; the group's maximum is over a quad of lanes; the quad transposes
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) mx_quant_kernel(QuantParams p)
 
 // Gathered inputs whose four rows fit LDS: a workgroup takes four rows, staged with the
 // rows' values of a column side by side, so that one 8-byte read gathers a column of all
-// four.  From memory, column by column, 2777 x 4608 took 45 us.
+// four: 2777 x 4608 14 us, from memory column by column 45.
 template <int B, bool BF16>
 __global__ void __launch_bounds__(kGatherThreads) mx_gather_kernel(QuantParams p)
 {
@@ -229,7 +230,8 @@ __global__ void __launch_bounds__(kGatherThreads) mx_gather_kernel(QuantParams p
     }
 }
 
-// The inverse.  A workgroup takes 32 rows x 128 columns, a thread 8 codes of one row twice
+// The inverse, bound by memory (43200 x 4608 to bf16: 90 to 99 us, 5.1 to 5.6 TB/s).  A
+// workgroup takes 32 rows x 128 columns, a thread 8 codes of one row twice
 // over: 16 neighbouring threads store 256 bytes of a row (16-bit types), and the 4-byte
 // pieces of codes that they read are all of the tile's two units between them.
 template <class T>
