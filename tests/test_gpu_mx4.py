@@ -70,6 +70,38 @@ def test_quantize_gathers_and_strides(clq, block):
     _same(_np(clq.clq_mx4_dequantize(q, torch.float32)), ref.quantize(_np(x), block))
 
 
+@pytest.mark.parametrize("K", [64, 12288, 20480, 32768])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_quantize_gathers_of_every_length(clq, K, shift):
+    """Rows that fit LDS by four, rows that do not, and indices off 16-byte boundaries."""
+    x, perm = _rand(K, 6, K, dtype=BF16), _perm(K, K)
+    buf = torch.zeros(K + shift, dtype=torch.int32, device="cuda")
+    buf[shift:] = torch.from_numpy(perm)
+    q = clq.clq_mx4_quantize(x.cuda(), block=64, perm=buf[shift:])
+    _same(_np(clq.clq_mx4_dequantize(q, torch.float32)), ref.quantize(_np(x), 64, perm))
+
+
+def test_offsets_past_32_bits(clq):
+    """Inputs and outputs of more than 2^32 bytes: the last rows are those of the last rows alone."""
+    M, K = 70000, 32768
+    x = torch.empty(M, K, dtype=F16, device="cuda")
+    x[-40:] = torch.randn(40, K, device="cuda", dtype=F16)
+    x[:-40] = 0
+    v = clq.clq_mx4_dequantize(clq.clq_mx4_quantize(x, 64), BF16)
+    assert torch.equal(v[-40:], clq.clq_mx4_dequantize(clq.clq_mx4_quantize(x[-40:], 64), BF16))
+    assert (v[-140:-40] == 0).all()
+    del x, v
+    M, N = 300000, 8192
+    x, w = torch.zeros(M, 64, dtype=F16, device="cuda"), torch.randn(N, 64, device="cuda", dtype=F16)
+    x[-33:] = torch.randn(33, 64, device="cuda", dtype=F16)
+    qw = clq.clq_mx4_quantize_weights(w)
+    y = clq.clq_mx4_linear(clq.clq_mx4_quantize(x), qw)
+    xv, wv = clq.clq_mx4_dequantize(clq.clq_mx4_quantize(x[-33:]), torch.float32), clq.clq_mx4_dequantize(qw, torch.float32)
+    want, mass = xv.double() @ wv.double().t().contiguous(), xv.abs() @ wv.abs().t().contiguous()
+    assert ((y[-33:].double() - want).abs() <= UNIT[F16] * want.abs() + 2.0 ** -18 * mass + 2.0 ** -25).all()
+    assert (y[:-33:997] == 0).all() and (y[-34] == 0).all()
+
+
 def test_quantize_every_rounding(clq):
     """Every fp16 magnitude up to 8 next to a 4 (scale 1): ties, saturation, both signs."""
     h = torch.arange(0, 0x4800 + 1, dtype=torch.int32).to(torch.int16).view(F16)
