@@ -414,7 +414,8 @@ def clq_expert_route(logits, top_k, score="softmax", bias=None, groups=1, top_gr
             return clq_expert_route(logits, top_k, score, bias, groups, top_groups, renormalize, scale)
     ids = torch.empty(T, top_k, dtype=torch.int32, device=device)
     weights = torch.empty(T, top_k, dtype=torch.float32, device=device)
-    _check(_lib.clq_expert_route(logits.data_ptr(), _TYPES[logits.dtype], max(ld, E), T, E, top_k, _SCORES[score], b,
+    # (a single row has no stride of its own)
+    _check(_lib.clq_expert_route(logits.data_ptr(), _TYPES[logits.dtype], ld if T > 1 else E, T, E, top_k, _SCORES[score], b,
                                  groups, top_groups, int(renormalize), scale, ids.data_ptr(), weights.data_ptr(),
                                  _raw_stream(i)), "clq_expert_route")
     return ids, weights

@@ -98,6 +98,15 @@ def test_route_strided_logits(clq):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_route_refuses_rows_that_overlap(clq):
+    x = torch.randn(4, 64, device="cuda")
+    for bad in (x[:1].expand(50, 64), x[:, :1].as_strided((50, 1), (0, 1)), x.as_strided((50, 64), (3, 1))):
+        with pytest.raises(clq.ClqError):
+            clq.clq_expert_route(bad, 1)
+    one = clq.clq_expert_route(x[:1].expand(1, 64), 6)
+    assert torch.equal(one[0], clq.clq_expert_route(x, 6)[0][:1])
+
+
 # ---- plan ----------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("T,k,E,kind", [
