@@ -199,9 +199,14 @@ def _buffer(out, rows, K, block, device, where):
         if data.numel() < n or not data.is_contiguous():
             raise ValueError("the output's buffer is too small")
         _together(device, "out", data)
-        out.rows, out.K, out.block = rows, K, block
     p = data.data_ptr()
     return out, p, p + codes
+
+
+def _holds(out, rows, K, block):
+    """`out` once a call has filled it (one that was refused leaves it what it was)."""
+    out.rows, out.K, out.block = rows, K, block
+    return out
 
 
 def clq_mx4_quantize(X, block=0, perm=None, out=None, stream=None):
@@ -217,7 +222,7 @@ def clq_mx4_quantize(X, block=0, perm=None, out=None, stream=None):
     q, codes, scales = _buffer(out, M, K, block, device, "clq_mx4_quantize")
     _check(_lib.clq_mx4_quantize(X.data_ptr(), _TYPES[X.dtype], ldx, None if perm is None else _gather(perm, K, device),
                                  M, K, block, codes, scales, _raw_stream(i)), "clq_mx4_quantize")
-    return q
+    return _holds(q, M, K, block)
 
 
 def _weight_shape(W, name):
@@ -383,7 +388,7 @@ def clq_mx4_linear_mx4(q, qw, bias=None, act=None, block=0, out=None, stream=Non
     p = q.data.data_ptr()
     _check(_lib.clq_mx4_linear_mx4(p, p + _code_bytes(M, K), qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, M, qw.N,
                                    K, a, block, codes, scales, _raw_stream(i)), "clq_mx4_linear_mx4")
-    return o
+    return _holds(o, M, C, block)
 
 
 def clq_expert_route(logits, top_k, score="softmax", bias=None, groups=1, top_groups=1, renormalize=True, scale=1.0,
@@ -415,9 +420,9 @@ def clq_expert_route(logits, top_k, score="softmax", bias=None, groups=1, top_gr
     ids = torch.empty(T, top_k, dtype=torch.int32, device=device)
     weights = torch.empty(T, top_k, dtype=torch.float32, device=device)
     # (a single row has no stride of its own)
-    _check(_lib.clq_expert_route(logits.data_ptr(), _TYPES[logits.dtype], ld if T > 1 else E, T, E, top_k, _SCORES[score], b,
-                                 groups, top_groups, int(renormalize), scale, ids.data_ptr(), weights.data_ptr(),
-                                 _raw_stream(i)), "clq_expert_route")
+    _check(_lib.clq_expert_route(logits.data_ptr(), _TYPES[logits.dtype], ld if T > 1 else E, T, E, top_k,
+                                 _SCORES[score], b, groups, top_groups, int(renormalize), scale, ids.data_ptr(),
+                                 weights.data_ptr(), _raw_stream(i)), "clq_expert_route")
     return ids, weights
 
 
@@ -475,7 +480,7 @@ def clq_mx4_dispatch(X, plan, block=0, perm=None, out=None, stream=None):
     _check(_lib.clq_mx4_dispatch(X.data_ptr(), _TYPES[X.dtype], ldx, g, T, plan.top_k, plan.experts, K, block, t,
                                  t + 4 * plan.at_source, codes, scales, _raw_stream(i)), "clq_mx4_dispatch")
     plan.dtype = X.dtype
-    return q
+    return _holds(q, n, K, block)
 
 
 def _plan_operands(q, plan, qw, bias):
@@ -531,7 +536,7 @@ def clq_mx4_experts_mx4(q, plan, qw, bias=None, act=None, block=0, out=None, str
     _check(_lib.clq_mx4_experts_mx4(p, p + _code_bytes(M, K), plan.data.data_ptr(), plan.tokens, plan.top_k,
                                     plan.experts, qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, qw.N, K, a, block,
                                     codes, scales, _raw_stream(i)), "clq_mx4_experts_mx4")
-    return o
+    return _holds(o, M, C, block)
 
 
 def clq_expert_combine(Y, plan, weights, dtype=None, out=None, stream=None):

@@ -336,6 +336,20 @@ def test_mlp_through_both_products(clq):
 
 # ---- streams and graphs ------------------------------------------------------------------------
 
+def test_refused_calls_leave_their_output_alone(clq):
+    x, w = _rand(1, 300, 1152).cuda(), _rand(2, 640, 1152).cuda()
+    q, qw = clq.clq_mx4_quantize(x, 64), clq.clq_mx4_quantize_weights(w, 64)
+    o = clq.clq_mx4_quantize(x[:70, :256], 32)
+    want = clq.clq_mx4_dequantize(o)
+    o.data.resize_(1 << 20)
+    for call in (lambda: clq.clq_mx4_quantize(x[:, 1:65], 64, out=o), lambda: clq.clq_mx4_quantize(x, 48, out=o),
+                 lambda: clq.clq_mx4_linear_mx4(q, qw, block=48, out=o)):
+        with pytest.raises(clq.ClqError):
+            call()
+        assert (o.rows, o.K, o.block) == (70, 256, 32)
+    assert torch.equal(clq.clq_mx4_dequantize(o), want)
+
+
 def test_side_stream(clq):
     x, w = _rand(1, 300, 1152).cuda(), _rand(2, 640, 1152).cuda()
     want = clq.clq_mx4_linear(clq.clq_mx4_quantize(x, 64), clq.clq_mx4_quantize_weights(w, 64))
