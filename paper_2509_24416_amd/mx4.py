@@ -65,6 +65,8 @@ class MX4:
 
     def __init__(self, data, rows, K, block=0):
         self.data, self.rows, self.K, self.block = data, rows, K, block
+        if data.is_cuda:
+            _bytes(data, _code_bytes(rows, K) + _scale_bytes(rows, K), "data")
 
     @property
     def codes(self):
@@ -90,6 +92,13 @@ class MX4Weight:
     perm: torch.Tensor = None
     experts: int = None     # None: a plain matrix
     gated: bool = False
+
+    def __post_init__(self):
+        if self.codes.is_cuda:
+            rows = (self.experts or 1) * ((self.N + 63) // 64 * 64)
+            _bytes(self.codes, _code_bytes(rows, self.K), "codes")
+            _bytes(self.scales, _scale_bytes(rows, self.K), "scales")
+            _together(self.codes.device, "scales", self.scales)
 
 
 class ExpertPlan:
@@ -167,6 +176,11 @@ def _elsewhere(device, stream):
     return torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
 
 
+def _bytes(t, n, name):
+    if t.dtype is not torch.uint8 or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous uint8 tensor of at least {n} bytes")
+
+
 def _code_bytes(rows, K):
     return (rows + 31) // 32 * 32 * (K // 2)
 
@@ -184,8 +198,8 @@ def clq_mx4_scale_bytes(rows, K, weights=False):
 
 
 def _buffer(out, rows, K, block, device, where):
-    """An MX4 of that shape, the caller's, checked, or a new one; its codes' and scales'
-    pointers."""
+    """A buffer for an MX4 of that shape, the caller's, checked, or a new one; its codes' and
+    scales' pointers."""
     if not 0 < rows < 2147483648 or not 64 <= K <= 32768 or K & 63:
         raise ClqError(CLQ_ERR_SHAPE, where)
     units = (rows + 31) >> 5
@@ -193,7 +207,8 @@ def _buffer(out, rows, K, block, device, where):
     n = codes + (units * ((K + 255) >> 8) << 8)
     if out is None:
         data = torch.empty(n, dtype=torch.uint8, device=device)
-        out = MX4(data, rows, K, block)
+        out = object.__new__(MX4)   # (of that size: nothing to check)
+        out.data = data
     else:
         data = _dev(out.data, "out", (torch.uint8,))
         if data.numel() < n or not data.is_contiguous():
@@ -330,6 +345,11 @@ def _product(q, qw, bias, experts):
     return device, bias.data_ptr(), _TYPES[bias.dtype]
 
 
+def _distinct(q, out):
+    if out is not None and out.data.data_ptr() == q.data.data_ptr():
+        raise ValueError("the output's buffer is the input's")
+
+
 def _output(out, rows, N, dtype, device):
     if dtype not in _TYPES:
         raise TypeError(f"dtype must be fp16, bf16 or fp32, got {dtype}")
@@ -379,6 +399,7 @@ def clq_mx4_linear_mx4(q, qw, bias=None, act=None, block=0, out=None, stream=Non
     (gated weights, N / 2 columns)."""
     a = _act(act)
     device, b, bt = _product(q, qw, bias, None)
+    _distinct(q, out)
     i = device.index
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
@@ -526,6 +547,7 @@ def clq_mx4_experts_mx4(q, plan, qw, bias=None, act=None, block=0, out=None, str
     """clq_mx4_linear_mx4 with each row times its expert's weights."""
     a = _act(act)
     device, b, bt = _plan_operands(q, plan, qw, bias)
+    _distinct(q, out)
     i = device.index
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):

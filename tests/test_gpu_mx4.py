@@ -350,6 +350,21 @@ def test_refused_calls_leave_their_output_alone(clq):
     assert torch.equal(clq.clq_mx4_dequantize(o), want)
 
 
+def test_buffers_of_the_wrong_size_are_refused(clq):
+    def u8(n):
+        return torch.zeros(n, dtype=torch.uint8, device="cuda")
+
+    clq.MX4(u8(2 * 512 * 2 + 512), 33, 64)
+    clq.MX4Weight(u8(2 * 64 * 160), u8(2 * 2 * 512), 64, 320, experts=2)
+    for make in (lambda: clq.MX4(u8(2 * 512 * 2 + 511), 33, 64), lambda: clq.MX4(u8(4096).half(), 33, 64),
+                 lambda: clq.MX4(u8(8192)[::2], 33, 64),
+                 lambda: clq.MX4Weight(u8(2 * 64 * 160 - 1), u8(2 * 2 * 512), 64, 320, experts=2),
+                 lambda: clq.MX4Weight(u8(2 * 64 * 160), u8(2 * 2 * 512 - 1), 64, 320, experts=2),
+                 lambda: clq.MX4Weight(u8(2 * 64 * 160), u8(2 * 2 * 512).cpu(), 64, 320, experts=2)):
+        with pytest.raises(ValueError):
+            make()
+
+
 def test_side_stream(clq):
     x, w = _rand(1, 300, 1152).cuda(), _rand(2, 640, 1152).cuda()
     want = clq.clq_mx4_linear(clq.clq_mx4_quantize(x, 64), clq.clq_mx4_quantize_weights(w, 64))

@@ -176,6 +176,17 @@ def test_binding_refuses_host_tensors_and_wrong_kinds():
         clq.clq_mx4_linear_mx4(a, w, act="relu")
 
 
+def test_binding_refuses_to_write_over_its_input():
+    q = clq.MX4(torch.zeros(32 * 32 + 256, dtype=torch.uint8), 4, 64)
+    w = clq.MX4Weight(torch.zeros(64 * 32, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 64, 64)
+    plan = clq.ExpertPlan(torch.zeros(4, dtype=torch.int32), 1, 1, None, 4, 0)
+    for out in (q, clq.MX4(q.data, 4, 64), clq.MX4(q.data.view(-1), 4, 64)):
+        with pytest.raises(ValueError, match="output"):
+            clq.clq_mx4_linear_mx4(q, w, out=out)
+        with pytest.raises(ValueError, match="output"):
+            clq.clq_mx4_experts_mx4(q, plan, w, out=out)
+
+
 # ---- pins of the oracle itself -----------------------------------------------------------
 
 def test_oracle_grid_by_hand():
