@@ -127,14 +127,15 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 }
 
 // ---- the tile kernel ---------------------------------------------------------------
-// A workgroup of NW waves computes 128 channels x 64 NW tokens, each wave 128 channels x 64
-// tokens (4 x 2 fragments of 32 x 32).  A k-stage is 64 codes, one matrix instruction per
-// fragment.  The channel units are shared by the waves: they go global -> LDS without
-// registers through a ring of NS stages, and a wave reads a stage's units back one stage
-// ahead of its use.  The token units belong to one wave each and go straight to registers,
-// kDepth stages ahead (through LDS the reads and writes of both operands came to 144 of
-// its 128 bytes a clock at full rate).  The scale dwords of four stages (a quad) take the
-// same two ways, the channels' through a ring of two, read at the end of the quad before.
+// A workgroup of NW waves computes 32 FN channels x 64 NW tokens, each wave all of the channels
+// x 64 tokens (FN x 2 fragments of 32 x 32; FN = 4, or 3 where that fills the chip better).  A
+// k-stage is 64 codes, one matrix instruction per fragment.  The channel units are shared by
+// the waves: they go global -> LDS without registers through a ring of NS stages, and a wave
+// reads a stage's units back one stage ahead of its use.  The token units belong to one wave
+// each and go straight to registers, kDepth stages ahead (through LDS the reads and writes of
+// both operands came to 144 of its 128 bytes a clock at full rate).  The scale dwords of four
+// stages (a quad) take the same two ways, the channels' through a ring of two, read at the end
+// of the quad before.
 //
 // Ring protocol: iteration s waits until stage s + 1 has landed (transfers and loads
 // complete in issue order: at most the later stages' may be outstanding) and its own LDS
@@ -150,22 +151,24 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 // 68% busy; 43200 x 4608 -> 1152 116 us, 4.0 PFLOP/s; 43200 x 1152 -> 4608 140 to 186 us (2.8
 // TB/s of fp16 results at best; 78 with two stages of k loop), with GELU and requantization 185;
 // 8192 x 1152 -> 4608 the same 41 us.
-constexpr int kBN = 128;
-constexpr int kStageBytes = 4 * kMxUnit;        // 4 / NW units transferred by each wave
+constexpr int kBN = 128;                        // channels (FN = 4)
+constexpr int kStageBytes = 4 * kMxUnit;        // 4 / NW units from each wave (FN = 3: the last twice)
 constexpr int kQuadBytes = 4 * kMxScaleRow;
 constexpr int kDepth = 4;                       // stages of token units in registers
 // Ring of channel units: one more than kDepth, so that the stages that the prologue leaves in
 // flight are as many transfers and loads as the loop's wait counts take them for.
 constexpr int kStages = kDepth + 1;
 
+template <int FN>
 struct Operands {
-    v4u w[4];
+    v4u w[FN];
     __device__ __forceinline__ void read(uint32_t wa) {
-        static_for<0, 4>([&](auto f) { w[f] = read16<decltype(f)::value * kMxUnit>(wa); });
+        static_for<0, FN>([&](auto f) { w[f] = read16<decltype(f)::value * kMxUnit>(wa); });
     }
 };
+template <int FN>
 struct Scales {
-    uint32_t s[4];
+    uint32_t s[FN];
 };
 // At most VM transfers outstanding, the LDS reads in, the workgroup barrier.  The
 // destinations of those reads are named, so that nothing touches them before; a
@@ -174,14 +177,25 @@ struct Scales {
 // ahead of this wait).
 #define CLQ_MX_WAIT "s_waitcnt vmcnt(%c[vm]) lgkmcnt(0)\n\ts_barrier"
 template <int VM>
-__device__ __forceinline__ void wait_stage(Operands &o) {
+__device__ __forceinline__ void wait_stage(Operands<4> &o) {
     asm volatile(CLQ_MX_WAIT : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(o.w[3]) : [vm] "n"(VM) : "memory");
 }
 template <int VM>
-__device__ __forceinline__ void wait_stage(Operands &o, Scales &s) {
+__device__ __forceinline__ void wait_stage(Operands<4> &o, Scales<4> &s) {
     asm volatile(CLQ_MX_WAIT
                  : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(o.w[3]), "+v"(s.s[0]), "+v"(s.s[1]), "+v"(s.s[2]),
                    "+v"(s.s[3])
+                 : [vm] "n"(VM)
+                 : "memory");
+}
+template <int VM>
+__device__ __forceinline__ void wait_stage(Operands<3> &o) {
+    asm volatile(CLQ_MX_WAIT : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]) : [vm] "n"(VM) : "memory");
+}
+template <int VM>
+__device__ __forceinline__ void wait_stage(Operands<3> &o, Scales<3> &s) {
+    asm volatile(CLQ_MX_WAIT
+                 : "+v"(o.w[0]), "+v"(o.w[1]), "+v"(o.w[2]), "+v"(s.s[0]), "+v"(s.s[1]), "+v"(s.s[2])
                  : [vm] "n"(VM)
                  : "memory");
 }
@@ -231,15 +245,15 @@ __device__ __forceinline__ void store8(const Args &a, const float *s, int64_t m,
 // are 64 bytes a lane, whole requests as they are.)
 constexpr int kRowPitch = 272, kTurnBytes = 32 * kRowPitch;
 
-template <bool RAGGED, MxType T>
-__device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][2], int fm, uint8_t *turn, int64_t row0,
+template <int FN, bool RAGGED, MxType T>
+__device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[FN][2], int fm, uint8_t *turn, int64_t row0,
                                             int64_t row_end, int n0, int lane) {
     const int h16 = (lane >> 5) * 16;
     if constexpr (T == MxType::F32) {
         const int64_t m = row0 + (lane & 31);
         if (m >= row_end) return;
 #pragma unroll
-        for (int fn = 0; fn < 4; ++fn)
+        for (int fn = 0; fn < FN; ++fn)
 #pragma unroll
             for (int q = 0; q < 16; q += 8) {
                 const int n = n0 + fn * 32 + h16 + q;
@@ -252,7 +266,7 @@ __device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][
     }
     uint8_t *w = turn + (lane & 31) * kRowPitch + h16 * 2;
 #pragma unroll
-    for (int fn = 0; fn < 4; ++fn) {
+    for (int fn = 0; fn < FN; ++fn) {
         const v16f &x = acc[fn][fm];
         uint32_t h[8];
 #pragma unroll
@@ -262,7 +276,7 @@ __device__ __forceinline__ void store_plain(const Args &a, const v16f (&acc)[4][
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses stay in order)
     const int c = lane & 15, n = n0 + 8 * c;
-    if (n >= a.N) return;
+    if (c >= 4 * FN || n >= a.N) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = i * 4 + (lane >> 4);
@@ -359,14 +373,16 @@ __device__ __forceinline__ void requantize(const Args &a, float (&f)[NF][16], in
     }
 }
 
-template <int NW, Out OUT, int B, bool GROUPED, bool RAGGED, MxType T>
+template <int NW, int FN, Out OUT, int B, bool GROUPED, bool RAGGED, MxType T>
 __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
 {
     constexpr int NS = kStages, PPW = 4 / NW;   // transfers per wave and stage
+    constexpr int BN = 32 * FN;   // channels
     constexpr bool GATED = OUT == Out::Swiglu;
+    static_assert(FN == 4 || OUT == Out::Plain, "a requantized tile");
     constexpr int kRing = NS * kStageBytes + 2 * kQuadBytes, kTurn = OUT == Out::Plain && T != MxType::F32 ? NW * kTurnBytes : 0;
     __shared__ __align__(16) uint8_t pool[kRing > kTurn ? kRing : kTurn];
-    __shared__ __align__(16) float ep[kBN];   // biases
+    __shared__ __align__(16) float ep[BN];   // biases
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nks = a.K >> 6, nq = (a.K + 255) >> 8;
@@ -399,7 +415,7 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
     Buffer wsrc[PPW], wssrc[PPW];
     static_for<0, PPW>([&](auto ic) {
         constexpr int i = decltype(ic)::value;
-        const int64_t wu = min(tn * 4 + wave * PPW + i, a.wunits - 1);
+        const int64_t wu = min(tn * FN + min(wave * PPW + i, FN - 1), a.wunits - 1);
         wsrc[i] = buffer_of(Wq + wu * nks * kMxUnit, (uint32_t)(nks * kMxUnit));
         wssrc[i] = buffer_of(Ws + wu * nq * kMxScaleRow, (uint32_t)(nq * kMxScaleRow));
     });
@@ -439,19 +455,19 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
     };
 
     // a channel's bias per thread: every sum starts from it
-    static_assert(NW * 64 >= kBN, "a thread per channel");
+    static_assert(NW * 64 >= BN, "a thread per channel");
     uint16_t bv = 0;
-    if (a.bias && tid < kBN)
-        bv = a.bias[(int64_t)rt.expert * a.N + bias_index(min(tn * kBN + tid, a.N - 1), a.N, GATED)];
+    if (a.bias && tid < BN)
+        bv = a.bias[(int64_t)rt.expert * a.N + bias_index(min(tn * BN + tid, a.N - 1), a.N, GATED)];
     __builtin_amdgcn_sched_barrier(0);
 
     // ---- k loop ------------------------------------------------------------------------
-    Operands op[2];
-    Scales sc[2];   // channel scales of even and odd quads
+    Operands<FN> op[2];
+    Scales<FN> sc[2];   // channel scales of even and odd quads
     const uint32_t wl = pool0 + l16, sl = spool + l4;
     auto read_scales = [&](auto qc) __attribute__((always_inline)) {
         constexpr int Q = decltype(qc)::value;
-        static_for<0, 4>([&](auto f) { sc[Q].s[f] = read4<Q * kQuadBytes + decltype(f)::value * kMxScaleRow>(sl); });
+        static_for<0, FN>([&](auto f) { sc[Q].s[f] = read4<Q * kQuadBytes + decltype(f)::value * kMxScaleRow>(sl); });
     };
     // prologue: two quads of scales and NS stages in flight, stage 0 and quad 0 landed
     produce_scales(0, 0);
@@ -464,12 +480,12 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
         if constexpr (Q < kDepth) load_x(qc, Q);
         __builtin_amdgcn_sched_barrier(0);
     });
-    if (tid < kBN) ep[tid] = widen(bv, a.bias_bf16);
+    if (tid < BN) ep[tid] = widen(bv, a.bias_bf16);
     // outstanding: what came after stage 0's transfers and loads
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 1) * PPW + 2 * (kDepth - 1)) : "memory");
-    v16f acc[4][2];
+    v16f acc[FN][2];
     const int h16 = (lane >> 5) * 16;
-    static_for<0, 4>([&](auto fc) {
+    static_for<0, FN>([&](auto fc) {
         constexpr int fn = decltype(fc)::value;
         const v4f *b = reinterpret_cast<const v4f *>(ep + fn * 32 + h16);
 #pragma unroll
@@ -496,7 +512,7 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
             load_xs(IC<1 - Q>{}, q);
             produce_scales(Q * kQuadBytes, ++q);
         }
-        static_for<0, 4>([&](auto fc) {
+        static_for<0, FN>([&](auto fc) {
             static_for<0, 2>([&](auto mc) {
                 constexpr int fn = decltype(fc)::value, fm = decltype(mc)::value;
                 acc[fn][fm] = mfma_mx4<P>(op[R].w[fn], x[P][fm], acc[fn][fm], sc[Q].s[fn], xs[Q][fm]);
@@ -523,7 +539,7 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
         if (u >= rt.unit_end) return;
         if constexpr (OUT == Out::Plain) {
             const int64_t end = GROUPED ? (int64_t)rt.unit_end * 32 : a.M;
-            store_plain<RAGGED, T>(a, acc, fm, pool + wave * kTurnBytes, (int64_t)u * 32, end, tn * kBN, lane);
+            store_plain<FN, RAGGED, T>(a, acc, fm, pool + wave * kTurnBytes, (int64_t)u * 32, end, tn * BN, lane);
         } else if constexpr (GATED) {
             float f[2][16];
             static_for<0, 2>([&](auto pc) {
@@ -723,15 +739,16 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
     }
 }
 
-// The kernels: tiles of 32 and 64 rows split over the k loop, of 128 and of 256 rows.
-enum Kernel { kSplit1, kSplit2, kTile128, kTile256 };
-constexpr int kLogUnits[] = {0, 1, 2, 3};   // row units of a tile
+// The kernels: tiles of 32 and 64 rows split over the k loop, of 128 and of 256 rows, the latter
+// also of 96 channels.
+enum Kernel { kSplit1, kSplit2, kTile128, kTile256, kTile256x96 };
+constexpr int kLogUnits[] = {0, 1, 2, 3, 3};   // row units of a tile
 
 template <Out OUT, int B, bool GROUPED, bool RAGGED, MxType T>
 void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
     using S1 = std::conditional_t<OUT == Out::Plain, Split1, SplitMx>;
     using S2 = std::conditional_t<OUT == Out::Plain && !GROUPED, Split2, S1>;
-    const int bn = kernel == kSplit1 ? S1::BN : kernel == kSplit2 ? S2::BN : kBN;
+    const int bn = kernel == kSplit1 ? S1::BN : kernel == kSplit2 ? S2::BN : kernel == kTile256x96 ? 96 : kBN;
     a.tiles_n = (a.N + bn - 1) / bn;
     const dim3 grid((unsigned)(row_tiles * a.tiles_n));
     switch (kernel) {
@@ -742,10 +759,14 @@ void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
             hipLaunchKernelGGL((mx_split_kernel<S2, OUT, B, GROUPED, RAGGED, T>), grid, dim3(S2::NT), 0, stream, a);
             break;
         case kTile128:
-            hipLaunchKernelGGL((mx_tile_kernel<2, OUT, B, GROUPED, RAGGED, T>), grid, dim3(128), 0, stream, a);
+            hipLaunchKernelGGL((mx_tile_kernel<2, 4, OUT, B, GROUPED, RAGGED, T>), grid, dim3(128), 0, stream, a);
             break;
         case kTile256:
-            hipLaunchKernelGGL((mx_tile_kernel<4, OUT, B, GROUPED, RAGGED, T>), grid, dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((mx_tile_kernel<4, 4, OUT, B, GROUPED, RAGGED, T>), grid, dim3(256), 0, stream, a);
+            break;
+        case kTile256x96:
+            if constexpr (OUT == Out::Plain && !GROUPED)
+                hipLaunchKernelGGL((mx_tile_kernel<4, 3, OUT, B, GROUPED, RAGGED, T>), grid, dim3(256), 0, stream, a);
             break;
     }
 }
@@ -811,7 +832,12 @@ hipError_t launch_out(const Args &a, MxAct act, int block, Kernel kernel, int64_
 //        17.2; 4096, 288: 51.4 / 28.6 / 24.2 / 18.0), and for experts of under 512 rows on
 //        average, whose last tiles are half empty (384 rows, 1152 -> 1536 gated: 38.5 of 128 /
 //        41.8 of 256; 512 rows, 1152 -> 4608: 51.6 / 50.2; 5400: 405 / 399);
-//   256  otherwise: the fewest operand bytes (43200 x 1152 -> 4608: 189 of 128 / 171 of 256).
+//   256  otherwise: the fewest operand bytes (43200 x 1152 -> 4608: 189 of 128 / 171 of 256);
+//        96 channels instead of 128, plain, where they take no more rounds of one tile to a unit
+//        (us of 128 / 96 channels, tiles: 4608 -> 1152 with 4096 rows, 144 / 192, 19.1 / 16.9; 8192,
+//        288 / 384, 30.0 / 26.5; 16384, 576 / 768, 49.0 / 44.7; but 5400, 198 / 264, 20.8 / 25.7;
+//        20000, 711 / 948, 52.9 / 58.1; 8192 x 1152 -> 1152, 288 / 384, 16.1 / 14.6; 8192^3, 2048 /
+//        2752, 230 / 251).
 inline Kernel pick_kernel(const MxGemmArgs &g, int64_t units, int64_t c) {
     const bool mx4 = g.Y == nullptr, longk = g.K >= 48 * 64;
     if (mx4) {
@@ -830,7 +856,9 @@ inline Kernel pick_kernel(const MxGemmArgs &g, int64_t units, int64_t c) {
         if (g.assignments < 512 * (int64_t)g.experts || (g.assignments / 128 + nonempty) * tiles_n <= c) return kTile128;
         return kTile256;
     }
-    return (units + 3) / 4 * tiles_n <= c ? kTile128 : kTile256;
+    if ((units + 3) / 4 * tiles_n <= c) return kTile128;
+    const int64_t rows = (units + 7) / 8, rounds = (rows * tiles_n + c - 1) / c;
+    return !mx4 && rows * ((g.N + 95) / 96) <= rounds * c ? kTile256x96 : kTile256;
 }
 
 }  // namespace mx

@@ -213,6 +213,25 @@ def test_linear_large(clq, M, N, K):
     _check_product(got, (xv @ wv.T).numpy(), (xv.abs() @ wv.abs().T).numpy(), K, F16)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, torch.float32])
+@pytest.mark.parametrize("M,N,K", [(4100, 1152, 4608), (8195, 1147, 192), (20001, 288, 64), (40000, 90, 320), (40000, 57, 128)])
+def test_linear_narrow_tiles(clq, M, N, K, dtype):
+    """Tiles of 96 channels: whole and ragged, every length of the last eight stages' rest."""
+    bd = BF16 if dtype is BF16 else F16
+    x, w, b = _rand(M, M, K, dtype=bd), _rand(N, N, K, scale=K ** -0.5, dtype=bd), _rand(7, N, dtype=bd)
+    q, qw = clq.clq_mx4_quantize(x.cuda(), 64), clq.clq_mx4_quantize_weights(w.cuda(), 64)
+    buf = torch.full((M + 1, (N + 7) // 8 * 8 + 8), 7.0, dtype=dtype, device="cuda")
+    got = clq.clq_mx4_linear(q, qw, b.cuda(), dtype=dtype, out=buf[:M, :N])
+    xv, wv = clq.clq_mx4_dequantize(q, torch.float32).cpu(), clq.clq_mx4_dequantize(qw, torch.float32).cpu()
+    want = (xv.double() @ wv.double().T + b.double()).numpy()
+    mass = (xv.abs() @ wv.abs().T + b.abs().float()).numpy()
+    if dtype is torch.float32:
+        assert (np.abs(_np(got) - want) <= K * 2.0 ** -24 * mass).all()
+    else:
+        _check_product(_np(got), want, mass, K, dtype)
+    assert (buf[:, N:] == 7).all() and (buf[M] == 7).all()
+
+
 @pytest.mark.parametrize("M,N,K", [(43200, 4608, 1152), (20000, 1152, 4608), (30000, 3456, 192)])
 def test_linear_many_tiles(clq, M, N, K):
     """Many rounds of workgroups under full memory load, several times over: a transfer that was
