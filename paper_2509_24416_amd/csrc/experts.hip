@@ -241,20 +241,21 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
 }
 
 // ---- plan ---------------------------------------------------------------------------------
-// A stable counting sort.  A block owns a run of kPlanRun assignments; the first kernel
+// A stable counting sort.  A block owns a run of 1024 PER assignments; the first kernel
 // counts its experts, the second adds the counts of the runs before (every block for
 // itself: they are a few hundred rows of E counts), and places its own.  One run is a single
 // launch; past it two are quicker than every block counting all assignments (24576 to 64
-// experts: 4.8 + 6.9 us against 15.6).  Latency bounds it: 345600 to 256 experts take 5 + 12.
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kPlanPer = 4, kPlanRun = kPlanThreads * kPlanPer;
+// experts, 4 a thread: 4.8 + 6.9 us against 15.6).  Latency bounds it.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 
+template <int PER>
 __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const int32_t *ids, int64_t n, int E, int32_t *hist)
 {
     extern __shared__ int32_t count[];
     for (int e = threadIdx.x; e < E; e += kPlanThreads) count[e] = 0;
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * kPlanRun;
-    for (int j = 0; j < kPlanPer; ++j) {
+    const int64_t i0 = (int64_t)blockIdx.x * (kPlanThreads * PER);
+    for (int j = 0; j < PER; ++j) {
         const int64_t i = i0 + j * kPlanThreads + threadIdx.x;
         if (i < n) {
             const int id = ids[i];
@@ -266,6 +267,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const int32_t 
 }
 
 // hist: counts of every run (nullptr: there is one run, counted here)
+template <int PER>
 __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t *ids, int64_t n, int k, int E, int runs,
                                                                   const int32_t *hist, int32_t *info, int32_t *rows,
                                                                   int32_t *source)
@@ -280,11 +282,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
     for (int i = tid; i < kPlanWaves * E; i += kPlanThreads) wcount[i] = 0;
     for (int i = tid; i < E; i += kPlanThreads) all[i] = prior[i] = 0;
     __syncthreads();
-    // a wave owns 64 * kPlanPer consecutive assignments
-    const int64_t i0 = (int64_t)blockIdx.x * kPlanRun + wave * 64 * kPlanPer;
-    int id[kPlanPer];
+    // a wave owns 64 * PER consecutive assignments
+    const int64_t i0 = (int64_t)blockIdx.x * (kPlanThreads * PER) + wave * 64 * PER;
+    int id[PER];
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j) {
+    for (int j = 0; j < PER; ++j) {
         const int64_t i = i0 + j * 64 + lane;
         id[j] = i < n ? ids[i] : -1;
         if (id[j] < 0 || id[j] >= E) id[j] = -1;
@@ -349,7 +351,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
     __syncthreads();
     // place: 64 assignments at a time, in order
 #pragma unroll
-    for (int j = 0; j < kPlanPer; ++j) {
+    for (int j = 0; j < PER; ++j) {
         const int64_t i = i0 + j * 64 + lane;
         // lanes with the same expert
         uint64_t same = __ballot(id[j] >= 0);
@@ -377,6 +379,42 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
             const int e = i >> 5, r = first[e] * 32 + all[e] + (i & 31);
             if (r < first[e + 1] * 32) source[r] = -1;
         }
+}
+
+// Assignments of a thread.  Short runs fill more of the chip, until there is more than one a
+// compute unit or the counts of all runs, which every block reads, take longer.  us with 1 / 2 / 4
+// (both launches): 4096 x 6 to 64 experts 6.4 / 7.4 / 9.2; 8192 x 8 to 256, 64 / 32 / 16 runs,
+// 9.6 / 10.0 / 12.5; 10800 x 8, 85 / 43 / 22, 11.5 / 10.7 / 12.9; 43200 x 8, 338 / 169 / 85, 22.6 /
+// 14.2 / 14.7; 100000 x 8 to 64, 782 / 391 / 196, 25.8 / 14.5 / 13.0, to 512, 114 / 42.7 / 25.7.  One
+// run, a single launch, where there can be one: 512 x 2 to 16 3.4 / 3.7 / 4.7.
+inline int64_t plan_runs(int64_t n, int per) { return (n + kPlanThreads * per - 1) / (kPlanThreads * per); }
+// the most runs that there are of `per` assignments a thread (no limit for 4)
+inline int64_t plan_most(int per, int64_t E) {
+    const int64_t counts = (per == 1 ? 16384 : 49152) / E;
+    return counts < 256 ? counts : 256;
+}
+inline int plan_per(int64_t n, int64_t E) {
+    const bool single = plan_runs(n, 4) == 1;
+    for (int per = 1; per < 4; per *= 2)
+        if (plan_runs(n, per) <= (single ? 1 : plan_most(per, E))) return per;
+    return 4;
+}
+
+template <int PER>
+hipError_t launch_plan(const int32_t *ids, int64_t n, int k, int E, int32_t *info, int32_t *rows, int32_t *source,
+                       void *workspace, hipStream_t stream) {
+    const int runs = (int)plan_runs(n, PER);
+    int32_t *hist = runs > 1 ? static_cast<int32_t *>(workspace) : nullptr;
+    if (hist) {
+        hipLaunchKernelGGL((plan_count_kernel<PER>), dim3((unsigned)runs), dim3(kPlanThreads), E * sizeof(int32_t), stream,
+                           ids, n, E, hist);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const size_t lds = ((size_t)(kPlanWaves + 3) * E + 1) * sizeof(int32_t);
+    hipLaunchKernelGGL((plan_place_kernel<PER>), dim3((unsigned)runs), dim3(kPlanThreads), lds, stream, ids, n, k, E, runs,
+                       hist, info, rows, source);
+    return hipGetLastError();
 }
 
 // ---- combination ------------------------------------------------------------------------------
@@ -480,24 +518,23 @@ hipError_t launch_expert_route(const void *logits, MxType type, int64_t ld, int6
 }
 
 size_t expert_plan_workspace_bytes(int64_t n, int64_t E) {
-    const int64_t runs = (n + kPlanRun - 1) / kPlanRun;
-    return runs > 1 ? (size_t)(runs * E) * sizeof(int32_t) : 0;
+    int64_t runs = plan_runs(n, 4);
+    if (runs == 1) return 0;
+    // (no smaller n needs more)
+    for (int per = 1; per < 4; per *= 2) {
+        const int64_t most = plan_most(per, E), r = plan_runs(n, per) < most ? plan_runs(n, per) : most;
+        runs = r > runs ? r : runs;
+    }
+    return (size_t)(runs * E) * sizeof(int32_t);
 }
 
 hipError_t launch_expert_plan(const int32_t *ids, int64_t n, int k, int E, int32_t *info, int32_t *rows,
                               int32_t *source, void *workspace, hipStream_t stream) {
-    const int runs = (int)((n + kPlanRun - 1) / kPlanRun);
-    int32_t *hist = runs > 1 ? static_cast<int32_t *>(workspace) : nullptr;
-    if (hist) {
-        hipLaunchKernelGGL(plan_count_kernel, dim3((unsigned)runs), dim3(kPlanThreads), E * sizeof(int32_t), stream, ids,
-                           n, E, hist);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    switch (plan_per(n, E)) {
+        case 1: return launch_plan<1>(ids, n, k, E, info, rows, source, workspace, stream);
+        case 2: return launch_plan<2>(ids, n, k, E, info, rows, source, workspace, stream);
+        default: return launch_plan<4>(ids, n, k, E, info, rows, source, workspace, stream);
     }
-    const size_t lds = ((size_t)(kPlanWaves + 3) * E + 1) * sizeof(int32_t);
-    hipLaunchKernelGGL(plan_place_kernel, dim3((unsigned)runs), dim3(kPlanThreads), lds, stream, ids, n, k, E, runs, hist,
-                       info, rows, source);
-    return hipGetLastError();
 }
 
 hipError_t launch_expert_combine(const void *Y, MxType type, int64_t ldy, const int32_t *rows, const float *weights,

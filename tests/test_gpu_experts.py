@@ -134,6 +134,23 @@ def test_plan(clq, T, k, E, kind):
     assert off[-1] == len(source) and (np.diff(off) == (counts + 31) // 32 * 32).all()
 
 
+@pytest.mark.parametrize("T,k,E", [(1025, 1, 7), (600, 3, 512), (2500, 4, 512), (20000, 8, 256), (100000, 8, 64), (70000, 2, 512)])
+def test_plan_runs_of_every_length(clq, T, k, E):
+    ids = torch.from_numpy(np.random.default_rng(T).integers(-1, E, (T, k)).astype(np.int32))
+    p = clq.clq_expert_plan(ids.cuda(), E)
+    flat = ids.flatten().long()
+    order = torch.sort(torch.where(flat < 0, E, flat), stable=True)[1]
+    order = order[:int((flat >= 0).sum())]
+    counts = torch.bincount(flat[flat >= 0], minlength=E)
+    first = torch.cumsum((counts + 31) // 32 * 32, 0) - (counts + 31) // 32 * 32
+    row = torch.full((T * k,), -1, dtype=torch.int64)
+    row[order] = torch.arange(len(order)) - (torch.cumsum(counts, 0) - counts)[flat[order]] + first[flat[order]]
+    assert torch.equal(p.counts.cpu().long(), counts) and torch.equal(p.rows.flatten().cpu().long(), row)
+    source = torch.full((int(p.offsets()[-1]),), -1, dtype=torch.int64)
+    source[row[order]] = order // k
+    assert torch.equal(p.source[:len(source)].cpu().long(), source)
+
+
 # ---- grouped products --------------------------------------------------------------------------
 
 def _layer(seed, T, K, F, E, k, act, dtype):

@@ -17,6 +17,13 @@ A, MIS = 0x10000, 0x10002   # fake device addresses, never read
 L = clq.lib()
 
 
+def test_plan_workspace_grows_with_the_assignments():
+    """One that is large enough for some number of tokens is so for fewer."""
+    for E in (1, 7, 64, 256, 512):
+        sizes = [clq.clq_expert_plan_workspace_bytes(T, 8, E) for T in range(1, 200000, 97)]
+        assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[-1] >= 4 * E * (8 * 199000 // 4096)
+
+
 def test_exports_and_binding_names():
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "clq_mx4.h")).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(clq_[a-z0-9_]+)\s*\(", text)))
