@@ -22,28 +22,60 @@ namespace clq {
 namespace {
 
 // ---- routing ---------------------------------------------------------------------------
-// One wave per token.  Lane l holds the VPL consecutive experts from l * VPL, so that
+// LPT lanes per token, 64 or 32.  Lane l holds the VPL consecutive experts from l * VPL, so that
 // among equal ranks the lowest lane's first one is the lowest index.  Ranks are compared as
 // whole numbers in the floats' order, 0 for an expert that cannot be chosen.  A lane sorts
-// its own experts once; each of the top_k rounds then is a wave maximum of the lanes' heads
-// (six lane permutes) and a pop.  What bounds it are these vector instructions, some 600 a token
-// at 256 experts: 43200 tokens to 8 of them in 4 of 8 groups take 47 us, reading the logits 9
-// (one LDS read after another by a lane a group, and shuffles instead of permutes: 89).
-constexpr int kRouteWaves = 4;
+// its own experts once, in lists of up to four; each of the top_k rounds then is a maximum over the
+// token's lanes of their heads (four to six lane permutes) and a pop.  What bounds it are these
+// vector instructions, some 450 a token at 256 experts: 43200 tokens to 8 of them in 4 of 8 groups
+// take 40 us, reading the logits 9 (one LDS read after another by a lane a group, and shuffles
+// instead of permutes: 89).
+constexpr int kRouteWaves = 4, kRouteMost = 32;   // waves of a workgroup, experts of a token
 
-template <int CTRL, int ROWS>
+template <int CTRL, int ROWS = 0xf>
 __device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false));
 }
-// largest of the wave's values, in a scalar
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-    v = dpp_max<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8
-    v = dpp_max<0x112, 0xf>(v);
-    v = dpp_max<0x114, 0xf>(v);
-    v = dpp_max<0x118, 0xf>(v);
-    v = dpp_max<0x142, 0xa>(v);   // row_bcast 15 into rows 1 and 3
-    v = dpp_max<0x143, 0xc>(v);   // row_bcast 31 into rows 2 and 3
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+// largest value of the token's LPT lanes, in all of them
+template <int LPT>
+__device__ __forceinline__ uint32_t token_max(uint32_t v) {
+    if constexpr (LPT == 64) {
+        v = dpp_max<0x111>(v);        // row_shr 1, 2, 4, 8
+        v = dpp_max<0x112>(v);
+        v = dpp_max<0x114>(v);
+        v = dpp_max<0x118>(v);
+        v = dpp_max<0x142, 0xa>(v);   // row_bcast 15 into rows 1 and 3
+        v = dpp_max<0x143, 0xc>(v);   // row_bcast 31 into rows 2 and 3
+        return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+    } else {
+        static_assert(LPT == 32);
+        v = dpp_max<0xb1>(v);         // quad_perm 1 0 3 2, 2 3 0 1
+        v = dpp_max<0x4e>(v);
+        v = dpp_max<0x141>(v);        // row_half_mirror, row_mirror
+        v = dpp_max<0x140>(v);
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);   // the other row of the pair
+        return max((uint32_t)r[0], (uint32_t)r[1]);
+    }
+}
+// the token's lanes of a wave mask, lowest bit first
+template <int LPT>
+__device__ __forceinline__ uint64_t token_mask(uint64_t m, bool upper) {
+    if constexpr (LPT == 64) return m;
+    else return upper ? (uint32_t)(m >> 32) : (uint32_t)m;
+}
+// whether this is the token's lowest lane of a wave mask
+template <int LPT>
+__device__ __forceinline__ bool first_lane(uint64_t m) {
+    if constexpr (LPT == 64) return __builtin_amdgcn_inverse_ballot_w64(m & -m);
+    const uint32_t lo = (uint32_t)m, hi = (uint32_t)(m >> 32);
+    return __builtin_amdgcn_inverse_ballot_w64((uint64_t)(hi & -hi) << 32 | (lo & -lo));
+}
+// lane i of the token's lanes (i the same in all)
+template <int LPT>
+__device__ __forceinline__ uint32_t token_lane(uint32_t v, int i, bool upper) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+    if constexpr (LPT == 64) return lo;
+    else return upper ? (uint32_t)__builtin_amdgcn_readlane((int)v, 32 + i) : lo;
 }
 // floats (no NaN) as whole numbers of the same order, all above 0; equal zeros
 __device__ __forceinline__ uint32_t order_of(float f) {
@@ -95,34 +127,43 @@ __device__ __forceinline__ void load_logits(const RouteArgs &a, int64_t t, int l
     }
 }
 
-template <int VPL>
+template <int VPL, int LPT>
 __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
 {
-    __shared__ __align__(16) float sh_score[kRouteWaves][VPL * 64];
-    __shared__ __align__(16) uint32_t sh_rank[kRouteWaves][VPL * 64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int TPW = 64 / LPT;   // tokens of a wave
+    // lists of a lane's experts, each sorted
+    constexpr int NL = VPL > 4 ? VPL / 4 : 1, LEN = VPL / NL;
+    __shared__ __align__(16) float sh_score[kRouteWaves][TPW][VPL * LPT];
+    __shared__ __align__(16) uint32_t sh_rank[kRouteWaves][TPW][VPL * LPT];
+    __shared__ int sh_id[kRouteWaves][TPW][kRouteMost];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & (LPT - 1), token = (threadIdx.x & 63) / LPT;
+    const bool upper = token != 0;
     constexpr float kNone = -INFINITY;
-    float *scores = sh_score[wave];
+    float *scores = sh_score[wave][token];
+    int *chosen = sh_id[wave][token];
     // lanes of a group: the largest power of two that gives every group as many
-    int per_group = 64;
-    while (per_group * a.groups > 64) per_group >>= 1;
+    int per_group = LPT;
+    while (per_group * a.groups > LPT) per_group >>= 1;
     const bool by_logit = a.bias == nullptr && a.groups == 1;
     float balance[VPL];
 #pragma unroll
     for (int v = 0; v < VPL; ++v) balance[v] = a.bias && lane * VPL + v < a.E ? a.bias[lane * VPL + v] : 0.0f;
-    const int64_t step = (int64_t)gridDim.x * kRouteWaves;
-    int64_t t = (int64_t)blockIdx.x * kRouteWaves + wave;
+    // (whole waves: the upper half of the last one may repeat the last token)
+    const int64_t step = (int64_t)gridDim.x * kRouteWaves * TPW;
+    int64_t t0 = ((int64_t)blockIdx.x * kRouteWaves + wave) * TPW;
     float next[VPL];
-    if (t < a.T) load_logits<VPL>(a, t, lane, next);
-    for (; t < a.T; t += step) {
+    if (t0 < a.T) load_logits<VPL>(a, min(t0 + token, a.T - 1), lane, next);
+    for (; t0 < a.T; t0 += step) {
+        const int64_t t = t0 + token;
         float x[VPL], score[VPL];
 #pragma unroll
         for (int v = 0; v < VPL; ++v) x[v] = next[v];
-        if (t + step < a.T) load_logits<VPL>(a, t + step, lane, next);
+        if (t0 + step < a.T) load_logits<VPL>(a, min(t + step, a.T - 1), lane, next);
         bool nan = false;
 #pragma unroll
         for (int v = 0; v < VPL; ++v) nan |= x[v] != x[v];
-        nan = __any(nan);   // leaves the token's weights NaN; NaN ranks come last
+        nan = token_mask<LPT>(__ballot(nan), upper) != 0;   // leaves the token's weights NaN; NaN ranks come last
         if (a.sigmoid) {
 #pragma unroll
             for (int v = 0; v < VPL; ++v) score[v] = 1.0f / (1.0f + expf(-x[v]));
@@ -130,7 +171,7 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
             uint32_t mo = 0;
 #pragma unroll
             for (int v = 0; v < VPL; ++v) mo = max(mo, x[v] == x[v] ? order_of(x[v]) : 0u);
-            const float m = float_of(max(wave_max(mo), order_of(kNone)));
+            const float m = float_of(max(token_max<LPT>(mo), order_of(kNone)));
             // (the sum in 64 bits, so that the rounded sum does not depend on the order)
             double s = 0.0;
 #pragma unroll
@@ -139,7 +180,7 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
                 s += (double)score[v];   // (0 past the last expert)
             }
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+            for (int o = LPT / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
             const float sum = m == kNone ? 1.0f : (float)s;
 #pragma unroll
             for (int v = 0; v < VPL; ++v) score[v] = score[v] / sum;
@@ -156,7 +197,7 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
 #pragma unroll
         for (int v = 0; v < VPL; ++v) scores[lane * VPL + v] = score[v];
         if (a.groups > 1) {
-            uint32_t *ranks = sh_rank[wave];
+            uint32_t *ranks = sh_rank[wave][token];
 #pragma unroll
             for (int v = 0; v < VPL; ++v) ranks[lane * VPL + v] = key[v];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -180,49 +221,62 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
             // a group is kept if fewer than top_groups groups come before it
             int before = 0;
             for (int o = 0; o < a.groups; ++o) {
-                const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)bo, o * per_group);
+                const uint32_t other = token_lane<LPT>(bo, o * per_group, upper);
                 before += other > bo || (other == bo && o < g);
             }
-            const uint64_t kept = __ballot(g < a.groups && before < a.top_groups);
+            const uint64_t kept = token_mask<LPT>(__ballot(g < a.groups && before < a.top_groups), upper);
 #pragma unroll
             for (int v = 0; v < VPL; ++v) {
                 const int e = min(lane * VPL + v, a.E - 1);
                 key[v] = (kept >> (e / gs * per_group)) & 1 ? key[v] : 0u;
             }
         }
-        // the lane's experts, best first (an equal one stays behind: its index is higher);
-        // their places, four bits each, go along
-        uint32_t place[VPL];
+        // each list best first (an equal one stays behind: its index is higher); the places of its
+        // experts, four bits each, go along
+        uint32_t order[NL];
 #pragma unroll
-        for (int v = 0; v < VPL; ++v) place[v] = (uint32_t)v;
+        for (int n = 0; n < NL; ++n) {
+            uint32_t *list = key + n * LEN, place[LEN];
 #pragma unroll
-        for (int i = 1; i < VPL; ++i)
+            for (int v = 0; v < LEN; ++v) place[v] = (uint32_t)(n * LEN + v);
 #pragma unroll
-            for (int j = i; j > 0; --j) {
-                const uint32_t d = key[j] > key[j - 1] ? place[j] ^ place[j - 1] : 0u;
-                const uint32_t hi = max(key[j], key[j - 1]), lo = min(key[j], key[j - 1]);
-                key[j - 1] = hi;
-                key[j] = lo;
-                place[j - 1] ^= d;
-                place[j] ^= d;
-            }
-        uint32_t order = 0;
+            for (int i = 1; i < LEN; ++i)
 #pragma unroll
-        for (int v = 0; v < VPL; ++v) order |= place[v] << (4 * v);
-        int my_id = 0;
+                for (int j = i; j > 0; --j) {
+                    const bool swap = list[j] > list[j - 1];
+                    const uint32_t hi = list[j - 1], lo = list[j], p = place[j - 1], q = place[j];
+                    list[j - 1] = swap ? lo : hi;
+                    list[j] = swap ? hi : lo;
+                    place[j - 1] = swap ? q : p;
+                    place[j] = swap ? p : q;
+                }
+            order[n] = 0;
+#pragma unroll
+            for (int v = 0; v < LEN; ++v) order[n] |= place[v] << (4 * v);
+        }
         for (int j = 0; j < a.k; ++j) {
-            const uint32_t top = wave_max(key[0]);
-            const int from = __ffsll((unsigned long long)__ballot(key[0] == top)) - 1;
-            const int got = from * VPL + (__builtin_amdgcn_readlane((int)order, from) & 15);
-            my_id = lane == j ? got : my_id;
-            // the winner's lane moves its experts up
-            const uint32_t pop = lane == from ? ~0u : 0u;
+            uint32_t head = key[0], at = order[0];
+            if constexpr (NL == 2) {
+                at = key[LEN] > head ? order[1] : at;
+                head = max(head, key[LEN]);
+            }
+            const uint32_t top = token_max<LPT>(head);
+            const bool won = first_lane<LPT>(__ballot(head == top));
+            if (won) chosen[j] = lane * VPL + (int)(at & 15);
+            // the winner's list moves up (of two equal heads the first one's)
+            const uint32_t in_first = key[0] == top ? ~0u : 0u, mask = won ? ~0u : 0u;
 #pragma unroll
-            for (int v = 0; v + 1 < VPL; ++v) key[v] = (key[v + 1] & pop) | (key[v] & ~pop);
-            key[VPL - 1] &= ~pop;
-            order = ((order >> 4) & pop) | (order & ~pop);
+            for (int n = 0; n < NL; ++n) {
+                uint32_t *list = key + n * LEN;
+                const uint32_t pop = NL == 1 ? mask : n == 0 ? mask & in_first : mask & ~in_first;
+#pragma unroll
+                for (int v = 0; v + 1 < LEN; ++v) list[v] = (list[v + 1] & pop) | (list[v] & ~pop);
+                list[LEN - 1] &= ~pop;
+                order[n] = ((order[n] >> 4) & pop) | (order[n] & ~pop);
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int my_id = lane < a.k ? chosen[lane] : 0;
         float w = lane < a.k ? scores[my_id] : 0.0f;
         if (a.renormalize) {
             float total = w;
@@ -232,12 +286,29 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a)
         }
         w *= a.scale;
         if (nan) w = __uint_as_float(0x7fc00000u);
-        if (lane < a.k) {
+        if (lane < a.k && t < a.T) {
             a.ids[t * a.k + lane] = my_id;
             a.weights[t * a.k + lane] = w;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+}
+
+// Two tokens share a wave where there are enough to fill the chip all the same: the rounds cost
+// both of them what they cost one.  us of one / two tokens a wave: 64 experts, 6 of them, 1 token
+// 2.9 / 3.2, 4096 4.4 / 4.1, 43200 19.2 / 14.8; 128 experts, 8, 4096 tokens 5.2 / 4.9, 8192 7.4 / 6.6;
+// 256 experts, 8, in 4 of 8 groups, 4096 tokens 7.4 / 8.4, 20000 22.6 / 24.6, 24576 27.0 / 25.6, 43200
+// 44.4 / 39.8, 100000 91 / 78.
+inline bool route_shared(int64_t T, int E, int groups) {
+    return groups <= 32 && E <= 256 && T >= (E <= 128 ? 4096 : 24576);
+}
+
+template <int VPL, int LPT>
+void launch_route(const RouteArgs &a, hipStream_t stream) {
+    // as many waves as the chip holds, each with every so-many-th token
+    const int64_t tokens = kRouteWaves * (64 / LPT), want = (a.T + tokens - 1) / tokens, most = (int64_t)compute_units() * 8;
+    hipLaunchKernelGGL((route_kernel<VPL, LPT>), dim3((unsigned)(want < most ? want : most)), dim3(64 * kRouteWaves), 0,
+                       stream, a);
 }
 
 // ---- plan ---------------------------------------------------------------------------------
@@ -507,13 +578,16 @@ hipError_t launch_expert_route(const void *logits, MxType type, int64_t ld, int6
                                const float *bias, int groups, int top_groups, bool renormalize, float scale,
                                int32_t *ids, float *weights, hipStream_t stream) {
     const RouteArgs a = {logits, type, ld, T, E, k, groups, top_groups, sigmoid, renormalize, bias, scale, ids, weights};
-    // as many waves as the chip holds, each with every so-many-th token
-    const int64_t want = (T + kRouteWaves - 1) / kRouteWaves, most = (int64_t)compute_units() * 8;
-    const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kRouteWaves);
-    if (E <= 64) hipLaunchKernelGGL((route_kernel<1>), grid, block, 0, stream, a);
-    else if (E <= 128) hipLaunchKernelGGL((route_kernel<2>), grid, block, 0, stream, a);
-    else if (E <= 256) hipLaunchKernelGGL((route_kernel<4>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((route_kernel<8>), grid, block, 0, stream, a);   // (512 at most)
+    if (route_shared(T, E, groups)) {
+        if (E <= 64) launch_route<2, 32>(a, stream);
+        else if (E <= 128) launch_route<4, 32>(a, stream);
+        else launch_route<8, 32>(a, stream);
+    } else {
+        if (E <= 64) launch_route<1, 64>(a, stream);
+        else if (E <= 128) launch_route<2, 64>(a, stream);
+        else if (E <= 256) launch_route<4, 64>(a, stream);
+        else launch_route<8, 64>(a, stream);   // (512 at most)
+    }
     return hipGetLastError();
 }
 

@@ -98,6 +98,28 @@ def test_route_strided_logits(clq):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("T,E,k,groups,top,biased", [
+    (4097, 1, 1, 1, 1, False), (4099, 33, 5, 1, 1, False), (5000, 64, 6, 1, 1, True), (4103, 100, 32, 1, 1, True),
+    (4096, 128, 8, 32, 9, True), (24577, 256, 8, 8, 4, True), (24579, 130, 3, 1, 1, False), (30001, 192, 8, 32, 3, False)])
+def test_route_of_many_tokens_is_that_of_few(clq, T, E, k, groups, top, biased, score):
+    """With equal ranks, masked experts, masked rows and NaN among the tokens."""
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn(T, E, generator=g)
+    x[::5] = x[::5].round()
+    x[::7, : E // 2] = -float("inf")
+    x[3::1001] = -float("inf")
+    x[5::997, E // 3] = float("nan")
+    x[6::991, E // 4] = float("inf")
+    x = x.cuda()
+    b = torch.randn(E, generator=g).cuda() if biased else None
+    f = lambda x: clq.clq_expert_route(x, k, score=score, bias=b, groups=groups, top_groups=top)  # noqa: E731
+    ids, w = f(x)
+    parts = [f(x[i:i + 3000]) for i in range(0, T, 3000)]
+    assert torch.equal(ids, torch.cat([p[0] for p in parts]))
+    assert torch.equal(w.view(torch.int32), torch.cat([p[1] for p in parts]).view(torch.int32))
+
+
 def test_route_refuses_rows_that_overlap(clq):
     x = torch.randn(4, 64, device="cuda")
     for bad in (x[:1].expand(50, 64), x[:, :1].as_strided((50, 1), (0, 1)), x.as_strided((50, 64), (3, 1))):
