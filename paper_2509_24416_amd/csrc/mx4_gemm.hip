@@ -142,8 +142,8 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 // reads of stage s are in, then the workgroup barrier: every wave holds stage s in
 // registers, so its slot is refilled with stage s + NS.  Quad q's scale slot is likewise
 // free after the barrier of the quad's first iteration and refilled there with quad q + 2,
-// needed at the end of quad q + 1.  Transfers past the end repeat the last stage or quad,
-// so the wait counts stay constant.
+// needed at the end of quad q + 1.  Within the loop transfers past the end repeat the last
+// stage or quad, so that its wait counts are constant; the stages after it have their own.
 //
 // What bounds it: the matrix instructions (8 per wave and stage of 32 cycles) and the vector
 // instructions of the epilogue, which do not overlap on a SIMD, and on large products the power
@@ -158,6 +158,20 @@ constexpr int kDepth = 4;                       // stages of token units in regi
 // Ring of channel units: one more than kDepth, so that the stages that the prologue leaves in
 // flight are as many transfers and loads as the loop's wait counts take them for.
 constexpr int kStages = kDepth + 1;
+
+// What a stage at position p of eight fetches (negative: of the eight before, or of the
+// prologue): channel units for NS stages on, token units for kDepth stages on, at the start of
+// a quad the token scales of the next and the channel scales of the one after it.  The stages
+// after the loop (`last`, positions 0 .. 6) are followed by no others.
+constexpr bool fetches_w(int p, bool last) { return !last || p + kStages < 7; }
+constexpr bool fetches_x(int p, bool last) { return !last || p + kDepth < 7; }
+constexpr bool fetches_xs(int p, bool last) { return p % 4 == 0 && (!last || p == 0); }
+constexpr bool fetches_ws(int p, bool last) { return p % 4 == 0 && !last; }
+// its transfers and loads, per_wave transfers of each kind a wave
+constexpr int fetched(int p, bool last, int per_wave) {
+    if (p < 0) last = false;
+    return per_wave * (fetches_w(p, last) + fetches_ws(p, last)) + 2 * (fetches_x(p, last) + fetches_xs(p, last));
+}
 
 template <int FN>
 struct Operands {
@@ -496,36 +510,39 @@ __global__ void __launch_bounds__(NW * 64, 2) mx_tile_kernel(Args a)
     read_scales(IC<0>{});
     uint32_t cur = 0;
     int k = 0, q = 1;
-    // position P8 of the eight stages of an even and an odd quad
-    auto stage = [&](auto pc) __attribute__((always_inline)) {
+    // Position P8 of the eight stages of an even and an odd quad.  LAST: one of the stages after
+    // the loop, at most seven, which start on a quad; they fetch only what such a stage can still
+    // use, so that no load among those that the waits count is one without a use (the compiler
+    // drops it).
+    auto stage = [&](auto pc, auto lc) __attribute__((always_inline)) {
+        constexpr bool LAST = decltype(lc)::value;
         constexpr int P8 = decltype(pc)::value, P = P8 & 3, Q = P8 >> 2, R = P & 1;
-        // Outstanding: the last NS - 2 stages' transfers and two loads, and as many of the
-        // scales if a quad began among them.
-        constexpr int VM = (NS - 2) * (PPW + 2) + (P >= 1 && P <= NS - 2 ? PPW + 2 : 0);
+        // Outstanding: what the three stages before this one fetch, whatever the order within
+        // each; the next stage's transfers are those of the stage before them.
+        constexpr int VM = fetched(P8 - 1, LAST, PPW) + fetched(P8 - 2, LAST, PPW) + fetched(P8 - 3, LAST, PPW);
+        static_assert(NS == 5, "three stages between a transfer and the wait for it");
         if constexpr (P == 0) wait_stage<VM>(op[R], sc[Q]);
         else wait_stage<VM>(op[R]);
         const uint32_t nxt = cur == (uint32_t)((NS - 1) * kStageBytes) ? 0u : cur + kStageBytes;
         op[1 - R].read(wl + nxt);
         if constexpr (P == 3) read_scales(IC<1 - Q>{});
-        produce(cur, k + NS);
-        if constexpr (P == 0) {
-            load_xs(IC<1 - Q>{}, q);
-            produce_scales(Q * kQuadBytes, ++q);
-        }
+        if constexpr (fetches_w(P8, LAST)) produce(cur, k + NS);
+        if constexpr (fetches_xs(P8, LAST)) load_xs(IC<1 - Q>{}, q);
+        if constexpr (fetches_ws(P8, LAST)) produce_scales(Q * kQuadBytes, ++q);
         static_for<0, FN>([&](auto fc) {
             static_for<0, 2>([&](auto mc) {
                 constexpr int fn = decltype(fc)::value, fm = decltype(mc)::value;
                 acc[fn][fm] = mfma_mx4<P>(op[R].w[fn], x[P][fm], acc[fn][fm], sc[Q].s[fn], xs[Q][fm]);
             });
         });
-        load_x(IC<P>{}, k + kDepth);
+        if constexpr (fetches_x(P8, LAST)) load_x(IC<P>{}, k + kDepth);
         cur = nxt;
         ++k;
     };
-    for (int pairs = nks >> 3; pairs > 0; --pairs) static_for<0, 8>([&](auto p) { stage(p); });
+    for (int pairs = nks >> 3; pairs > 0; --pairs) static_for<0, 8>([&](auto p) { stage(p, std::false_type{}); });
     const int rest = nks & 7;
     static_for<0, 7>([&](auto p) {
-        if (rest > decltype(p)::value) stage(p);
+        if (rest > decltype(p)::value) stage(p, std::true_type{});
     });
     // drain: the last transfers, and the last reads, whose data is not used (all register
     // sets are named, so that no register of theirs serves another value meanwhile)
