@@ -21,15 +21,17 @@ class ExpertMLP:
     """router: [experts, hidden]; w1: [experts, mlp, hidden] (swiglu: 2 * mlp rows, the gates
     first), b1: [experts, rows of w1]; w2: [experts, hidden, mlp], b2: [experts, hidden]; fp16 or
     bf16 device tensors, biases of the inputs' type or None.  block: Hadamard block size of both
-    layers (swiglu: 64 at most).  route: further arguments of clq_expert_route."""
+    layers (swiglu: 64 at most).  results: type of the experts' results ahead of their sum (fp32:
+    the layer rounds once; fp16 and bf16 are quicker on many tokens).  route: further arguments of
+    clq_expert_route."""
 
-    def __init__(self, router, w1, b1, w2, b2, top_k, act="gelu", block=64, **route):
+    def __init__(self, router, w1, b1, w2, b2, top_k, act="gelu", block=64, results=torch.float32, **route):
         self.router = router.float()
         self.experts, self.top_k, self.act, self.block, self.route = router.shape[0], top_k, act, block, route
         # weights are rotated and quantized once
         self.w1 = clq_mx4_quantize_weights(w1, block, gated=act == "swiglu")
         self.w2 = clq_mx4_quantize_weights(w2, block)
-        self.b1, self.b2 = b1, b2
+        self.b1, self.b2, self.results = b1, b2, results
         self.graph = None
 
     def forward(self, x):
@@ -38,7 +40,7 @@ class ExpertMLP:
         plan = clq_expert_plan(ids, self.experts)
         q = clq_mx4_dispatch(x, plan, self.block)
         h = clq_mx4_experts_mx4(q, plan, self.w1, self.b1, act=self.act, block=self.block)
-        y = clq_mx4_experts(h, plan, self.w2, self.b2)
+        y = clq_mx4_experts(h, plan, self.w2, self.b2, dtype=self.results)
         return clq_expert_combine(y, plan, weights, dtype=x.dtype)
 
     def capture(self, tokens, dtype=torch.float16):

@@ -512,18 +512,10 @@ def _plan_operands(q, plan, qw, bias):
     return r
 
 
-# Results that are summed afterwards keep fp32 while they are this small: a rounding to 16 bits
-# and the one of the sum make 1.4 times the error of one.  Past it the bytes count, and the default
-# is the tokens' type (whole layers, us, 16 bits / fp32: 512 tokens to 2 of 16 experts of width
-# 1152, 7 MB of fp32, 49 / 50; 4096, 38 MB, 103 / 114; 43200, 382 MB, 704 / 823; 4096 to 6 of 64,
-# 117 MB, 102 / 137).
-_FP32_RESULTS = 8 << 20
-
-
 def clq_mx4_experts(q, plan, qw, bias=None, dtype=None, out=None, stream=None):
     """Each row of the plan times its expert's weights: Y [plan.plan_rows, N] of fp16, bf16 or fp32;
-    rows past the last expert's are left as they were.  dtype: by default that of `out`, or fp32
-    for results of up to 8 MB and the tokens' type for larger ones."""
+    rows past the last expert's are left as they were.  dtype: by default that of `out`, or fp32,
+    so that a sum of results is rounded once."""
     device, b, bt = _plan_operands(q, plan, qw, bias)
     if qw.gated:
         raise ValueError("gated weights go with clq_mx4_experts_mx4(act='swiglu')")
@@ -532,9 +524,11 @@ def clq_mx4_experts(q, plan, qw, bias=None, dtype=None, out=None, stream=None):
         with _elsewhere(device, stream):
             return clq_mx4_experts(q, plan, qw, bias, dtype, out)
     M, K, N = q.rows, q.K, qw.N
+    # (16-bit results make 1.4 times the error of one rounding in the sum, and halve the bytes; whole
+    # layers, us, 16 bits / fp32: 512 tokens to 2 of 16 experts of width 1152 49 / 50, 4096 103 / 114,
+    # 43200 704 / 823; 4096 to 6 of 64 102 / 137)
     if dtype is None:
-        dtype = (out.dtype if out is not None else torch.float32 if 4 * M * N <= _FP32_RESULTS else
-                 plan.dtype or (torch.float16 if bias is None else bias.dtype))
+        dtype = torch.float32 if out is None else out.dtype
     Y, ld = _output(out, M, N, dtype, device)
     p = q.data.data_ptr()
     _check(_lib.clq_mx4_experts(p, p + _code_bytes(M, K), plan.data.data_ptr(), plan.tokens, plan.top_k, plan.experts,
