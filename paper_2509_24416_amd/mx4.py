@@ -103,13 +103,17 @@ class MX4Weight:
 
 class ExpertPlan:
     """Assignments sorted by expert: `tokens` x `top_k` of them to `experts` experts, in buffers
-    of `plan_rows` rows.  One int32 buffer holds the tables, the rows and the sources; `dtype` is
-    the type of the tokens last dispatched."""
-    __slots__ = ("data", "tokens", "top_k", "experts", "plan_rows", "at_rows", "at_source", "dtype")
+    of `plan_rows` rows.  One int32 buffer holds the tables, the rows and the sources."""
+    __slots__ = ("data", "tokens", "top_k", "experts", "plan_rows", "at_rows", "at_source", "dispatched")
 
     def __init__(self, data, tokens, top_k, experts, plan_rows, ints):
         self.data, self.tokens, self.top_k, self.experts, self.plan_rows = data, tokens, top_k, experts, plan_rows
-        self.at_rows, self.at_source, self.dtype = ints, ints + tokens * top_k, None
+        self.at_rows, self.at_source, self.dispatched = ints, ints + tokens * top_k, set()
+
+    @property
+    def dtype(self):
+        """The type of the tokens dispatched with this plan; None before, and where there were two."""
+        return next(iter(self.dispatched)) if len(self.dispatched) == 1 else None
 
     @property
     def counts(self):
@@ -500,7 +504,7 @@ def clq_mx4_dispatch(X, plan, block=0, perm=None, out=None, stream=None):
     t = plan.data.data_ptr()
     _check(_lib.clq_mx4_dispatch(X.data_ptr(), _TYPES[X.dtype], ldx, g, T, plan.top_k, plan.experts, K, block, t,
                                  t + 4 * plan.at_source, codes, scales, _raw_stream(i)), "clq_mx4_dispatch")
-    plan.dtype = X.dtype
+    plan.dispatched.add(X.dtype)
     return _holds(q, n, K, block)
 
 
@@ -557,7 +561,8 @@ def clq_mx4_experts_mx4(q, plan, qw, bias=None, act=None, block=0, out=None, str
 
 def clq_expert_combine(Y, plan, weights, dtype=None, out=None, stream=None):
     """out[t] = sum over the slots of weights[t, j] * Y[plan.rows[t, j]], in fp32.  dtype: by default
-    that of `out`, or of the tokens that the plan dispatched (none: Y's)."""
+    that of `out`, or of the tokens dispatched with the plan (none: Y's; to be named if there were
+    tokens of two types)."""
     r, N, ldy = _rows2d(Y, "Y", _TYPES)
     _dev(weights, "weights", (torch.float32,))
     T, k = plan.tokens, plan.top_k
@@ -570,6 +575,8 @@ def clq_expert_combine(Y, plan, weights, dtype=None, out=None, stream=None):
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
             return clq_expert_combine(Y, plan, weights, dtype, out)
+    if dtype is None and out is None and len(plan.dispatched) > 1:
+        raise ValueError("tokens of two types were dispatched with the plan: name the result's dtype")
     if dtype is None:
         dtype = out.dtype if out is not None else plan.dtype or Y.dtype
     o, ld = _output(out, T, N, dtype, device)

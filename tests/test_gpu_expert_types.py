@@ -59,3 +59,30 @@ def test_layer_keeps_fp32_results_unless_asked(clq):
     for m, t in ((layer, F32), (half, F16)):
         y = clq.clq_mx4_experts(h, plan, layer.w2, b2, dtype=t)
         assert torch.equal(m.forward(x), clq.clq_expert_combine(y, plan, gates, dtype=F16))
+
+
+def test_tokens_of_two_types_with_one_plan(clq):
+    """Neither chain takes the other's type, in whatever order their calls come."""
+    T, k, E, K, N = 40, 2, 4, 128, 64
+    ids, gates = torch.randint(0, E, (T, k), dtype=torch.int32).cuda(), _gates(T, k)
+    w = clq.clq_mx4_quantize_weights(torch.randn(E, N, K).half().cuda())
+    xs = {t: torch.randn(T, K).to(t).cuda() for t in (F16, BF16)}
+    want = {}
+    for t, x in xs.items():   # each with a plan of its own
+        p = clq.clq_expert_plan(ids, E)
+        want[t] = clq.clq_expert_combine(clq.clq_mx4_experts(clq.clq_mx4_dispatch(x, p), p, w), p, gates)
+        assert want[t].dtype == p.dtype == t
+    plan = clq.clq_expert_plan(ids, E)
+    y = {F16: clq.clq_mx4_experts(clq.clq_mx4_dispatch(xs[F16], plan), plan, w)}
+    y[BF16] = clq.clq_mx4_experts(clq.clq_mx4_dispatch(xs[BF16], plan), plan, w)
+    for t in (F16, BF16):
+        with pytest.raises(ValueError, match="two types"):
+            clq.clq_expert_combine(y[t], plan, gates)
+        assert torch.equal(clq.clq_expert_combine(y[t], plan, gates, dtype=t), want[t])
+        out = torch.empty(T, N, dtype=t, device="cuda")
+        assert torch.equal(clq.clq_expert_combine(y[t], plan, gates, out=out), want[t])
+    # a plan that is used again with the same type keeps it
+    again = clq.clq_expert_plan(ids, E)
+    for _ in range(2):
+        q = clq.clq_mx4_dispatch(xs[BF16], again)
+    assert torch.equal(clq.clq_expert_combine(clq.clq_mx4_experts(q, again, w), again, gates), want[BF16])
