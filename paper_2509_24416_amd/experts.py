@@ -55,6 +55,10 @@ class ExpertMLP:
         return self.graph
 
     def replay(self, x):
+        """x: as many tokens as were captured, of the same type.  The result is overwritten by the
+        next replay."""
+        if x.shape != self.x_in.shape or x.dtype != self.x_in.dtype:
+            raise ValueError(f"x is {x.dtype} {tuple(x.shape)}, captured was {self.x_in.dtype} {tuple(self.x_in.shape)}")
         self.x_in.copy_(x)
         self.graph.replay()
         return self.x_out
