@@ -46,13 +46,15 @@ class ExpertMLP:
     def capture(self, tokens, dtype=torch.float16):
         """Captures forward for `tokens` tokens as one graph."""
         dev = self.router.device
-        self.x_in = torch.zeros(tokens, self.router.shape[1], dtype=dtype, device=dev)
-        self.forward(self.x_in)   # every kernel loaded first
+        x = torch.zeros(tokens, self.router.shape[1], dtype=dtype, device=dev)
+        self.forward(x)   # every kernel loaded first
         torch.cuda.synchronize(dev)
-        self.graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(self.graph):
-            self.x_out = self.forward(self.x_in)
-        return self.graph
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = self.forward(x)
+        # (together, and only now: a capture that fails leaves the one before as it was)
+        self.x_in, self.x_out, self.graph = x, y, graph
+        return graph
 
     def replay(self, x):
         """x: as many tokens as were captured, of the same type.  The result is overwritten by the

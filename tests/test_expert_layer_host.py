@@ -31,3 +31,39 @@ def test_replay_takes_the_captured_shape_and_type_only():
         with pytest.raises(ValueError, match="captured"):
             m.replay(bad)
     assert m.graph.replays == 1 and torch.equal(m.x_in, x)
+
+
+class _Recorder:
+    """torch.cuda's device and graph contexts, in the order they are entered."""
+
+    def __init__(self, monkeypatch):
+        self.entered = []
+        monkeypatch.setattr(torch.cuda, "device", lambda d: self._context(("device", d)))
+        monkeypatch.setattr(torch.cuda, "graph", lambda g: self._context(("graph",)))
+        monkeypatch.setattr(torch.cuda, "synchronize", lambda d=None: None)
+        monkeypatch.setattr(torch.cuda, "CUDAGraph", _Graph)
+
+    def _context(self, what):
+        import contextlib
+
+        @contextlib.contextmanager
+        def run():
+            self.entered.append(what)
+            yield
+        return run()
+
+
+def test_a_capture_that_fails_leaves_the_one_before(monkeypatch):
+    m = _layer(5)
+    x_in, x_out, graph = m.x_in, m.x_out, m.graph
+    _Recorder(monkeypatch)
+
+    def fail(x):
+        raise RuntimeError("no")
+
+    m.forward = fail
+    with pytest.raises(RuntimeError):
+        m.capture(9)
+    assert m.x_in is x_in and m.x_out is x_out and m.graph is graph
+    m.replay(torch.ones(5, 64, dtype=torch.float16))
+    assert graph.replays == 1
