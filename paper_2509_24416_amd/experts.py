@@ -50,7 +50,7 @@ class ExpertMLP:
         self.forward(x)   # every kernel loaded first
         torch.cuda.synchronize(dev)
         graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
+        with torch.cuda.device(dev), torch.cuda.graph(graph):   # (it captures the current device's stream)
             y = self.forward(x)
         # (together, and only now: a capture that fails leaves the one before as it was)
         self.x_in, self.x_out, self.graph = x, y, graph

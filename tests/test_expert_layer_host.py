@@ -67,3 +67,10 @@ def test_a_capture_that_fails_leaves_the_one_before(monkeypatch):
     assert m.x_in is x_in and m.x_out is x_out and m.graph is graph
     m.replay(torch.ones(5, 64, dtype=torch.float16))
     assert graph.replays == 1
+
+
+def test_capture_is_on_the_layers_device(monkeypatch):
+    m, r = _layer(), _Recorder(monkeypatch)
+    m.forward = lambda x: x + 1
+    m.capture(3)
+    assert r.entered == [("device", m.router.device), ("graph",)]
