@@ -50,7 +50,9 @@ class ExpertMLP:
         self.forward(x)   # every kernel loaded first
         torch.cuda.synchronize(dev)
         graph = torch.cuda.CUDAGraph()
-        with torch.cuda.device(dev), torch.cuda.graph(graph):   # (it captures the current device's stream)
+        # (on a stream of this device: by itself it takes one of the device that is current, or was when
+        # it was first used)
+        with torch.cuda.device(dev), torch.cuda.graph(graph, stream=torch.cuda.Stream(dev)):
             y = self.forward(x)
         # (together, and only now: a capture that fails leaves the one before as it was)
         self.x_in, self.x_out, self.graph = x, y, graph

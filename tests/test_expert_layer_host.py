@@ -39,7 +39,8 @@ class _Recorder:
     def __init__(self, monkeypatch):
         self.entered = []
         monkeypatch.setattr(torch.cuda, "device", lambda d: self._context(("device", d)))
-        monkeypatch.setattr(torch.cuda, "graph", lambda g: self._context(("graph",)))
+        monkeypatch.setattr(torch.cuda, "graph", lambda g, stream=None: self._context(("graph", stream)))
+        monkeypatch.setattr(torch.cuda, "Stream", lambda device: ("stream", device))
         monkeypatch.setattr(torch.cuda, "synchronize", lambda d=None: None)
         monkeypatch.setattr(torch.cuda, "CUDAGraph", _Graph)
 
@@ -73,4 +74,5 @@ def test_capture_is_on_the_layers_device(monkeypatch):
     m, r = _layer(), _Recorder(monkeypatch)
     m.forward = lambda x: x + 1
     m.capture(3)
-    assert r.entered == [("device", m.router.device), ("graph",)]
+    # (a stream of its own: the graph context's may be another device's)
+    assert r.entered == [("device", m.router.device), ("graph", ("stream", m.router.device))]
