@@ -547,8 +547,8 @@ __global__ void __launch_bounds__(256) combine_kernel(CombineArgs a)
 
 template <class TI, class TO, int W>
 hipError_t launch_combine(CombineArgs a, int64_t tokens, hipStream_t stream) {
-    // (a launch's threads stay under 2^31)
-    const int64_t most = ((int64_t)1 << 30) / a.per;
+    // (a launch's threads stay within 2^30, or are one token's, fewer than 2^31)
+    const int64_t fit = ((int64_t)1 << 30) / a.per, most = fit > 0 ? fit : 1;
     for (a.first = 0; a.first < tokens; a.first += a.tokens) {
         a.tokens = (int)(tokens - a.first < most ? tokens - a.first : most);
         const dim3 grid((unsigned)(((int64_t)a.tokens * a.per + 255) / 256));
