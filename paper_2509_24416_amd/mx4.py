@@ -228,6 +228,39 @@ def _holds(out, rows, K, block):
     return out
 
 
+# What a call reads and writes, as (address, pieces, bytes between them, bytes of each).
+def _meet(a, b):
+    """Whether two of those overlap (two sets of pieces at different distances: not looked at)."""
+    (at, n, pitch, width), (at2, n2, pitch2, width2) = ((x[0], 1, 1, x[1] * x[3]) if x[1] == 1 or x[2] == x[3] else x
+                                                     for x in (a, b))
+    pitch, pitch2 = (pitch2 if n == 1 else pitch), (pitch if n2 == 1 else pitch2)
+    if pitch != pitch2:
+        return False
+    # the first piece i of a, counted from piece 0 of b, that ends behind b's start
+    i = max((at2 - at - width) // max(pitch, 1) + 1, 1 - n2)
+    return i < n and i * pitch < at2 - at + width2
+
+
+def _mx4_bytes(data, rows, K):
+    n = _code_bytes(rows, K) + _scale_bytes(rows, K)
+    return data.data_ptr(), 1, n, n
+
+
+def _row_bytes(t, rows, columns, ld):
+    size = t.element_size()
+    return t.data_ptr(), rows, ld * size, columns * size
+
+
+def _weight_bytes(qw):
+    return tuple((t.data_ptr(), 1, t.numel(), t.numel()) for t in (qw.codes, qw.scales))
+
+
+def _apart(out, *inputs):
+    """An output of the caller's must not lie in what the launch reads."""
+    if any(_meet(out, x) for x in inputs):
+        raise ValueError("the output overlaps an input")
+
+
 def clq_mx4_quantize(X, block=0, perm=None, out=None, stream=None):
     """Rotates each row by blocks of `block` (0: none), after gathering its columns by
     `perm`, and quantizes it to MX4.  X: fp16 or bf16 [M, K], any row stride that is a
@@ -238,6 +271,8 @@ def clq_mx4_quantize(X, block=0, perm=None, out=None, stream=None):
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
             return clq_mx4_quantize(X, block, perm, out)
+    if out is not None:
+        _apart(_mx4_bytes(out.data, M, K), _row_bytes(X, M, K, ldx))
     q, codes, scales = _buffer(out, M, K, block, device, "clq_mx4_quantize")
     _check(_lib.clq_mx4_quantize(X.data_ptr(), _TYPES[X.dtype], ldx, None if perm is None else _gather(perm, K, device),
                                  M, K, block, codes, scales, _raw_stream(i)), "clq_mx4_quantize")
@@ -323,6 +358,7 @@ def clq_mx4_dequantize(q, dtype=torch.float16, out=None, stream=None):
         if _dev(out, "out", (dtype,)).shape != shape or not out.is_contiguous():
             raise ValueError(f"out must be a contiguous {shape} tensor")
         _together(device, "out", out)
+        _apart(_row_bytes(out, out.numel() // K, K, K), *(_weight_bytes(q) if w else (_mx4_bytes(q.data, rows, K),)))
     _check(_lib.clq_mx4_dequantize(c, s, w, gated, mats, rows, K, _TYPES[dtype], out.data_ptr(), K, _raw_stream(i)),
            "clq_mx4_dequantize")
     return out
@@ -347,11 +383,6 @@ def _product(q, qw, bias, experts):
         raise ValueError("bias must be a contiguous [N] or [experts, N] tensor")
     _together(device, "bias", bias)
     return device, bias.data_ptr(), _TYPES[bias.dtype]
-
-
-def _distinct(q, out):
-    if out is not None and out.data.data_ptr() == q.data.data_ptr():
-        raise ValueError("the output's buffer is the input's")
 
 
 def _output(out, rows, N, dtype, device):
@@ -391,6 +422,8 @@ def clq_mx4_linear(q, qw, bias=None, dtype=torch.float16, out=None, stream=None)
             return clq_mx4_linear(q, qw, bias, dtype, out)
     M, K, N = q.rows, q.K, qw.N
     Y, ld = _output(out, M, N, dtype, device)
+    if out is not None:
+        _apart(_row_bytes(Y, M, N, ld), _mx4_bytes(q.data, M, K), *_weight_bytes(qw))
     p = q.data.data_ptr()
     _check(_lib.clq_mx4_linear(p, p + _code_bytes(M, K), qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, M, N, K,
                                _TYPES[dtype], Y.data_ptr(), ld, _raw_stream(i)), "clq_mx4_linear")
@@ -403,7 +436,8 @@ def clq_mx4_linear_mx4(q, qw, bias=None, act=None, block=0, out=None, stream=Non
     (gated weights, N / 2 columns)."""
     a = _act(act)
     device, b, bt = _product(q, qw, bias, None)
-    _distinct(q, out)
+    if out is not None:
+        _apart(_mx4_bytes(out.data, q.rows, _columns(qw, a)), _mx4_bytes(q.data, q.rows, q.K), *_weight_bytes(qw))
     i = device.index
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
@@ -500,6 +534,8 @@ def clq_mx4_dispatch(X, plan, block=0, perm=None, out=None, stream=None):
             return clq_mx4_dispatch(X, plan, block, perm, out)
     g = None if perm is None else _gather(perm, K, device)
     n = plan.plan_rows
+    if out is not None:
+        _apart(_mx4_bytes(out.data, n, K), _row_bytes(X, T, K, ldx))
     q, codes, scales = _buffer(out, n, K, block, device, "clq_mx4_dispatch")
     t = plan.data.data_ptr()
     _check(_lib.clq_mx4_dispatch(X.data_ptr(), _TYPES[X.dtype], ldx, g, T, plan.top_k, plan.experts, K, block, t,
@@ -534,6 +570,8 @@ def clq_mx4_experts(q, plan, qw, bias=None, dtype=None, out=None, stream=None):
     if dtype is None:
         dtype = torch.float32 if out is None else out.dtype
     Y, ld = _output(out, M, N, dtype, device)
+    if out is not None:
+        _apart(_row_bytes(Y, M, N, ld), _mx4_bytes(q.data, M, K), *_weight_bytes(qw))
     p = q.data.data_ptr()
     _check(_lib.clq_mx4_experts(p, p + _code_bytes(M, K), plan.data.data_ptr(), plan.tokens, plan.top_k, plan.experts,
                                 qw.codes.data_ptr(), qw.scales.data_ptr(), b, bt, N, K, _TYPES[dtype], Y.data_ptr(),
@@ -545,7 +583,8 @@ def clq_mx4_experts_mx4(q, plan, qw, bias=None, act=None, block=0, out=None, str
     """clq_mx4_linear_mx4 with each row times its expert's weights."""
     a = _act(act)
     device, b, bt = _plan_operands(q, plan, qw, bias)
-    _distinct(q, out)
+    if out is not None:
+        _apart(_mx4_bytes(out.data, q.rows, _columns(qw, a)), _mx4_bytes(q.data, q.rows, q.K), *_weight_bytes(qw))
     i = device.index
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
@@ -580,6 +619,8 @@ def clq_expert_combine(Y, plan, weights, dtype=None, out=None, stream=None):
     if dtype is None:
         dtype = out.dtype if out is not None else plan.dtype or Y.dtype
     o, ld = _output(out, T, N, dtype, device)
+    if out is not None:
+        _apart(_row_bytes(o, T, N, ld), _row_bytes(Y, plan.plan_rows, N, ldy))
     _check(_lib.clq_expert_combine(Y.data_ptr(), _TYPES[Y.dtype], ldy, plan.data.data_ptr() + 4 * plan.at_rows,
                                    weights.data_ptr(), T, k, plan.experts, N, o.data_ptr(), _TYPES[dtype], ld,
                                    _raw_stream(i)), "clq_expert_combine")
