@@ -177,7 +177,10 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 
 
 def _elsewhere(device, stream):
-    return torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return torch.cuda.device(device)
+    _together(device, "stream", stream)
+    return torch.cuda.stream(stream)
 
 
 def _bytes(t, n, name):
