@@ -392,14 +392,15 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
         if (!hist) all[e] = sum;
     }
     __syncthreads();
-    // per expert: first row units and, for the products, first tiles of 2, 4 and 8 units
+    // per expert: first row units and, for the products, first tiles of 4 and 8 units
     if (wave < kPlanTables) {
-        int32_t *table = info + plan_table_offset(E, wave);
+        const int log_units = plan_log_units(wave);
+        int32_t *table = info + plan_table_offset(E, log_units);
         int run = 0;
         for (int e0 = 0; e0 < E; e0 += 64) {
             const int e = e0 + lane;
             const int units = e < E ? (all[e] + 31) >> 5 : 0;
-            const int v = (units + (1 << wave) - 1) >> wave;
+            const int v = (units + (1 << log_units) - 1) >> log_units;
             int s = v;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {

@@ -46,12 +46,16 @@ enum class MxType { F16 = 0, BF16 = 1, F32 = 2 };
 enum class MxAct { None = 0, Gelu = 1, Swiglu = 2 };
 
 // Where the rows of an expert plan lie (experts.hip): per-expert tables of int32.
-// counts [E], then for tiles of 1, 2, 4 and 8 row units the number of tiles before
-// each expert, E + 1 entries (the last one the total).  The first of the four is the
-// experts' first row units.
-constexpr int kPlanTables = 4;
+// counts [E], then for tiles of 1, 4 and 8 row units (those of the grouped products) the
+// number of tiles before each expert, E + 1 entries (the last one the total).  The first of the
+// three is the experts' first row units.
+constexpr int kPlanTables = 3;
+__host__ __device__ constexpr int plan_log_units(int table) { return table ? table + 1 : 0; }
 __host__ __device__ inline int64_t plan_info_ints(int64_t E) { return E + kPlanTables * (E + 1); }
-__host__ __device__ inline int64_t plan_table_offset(int64_t E, int log_units) { return E + log_units * (E + 1); }
+// log_units: 0, 2 or 3
+__host__ __device__ inline int64_t plan_table_offset(int64_t E, int log_units) {
+    return E + (log_units ? log_units - 1 : 0) * (E + 1);
+}
 // row units an expert plan of n assignments can need: every expert's last unit may
 // hold a single row
 __host__ __device__ inline int64_t plan_max_units(int64_t n, int64_t E) {

@@ -757,15 +757,15 @@ __global__ void __launch_bounds__(C::NT) mx_split_kernel(Args a)
 }
 
 // The kernels: tiles of 32 and 64 rows split over the k loop, of 128 and of 256 rows, the latter
-// also of 96 channels.
+// also of 96 channels.  (A plan has tables for those of 1, 4 and 8 row units.)
 enum Kernel { kSplit1, kSplit2, kTile128, kTile256, kTile256x96 };
 constexpr int kLogUnits[] = {0, 1, 2, 3, 3};   // row units of a tile
 
 template <Out OUT, int B, bool GROUPED, bool RAGGED, MxType T>
 void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
+    constexpr bool DENSE = OUT == Out::Plain && !GROUPED;   // what kSplit2 and kTile256x96 are for
     using S1 = std::conditional_t<OUT == Out::Plain, Split1, SplitMx>;
-    using S2 = std::conditional_t<OUT == Out::Plain && !GROUPED, Split2, S1>;
-    const int bn = kernel == kSplit1 ? S1::BN : kernel == kSplit2 ? S2::BN : kernel == kTile256x96 ? 96 : kBN;
+    const int bn = kernel == kSplit1 ? S1::BN : kernel == kSplit2 ? Split2::BN : kernel == kTile256x96 ? 96 : kBN;
     a.tiles_n = (a.N + bn - 1) / bn;
     const dim3 grid((unsigned)(row_tiles * a.tiles_n));
     switch (kernel) {
@@ -773,7 +773,9 @@ void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
             hipLaunchKernelGGL((mx_split_kernel<S1, OUT, B, GROUPED, RAGGED, T>), grid, dim3(S1::NT), 0, stream, a);
             break;
         case kSplit2:
-            hipLaunchKernelGGL((mx_split_kernel<S2, OUT, B, GROUPED, RAGGED, T>), grid, dim3(S2::NT), 0, stream, a);
+            if constexpr (DENSE)
+                hipLaunchKernelGGL((mx_split_kernel<Split2, OUT, B, GROUPED, RAGGED, T>), grid, dim3(Split2::NT), 0, stream,
+                                   a);
             break;
         case kTile128:
             hipLaunchKernelGGL((mx_tile_kernel<2, 4, OUT, B, GROUPED, RAGGED, T>), grid, dim3(128), 0, stream, a);
@@ -782,7 +784,7 @@ void launch_one(Args a, Kernel kernel, int64_t row_tiles, hipStream_t stream) {
             hipLaunchKernelGGL((mx_tile_kernel<4, 4, OUT, B, GROUPED, RAGGED, T>), grid, dim3(256), 0, stream, a);
             break;
         case kTile256x96:
-            if constexpr (OUT == Out::Plain && !GROUPED)
+            if constexpr (DENSE)
                 hipLaunchKernelGGL((mx_tile_kernel<4, 3, OUT, B, GROUPED, RAGGED, T>), grid, dim3(256), 0, stream, a);
             break;
     }

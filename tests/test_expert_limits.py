@@ -42,3 +42,9 @@ def test_very_wide_rows():
     assert torch.equal(out[0, :N], y[0, :N]) and (out[1, :N] == 0).all()
     assert torch.equal(out[2, :N], 0 - y[0, :N])
     assert (out[:, N:] == 5).all()
+
+
+def test_a_plan_holds_the_tables_that_products_read():
+    """Counts, and the tiles before each expert for tiles of 32, 128 and 256 rows."""
+    for E in (1, 64, 512):
+        assert clq.clq_expert_plan_ints(E) == E + 3 * (E + 1)
