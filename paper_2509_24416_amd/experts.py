@@ -35,7 +35,10 @@ class ExpertMLP:
         self.graph = None
 
     def forward(self, x):
-        """x: fp16 or bf16 [tokens, hidden] -> the same shape and type."""
+        """x: fp16 or bf16 [tokens, hidden] -> the same shape and type.  No tokens (a process that was
+        sent none) give none."""
+        if x.shape[0] == 0 and x.dtype in (torch.float16, torch.bfloat16) and x.shape[1:] == self.router.shape[1:]:
+            return torch.empty_like(x)   # (the operators take one token or more)
         ids, weights = clq_expert_route(x.float() @ self.router.t(), self.top_k, **self.route)
         plan = clq_expert_plan(ids, self.experts)
         q = clq_mx4_dispatch(x, plan, self.block)

@@ -76,3 +76,14 @@ def test_capture_is_on_the_layers_device(monkeypatch):
     m.capture(3)
     # (a stream of its own: the graph context's may be another device's)
     assert r.entered == [("device", m.router.device), ("graph", ("stream", m.router.device))]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_a_process_without_tokens_gets_none_back(dtype):
+    m = _layer()
+    m.top_k, m.route = 2, {}
+    y = m.forward(torch.zeros(0, 64, dtype=dtype))
+    assert y.shape == (0, 64) and y.dtype == dtype
+    for bad in (torch.zeros(0, 32, dtype=dtype), torch.zeros(0, 64), torch.zeros(0, dtype=dtype)):
+        with pytest.raises(Exception):
+            m.forward(bad)
