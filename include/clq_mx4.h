@@ -23,7 +23,10 @@
  *   - Matrix and code pointers are 16-byte aligned, scales 16-byte aligned, bias 2-byte,
  *     int32 and float tables 4-byte aligned.
  *   - perm must be a permutation of 0..K-1 and activations and weights quantized with the
- *     same block and perm.  These are not checked.
+ *     same block and perm.  These are not checked (activations may also come gathered
+ *     already, and are then quantized without perm).
+ *   - An output must not overlap the matrices that the call reads (the Python binding
+ *     refuses it).
  */
 #ifndef CLQ_MX4_H
 #define CLQ_MX4_H

@@ -493,7 +493,7 @@ hipError_t launch_plan(const int32_t *ids, int64_t n, int k, int E, int32_t *inf
 // out[t] = sum over the slots, in order and in fp32, of weight * Y[row]; a slot without
 // a row adds nothing.  W columns per thread; the rows and weights of four slots are read
 // ahead of their values, whose loads are then in flight together.  Bound by memory (43200 x 1152 of
-// two slots, fp16: 51 us, 5.9 TB/s with the memory-side cache).
+// two slots, fp16: 51 us, 5.9 TB/s with the memory-side cache; fp32 values: 88 us, 5.6 TB/s).
 struct CombineArgs {
     const void *Y;
     const int32_t *rows;

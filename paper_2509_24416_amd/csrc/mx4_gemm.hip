@@ -89,8 +89,11 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b) {
 }
 
 // The tanh form of GELU: 0.5 h (1 + tanh u) = h / (1 + exp(-2u)), the exponent's constants
-// times log2 e.  The hardware's exp2 and reciprocal (1 ulp each) keep the relative error near
-// 3e-7, under that of the sum it is applied to.
+// times log2 e.  With the hardware's exp2 and reciprocal (1 ulp each) the relative error is under
+// 6e-7 for h > -2; below, exp2 scales up its argument's rounding with the argument (2e-6 at -5,
+// 1e-5 at -10, where the results are -2e-7 and -1e-37).  The absolute error is under 1e-7 for
+// negative h: that of the sum it is applied to, or less.  SiLU, whose argument is h itself: 1e-6 at
+// -16.
 __device__ __forceinline__ float gelu(float h) {
     const float t = h * __builtin_fmaf(-0.10294324f, h * h, -2.3022082f);   // -2u log2 e
     return h * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
@@ -145,12 +148,15 @@ __device__ __forceinline__ RowTile find_tile(const Args &a, int t, int lane) {
 // needed at the end of quad q + 1.  Within the loop transfers past the end repeat the last
 // stage or quad, so that its wait counts are constant; the stages after it have their own.
 //
-// What bounds it: the matrix instructions (8 per wave and stage of 32 cycles) and the vector
-// instructions of the epilogue, which do not overlap on a SIMD, and on large products the power
-// limit (the clock falls from 2.4 to 1.6 .. 2.0 GHz).  8192^3 244 us, 4.5 PFLOP/s, matrix cores
-// 68% busy; 43200 x 4608 -> 1152 116 us, 4.0 PFLOP/s; 43200 x 1152 -> 4608 140 to 186 us (2.8
-// TB/s of fp16 results at best; 78 with two stages of k loop), with GELU and requantization 185;
-// 8192 x 1152 -> 4608 the same 41 us.
+// What bounds it: on long k loops the matrix instructions (8 per wave and stage of 32 cycles) at
+// the clock that the power limit leaves (8192^3 228 to 244 us, 4.5 to 4.8 PFLOP/s, matrix cores
+// 68% busy; 43200 x 4608 -> 1152 104 to 116 us, 4.0 to 4.4 PFLOP/s); with GELU and requantization
+// on many rows the epilogue's vector instructions (62% of issue beside 30% of matrix cycles).
+// Otherwise no unit by itself: a tile's prologue, its few stages and its stores follow one another,
+// and the other workgroup of the compute unit covers a part of that.  43200 x 1152 -> 4608: 140
+// to 186 us, matrix cores 36% busy, vector issue 16%, 2.0 of 2.4 GHz (76 us with one stage of k
+// loop); 8192 x 1152 -> 4608 with GELU and requantization 41 us, 20% and 42% at full clock, its
+// 1152 tiles being 2.25 rounds of the 512 workgroups that run at a time.
 constexpr int kBN = 128;                        // channels (FN = 4)
 constexpr int kStageBytes = 4 * kMxUnit;        // 4 / NW units from each wave (FN = 3: the last twice)
 constexpr int kQuadBytes = 4 * kMxScaleRow;
@@ -255,8 +261,9 @@ __device__ __forceinline__ void store8(const Args &a, const float *s, int64_t m,
 // Stores the 16-bit outputs of one 32-row unit (row0 ..), 128 channels from n0.  A lane's
 // 16 channels of a row are 32 bytes of 32 different rows to a store, and the L2 takes a
 // request for each; so the wave turns the unit in its own part of LDS (rows kRowPitch bytes
-// apart, for the banks) and stores four whole 256-byte row pieces at a time.  (fp32 outputs
-// are 64 bytes a lane, whole requests as they are.)
+// apart, for the banks) and stores four whole 256-byte row pieces at a time.  (fp32 outputs are
+// stored as they lie, 16 bytes of 64 places at a time: 43200 x 1152 -> 4608 322 us, 2.5 TB/s of
+// results.)
 constexpr int kRowPitch = 272, kTurnBytes = 32 * kRowPitch;
 
 template <int FN, bool RAGGED, MxType T>

@@ -568,8 +568,8 @@ def clq_mx4_experts(q, plan, qw, bias=None, dtype=None, out=None, stream=None):
             return clq_mx4_experts(q, plan, qw, bias, dtype, out)
     M, K, N = q.rows, q.K, qw.N
     # (16-bit results make 1.4 times the error of one rounding in the sum, and halve the bytes; whole
-    # layers, us, 16 bits / fp32: 512 tokens to 2 of 16 experts of width 1152 49 / 50, 4096 103 / 114,
-    # 43200 704 / 823; 4096 to 6 of 64 102 / 137)
+    # layers, us, 16 bits / fp32: 512 tokens to 2 of 16 experts of width 1152 46 / 48, 4096 102 / 115,
+    # 43200 716 / 842; 4096 to 6 of 64 105 / 136)
     if dtype is None:
         dtype = torch.float32 if out is None else out.dtype
     Y, ld = _output(out, M, N, dtype, device)
