@@ -95,7 +95,7 @@ class MX4Weight:
 
     def __post_init__(self):
         if self.codes.is_cuda:
-            rows = (self.experts or 1) * ((self.N + 63) // 64 * 64)
+            rows = _weight_rows(self.experts, self.N)
             _bytes(self.codes, _code_bytes(rows, self.K), "codes")
             _bytes(self.scales, _scale_bytes(rows, self.K), "scales")
             _together(self.codes.device, "scales", self.scales)
@@ -188,6 +188,10 @@ def _bytes(t, n, name):
         raise ValueError(f"{name} must be a contiguous uint8 tensor of at least {n} bytes")
 
 
+def _weight_rows(experts, N):
+    return (experts or 1) * ((N + 63) // 64 * 64)
+
+
 def _code_bytes(rows, K):
     return (rows + 31) // 32 * 32 * (K // 2)
 
@@ -255,7 +259,9 @@ def _row_bytes(t, rows, columns, ld):
 
 
 def _weight_bytes(qw):
-    return tuple((t.data_ptr(), 1, t.numel(), t.numel()) for t in (qw.codes, qw.scales))
+    rows = _weight_rows(qw.experts, qw.N)
+    sizes = _code_bytes(rows, qw.K), _scale_bytes(rows, qw.K)
+    return tuple((t.data_ptr(), 1, n, n) for t, n in zip((qw.codes, qw.scales), sizes))
 
 
 def _apart(out, *inputs):

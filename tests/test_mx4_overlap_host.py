@@ -70,3 +70,22 @@ def test_pieces_of_rows():
         for rows, width in ((1, 3), (2, 7), (3, 10)):
             x, y = (20, 3, 10, 4), (at, rows, 10, width)
             assert _meet(x, y) == bool(covered(*x) & covered(*y)), (x, y)
+
+
+def test_weights_reach_as_far_as_their_matrices(accepting):
+    """What lies behind them in a larger buffer is the caller's."""
+    buf, plan = _bytes(), _plan()
+    q, size = _mx4(buf, 0), 64 * 64 + 2 * 256
+    codes, scales = buf[16384:], buf[40960:]
+    for at, bad in ((16384 + 128 * 64, False), (16384 + 128 * 64 - 16, True), (40960 + 4 * 256, False),
+                    (40960 + 4 * 256 - 16, True), (40960 - size, False)):
+        for call in _calls(_mx4(buf, at), q, _weight(codes, scales), plan):
+            with pytest.raises(ValueError if bad else _Accepted):
+                call()
+    # several experts' matrices
+    two = clq.MX4Weight(codes, scales, 100, 128, experts=2)
+    plan.experts = 2
+    for at, bad in ((16384 + 2 * 128 * 64 - 16, True), (16384 + 2 * 128 * 64, False), (40960 + 2 * 4 * 256 - 16, True),
+                    (40960 + 2 * 4 * 256, False)):
+        with pytest.raises(ValueError if bad else _Accepted):
+            clq.clq_mx4_experts_mx4(q, plan, two, out=_mx4(buf, at))
