@@ -845,3 +845,6 @@ def clq_clps_search(X, W, Y0, block, perm=None, gamma=0.01, grid=20, workspace=N
 
 # the microscaled 4-bit operators and the expert layer (include/clq_mx4.h)
 from .mx4 import *  # noqa: E402,F401,F403
+
+# RMS norm, rotary positions and the 8-bit linear's epilogue (include/clq_block.h)
+from .block import *  # noqa: E402,F401,F403

@@ -1,0 +1,337 @@
+"""Python binding of the operators around the 8-bit linears of a transformer block
+(``include/clq_block.h``).
+
+Argument marshalling only, in the manner of the package's other entry points:
+
+    clq_rms_norm(X, weight=None, residual=None, eps=1e-6)            -> Y, or (Y, sum)
+    clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None)
+                                                                     -> (Xq8, x_scale), or (Xq8, x_scale, sum)
+    clq_dequantize_act8(Xq8, x_scale, K, dtype=torch.float16)        -> values
+    clq_rope_freqs(axes, theta=10000.0, device="cuda")               -> freqs
+    clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, weight=None) -> Y
+    clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual=None) -> Y
+
+Every call enqueues on the current stream, or on `stream`; what it allocates belongs
+to that stream.  Nothing here has a gradient of its own: the package is post-training quantization.
+"""
+import ctypes
+
+import torch
+
+from . import (CLQ_ERR_ARG, CLQ_ERR_SHAPE, ClqError, _check, _check_xq8, _lib, _ptr, _raw_stream, clq_act8_bytes,
+               clq_weight8_bytes, clq_weight_bytes)
+from .mx4 import _HALF, _TYPES, _apart, _current_device, _dev, _elsewhere, _gather, _output, _row_bytes, _rows2d, _together
+
+_i64, _i32, _f32, _p = ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
+_SIGNATURES = {
+    "clq_rms_norm": (_i32, [_p, _i32, _i64, _p, _i32, _i64, _p, _i32, _i64, _f32, _i64, _i64, _p, _i32, _i64, _p, _i64,
+                            _p]),
+    "clq_rms_norm_act8": (_i32, [_p, _i32, _i64, _p, _i32, _i64, _p, _i32, _i64, _f32, _p, _i64, _i64, _i32, _p, _p, _p,
+                                 _i64, _p]),
+    "clq_dequantize_act8": (_i32, [_p, _p, _i64, _i64, _i32, _p, _i64, _p]),
+    "clq_rope_axes": (_i32, [_p, _i32, _i64, _i64, _p, _i32, _i64, _p, _p, _i32, _i32, _i32, _p, _i32, _i64, _f32, _i64,
+                             _i64, _i64, _p, _i64, _i64, _p]),
+    "clq_a8_linear_act": (_i32, [_p, _p, _p, _p, _i32, _p, _i32, _i32, _p, _i32, _i64, _p, _i64, _i64, _i64, _i64, _i32, _p,
+                                 _i64, _p]),
+}
+for _name, (_res, _args) in _SIGNATURES.items():
+    getattr(_lib, _name).restype = _res
+    getattr(_lib, _name).argtypes = _args
+
+BLOCK_EXPORTS = tuple(_SIGNATURES)
+__all__ = ["BLOCK_EXPORTS", "clq_rope_freqs", *BLOCK_EXPORTS]
+
+_ACTS = {None: 0, "none": 0, "gelu": 1, "silu": 3}
+
+
+def _flat_bytes(t):
+    n = t.numel() * t.element_size()
+    return t.data_ptr(), 1, n, n
+
+
+def _modulation(w, name, K, M, device, types=_TYPES):
+    """Pointer, type and samples of a [K] or [samples, K] matrix (None: none)."""
+    if w is None:
+        return None, 0, 1
+    _dev(w, name, types)
+    if w.dim() not in (1, 2) or w.shape[-1] != K or not w.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{K}] or [samples, {K}] tensor")
+    samples = 1 if w.dim() == 1 else w.shape[0]
+    if samples < 1 or M % samples:
+        raise ValueError(f"{name} has {samples} samples, which do not divide {M} rows")
+    _together(device, name, w)
+    return w.data_ptr(), _TYPES[w.dtype], samples
+
+
+def _in_place(out, t, ld_out, ld):
+    """Whether an output is that very matrix."""
+    return out.data_ptr() == t.data_ptr() and ld_out == ld and out.dtype == t.dtype
+
+
+def _norm_operands(X, weight, residual, sum_out):
+    """Checks what both forms of the norm share; (rows, columns, stride, weight, residual, sum) with the last
+    three as the C call takes them."""
+    M, K, ldx = _rows2d(X, "X")
+    device = X.device
+    w = _modulation(weight, "weight", K, M, device)
+    if residual is None:
+        if sum_out is not None:
+            raise ValueError("there is no sum without a residual")
+        return M, K, ldx, w, (None, 0, 0)
+    r, k, ldr = _rows2d(residual, "residual", _TYPES)
+    if (r, k) != (M, K):
+        raise ValueError(f"residual must be [{M}, {K}]")
+    _together(device, "residual", residual)
+    if sum_out is not None:
+        _sum_rows(X, residual, sum_out, M, K, ldx, ldr, weight)
+    return M, K, ldx, w, (residual.data_ptr(), _TYPES[residual.dtype], ldr)
+
+
+def _sum_rows(X, residual, sum_out, M, K, ldx, ldr, weight):
+    s, n, lds = _rows2d(sum_out, "sum_out", (residual.dtype,))
+    if (s, n) != (M, K):
+        raise ValueError(f"sum_out must be [{M}, {K}]")
+    _together(X.device, "sum_out", sum_out)
+    at = _row_bytes(sum_out, M, K, lds)
+    if not _in_place(sum_out, residual, lds, ldr):
+        _apart(at, _row_bytes(residual, M, K, ldr))
+    _apart(at, _row_bytes(X, M, K, ldx), *(() if weight is None else (_flat_bytes(weight),)))
+    return lds
+
+
+def _norm_inputs(X, weight, residual, M, K, ldx, r):
+    """What a norm's output must not lie in, X apart."""
+    return (*(() if weight is None else (_flat_bytes(weight),)),
+            *(() if residual is None else (_row_bytes(residual, M, K, r[2]),)))
+
+
+def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, sum_out=None, stream=None):
+    """Y = s / sqrt(mean(s^2) + eps) * weight with s = X + residual, per row.  X: fp16 or bf16 [M, K], any
+    row stride that is a multiple of 8.  weight: [K], or [samples, K] for rows of that many equal samples.
+    residual: fp16, bf16 or fp32 [M, K]; the sum comes back too, in its type (sum_out: where, the residual
+    itself included).  dtype: of Y (X's by default).  out: where, X itself included."""
+    M, K, ldx, w, r = _norm_operands(X, weight, residual, sum_out)
+    device = X.device
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_rms_norm(X, weight, residual, eps, dtype, out, sum_out)
+    if dtype is None:
+        dtype = X.dtype if out is None else out.dtype
+    Y, ldy = _output(out, M, K, dtype, device)
+    if out is not None:
+        at = _row_bytes(Y, M, K, ldy)
+        if not _in_place(Y, X, ldy, ldx):
+            _apart(at, _row_bytes(X, M, K, ldx))
+        _apart(at, *_norm_inputs(X, weight, residual, M, K, ldx, r))
+    S, lds = None, 0
+    if residual is not None:
+        S, lds = _output(sum_out, M, K, residual.dtype, device)
+        if out is not None and sum_out is not None:
+            _apart(_row_bytes(S, M, K, lds), _row_bytes(Y, M, K, ldy))
+    _check(_lib.clq_rms_norm(X.data_ptr(), _TYPES[X.dtype], ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, M, K,
+                             Y.data_ptr(), _TYPES[dtype], ldy, _ptr(S), lds, _raw_stream(i)), "clq_rms_norm")
+    return Y if S is None else (Y, S)
+
+
+def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None, out=None, scale_out=None,
+                      sum_out=None, stream=None):
+    """The norm of clq_rms_norm rotated by blocks of `block` (after gathering its columns by `perm`) and
+    quantized to 8 bits a value with one scale a row, without a rounding in between: what
+    clq_rotate_quant_act8 returns, (Xq8 uint8 [clq_act8_bytes(M, K)], x_scale fp32 [M]), and with a
+    residual the sum."""
+    M, K, ldx, w, r = _norm_operands(X, weight, residual, sum_out)
+    device = X.device
+    g = None if perm is None else _gather(perm, K, device)
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_rms_norm_act8(X, block, weight, residual, eps, perm, out, scale_out, sum_out)
+    n = clq_act8_bytes(M, K)
+    if n == 0:
+        raise ClqError(CLQ_ERR_SHAPE, "clq_rms_norm_act8")
+    reads = None
+    if out is not None or scale_out is not None:
+        reads = (_row_bytes(X, M, K, ldx), *_norm_inputs(X, weight, residual, M, K, ldx, r),
+                 *(() if perm is None else (_flat_bytes(perm),)),
+                 *(() if sum_out is None else (_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K),)))
+    if out is None:
+        out = torch.empty(n, dtype=torch.uint8, device=device)
+    else:
+        if _dev(out, "out", (torch.uint8,)).numel() < n or not out.is_contiguous():
+            raise ValueError("the output's buffer is too small")
+        _together(device, "out", out)
+        _apart((out.data_ptr(), 1, n, n), *reads)
+    if scale_out is None:
+        scale_out = torch.empty(M, dtype=torch.float32, device=device)
+    else:
+        if _dev(scale_out, "scale_out", (torch.float32,)).numel() < M or not scale_out.is_contiguous():
+            raise ValueError("the scales' buffer is too small")
+        _together(device, "scale_out", scale_out)
+        _apart((scale_out.data_ptr(), 1, 4 * M, 4 * M), (out.data_ptr(), 1, n, n), *(reads or ()))
+    S, lds = (None, 0) if residual is None else _output(sum_out, M, K, residual.dtype, device)
+    _check(_lib.clq_rms_norm_act8(X.data_ptr(), _TYPES[X.dtype], ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, g, M, K,
+                                  block, out.data_ptr(), scale_out.data_ptr(), _ptr(S), lds, _raw_stream(i)),
+           "clq_rms_norm_act8")
+    return (out, scale_out) if S is None else (out, scale_out, S)
+
+
+def clq_dequantize_act8(Xq8, x_scale, K, dtype=torch.float16, out=None, stream=None):
+    """The values that 8-bit activations stand for (still rotated): fp16, bf16 or fp32 [M, K], M =
+    len(x_scale)."""
+    M = _check_xq8(Xq8, x_scale, K)
+    device = Xq8.device
+    _together(device, "x_scale", x_scale)
+    if x_scale.dim() != 1 or not x_scale.is_contiguous():
+        raise ValueError("x_scale must be a contiguous [M] tensor")
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_dequantize_act8(Xq8, x_scale, K, dtype, out)
+    o, ld = _output(out, M, K, dtype, device)
+    if out is not None:
+        _apart(_row_bytes(o, M, K, ld), _flat_bytes(Xq8), _flat_bytes(x_scale))
+    _check(_lib.clq_dequantize_act8(Xq8.data_ptr(), x_scale.data_ptr(), M, K, _TYPES[dtype], o.data_ptr(), ld,
+                                    _raw_stream(i)), "clq_dequantize_act8")
+    return o
+
+
+def _pair_ends(axes):
+    """Pairs of the axes so far, from the columns each axis turns."""
+    axes = tuple(axes)
+    if not 1 <= len(axes) <= 4 or any(int(d) != d or d < 2 or d % 2 for d in axes):
+        raise ValueError("axes must be one to four positive even numbers of columns")
+    ends, n = (_i32 * len(axes))(), 0
+    for j, d in enumerate(axes):
+        n += int(d) // 2
+        ends[j] = n
+    return ends, n
+
+
+def clq_rope_freqs(axes, theta=10000.0, device="cuda"):
+    """Radians a position for each pair: an axis of d columns has theta^(-2 j / d), j = 0 .. d / 2 - 1
+    (fp64 [sum(axes) / 2])."""
+    _pair_ends(axes)
+    return torch.cat([float(theta) ** (-torch.arange(0, d, 2, dtype=torch.float64, device=device) / d) for d in axes])
+
+
+def _head_strides(X, name, types):
+    """Rows, heads, head width, row and head strides of [M, heads, D]."""
+    _dev(X, name, types)
+    if X.dim() != 3 or (X.stride(2) != 1 and X.shape[2] != 1):
+        raise ValueError(f"{name} must be [rows, heads, D] with unit column stride")
+    M, H, D = X.shape
+    ld, lh = X.stride(0), X.stride(1)
+    # (a single row or head has no stride of its own; torch gives such a view any)
+    lh = D if H == 1 else lh
+    return M, H, D, (max(H * lh, D) + 7) & ~7 if M == 1 else ld, lh
+
+
+def _head_bytes(X, M, H, D, ld, lh):
+    size = X.element_size()
+    if ld >= lh or H == 1:
+        return X.data_ptr(), M, ld * size, ((H - 1) * lh + D) * size
+    return X.data_ptr(), H, lh * size, ((M - 1) * ld + D) * size
+
+
+def clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, weight=None, eps=1e-6, out=None,
+                  stream=None):
+    """Turns the first sum(axes) columns of each head by its row's position on each axis.  X: fp16 or bf16
+    [rows, heads, D], strides multiples of 8 (columns of a wider projection, queries and keys together).
+    positions: int32 or fp32 [tokens, len(axes)], for rows that repeat those tokens (a batch).  freqs: fp64
+    [sum(axes) / 2] radians a position (clq_rope_freqs).  interleaved: pairs are neighbours; otherwise a column
+    pairs with the one half of the turned columns on.  inverse: by the opposite angles.  weight: [D] or
+    [heads, D] of an RMS norm of each head ahead of the turn.  out: where, X itself included."""
+    M, H, D, ldx, lhx = _head_strides(X, "X", _HALF)
+    device = X.device
+    ends, n = _pair_ends(axes)
+    _dev(positions, "positions", (torch.int32, torch.float32))
+    if positions.dim() != 2 or positions.shape[1] != len(ends) or not positions.is_contiguous():
+        raise ValueError(f"positions must be a contiguous [tokens, {len(ends)}] tensor")
+    tokens = positions.shape[0]
+    if tokens < 1 or M % tokens:
+        raise ValueError(f"positions of {tokens} tokens do not repeat over {M} rows")
+    _dev(freqs, "freqs", (torch.float64,))
+    if freqs.shape != (n,) or not freqs.is_contiguous():
+        raise ValueError(f"freqs must be a contiguous fp64 [{n}] tensor")
+    if 2 * n > D:
+        raise ValueError(f"the axes turn {2 * n} columns, a head has {D}")
+    for t, name in ((positions, "positions"), (freqs, "freqs")):
+        _together(device, name, t)
+    w, wt, wh = None, 0, 1
+    if weight is not None:
+        _dev(weight, "weight", _TYPES)
+        if weight.shape not in ((D,), (H, D)) or not weight.is_contiguous():
+            raise ValueError(f"weight must be a contiguous [{D}] or [{H}, {D}] tensor")
+        _together(device, "weight", weight)
+        w, wt, wh = weight.data_ptr(), _TYPES[weight.dtype], 1 if weight.dim() == 1 else H
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_rope_axes(X, positions, freqs, axes, interleaved, inverse, weight, eps, out)
+    if out is None:
+        Y, ldy, lhy = torch.empty(M, H, D, dtype=X.dtype, device=device), H * D, D
+    else:
+        m, h, d, ldy, lhy = _head_strides(out, "out", (X.dtype,))
+        if (m, h, d) != (M, H, D):
+            raise ValueError(f"out must be [{M}, {H}, {D}]")
+        _together(device, "out", out)
+        Y, at = out, _head_bytes(out, M, H, D, ldy, lhy)
+        if not (_in_place(Y, X, ldy, ldx) and lhy == lhx):
+            _apart(at, _head_bytes(X, M, H, D, ldx, lhx))
+        _apart(at, _flat_bytes(positions), _flat_bytes(freqs), *(() if weight is None else (_flat_bytes(weight),)))
+    _check(_lib.clq_rope_axes(X.data_ptr(), _TYPES[X.dtype], ldx, lhx, positions.data_ptr(),
+                              int(positions.dtype is torch.float32), tokens, freqs.data_ptr(), ends, len(ends),
+                              int(bool(interleaved)), int(bool(inverse)), w, wt, wh, eps, M, H, D, Y.data_ptr(), ldy, lhy,
+                              _raw_stream(i)), "clq_rope_axes")
+    return Y
+
+
+def clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual=None, dtype=None, out=None, stream=None):
+    """clq_a8_linear with an epilogue: Y = residual + gate * act(X . W^T + bias), fp32 throughout and rounded
+    once.  act: None, "gelu" (tanh form) or "silu".  gate: [N], or [samples, N] for rows of that many equal
+    samples.  residual: of Y's type [M, N].  dtype: of Y (by default that of `out`, of the residual, or fp16).
+    out: where, the residual itself included."""
+    M = _check_xq8(Xq8, x_scale, qw.K)
+    N, K, device = qw.N, qw.K, Xq8.device
+    if x_scale.dim() != 1 or not x_scale.is_contiguous():
+        raise ValueError("x_scale must be a contiguous [M] tensor")
+    if qw.bits not in (4, 8):
+        raise ClqError(CLQ_ERR_ARG, "clq_a8_linear_act")
+    if qw.wq.numel() < (clq_weight_bytes if qw.bits == 4 else clq_weight8_bytes)(N, K) or qw.w_scale.numel() < N:
+        raise ValueError("the weights' buffers are too small for their N and K")
+    if act not in _ACTS:
+        raise ValueError(f"act must be None, 'gelu' or 'silu', not {act!r}")
+    for t, name in ((x_scale, "x_scale"), (qw.wq, "weights"), (qw.w_scale, "weights")):
+        _together(device, name, t)
+    b, bt = None, 0
+    if bias is not None:
+        _dev(bias, "bias", _HALF)
+        if bias.shape != (N,) or not bias.is_contiguous():
+            raise ValueError(f"bias must be a contiguous [{N}] tensor")
+        _together(device, "bias", bias)
+        b, bt = bias.data_ptr(), _TYPES[bias.dtype]
+    g, gt, samples = _modulation(gate, "gate", N, M, device)
+    if dtype is None:
+        dtype = out.dtype if out is not None else residual.dtype if residual is not None else torch.float16
+    r, ldr = None, 0
+    if residual is not None:
+        rows, columns, ldr = _rows2d(residual, "residual", (dtype,))
+        if (rows, columns) != (M, N):
+            raise ValueError(f"residual must be [{M}, {N}]")
+        _together(device, "residual", residual)
+        r = residual.data_ptr()
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_a8_linear_act(Xq8, x_scale, qw, bias, act, gate, residual, dtype, out)
+    Y, ld = _output(out, M, N, dtype, device)
+    if out is not None:
+        at = _row_bytes(Y, M, N, ld)
+        if residual is not None and not _in_place(Y, residual, ld, ldr):
+            _apart(at, _row_bytes(residual, M, N, ldr))
+        _apart(at, *(_flat_bytes(t) for t in (Xq8, x_scale, qw.wq, qw.w_scale, bias, gate) if t is not None))
+    _check(_lib.clq_a8_linear_act(Xq8.data_ptr(), x_scale.data_ptr(), qw.wq.data_ptr(), qw.w_scale.data_ptr(), qw.bits, b,
+                                  bt, _ACTS[act], g, gt, samples, r, ldr, M, N, K, _TYPES[dtype], Y.data_ptr(), ld,
+                                  _raw_stream(i)), "clq_a8_linear_act")
+    return Y

@@ -1,0 +1,417 @@
+// RMS norm with the residual's addition, its result plain (fp16, bf16, fp32) or rotated
+// (CLQ, arXiv 2509.24416, Sec. 3.3) and quantized to 8 bits a token (Sec. 3.1, Eq. (1) with
+// n = 8) for the 8-bit linears.
+//
+//   s = x + r,  n = s w / sqrt(mean(s^2) + eps),  x~ = FWHT_b(gather(n, perm))
+//
+// The rotation is linear, so a row's factor 1 / sqrt(..) is left out of it: with v = FWHT_b(gather(s w))
+// and m = max|v|, the codes are rne(v * 127 / m), which do not hold the factor at all, and the scale is
+// m / 127 times the factor.  One pass over a row then yields its squares' sum and its maximum together,
+// between one pair of barriers, and no value is kept anywhere but in registers.
+//
+// What bounds it is memory, so the split is the rotate+quantize kernels': a lane owns one 16-byte
+// chunk (8 columns) of four rows.  Sums and maxima meet over 8 lanes by lane permutes, then through LDS
+// in a fixed order (each lane of an octet adds every eighth octet's partials, then the octet adds up),
+// so that results do not depend on the order in which waves arrive.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "block.h"
+#include "rq_device.h"
+
+namespace clq {
+namespace {
+
+constexpr int kMaxGroups = 8;    // four-row groups per workgroup
+constexpr int kMaxLanes = 1024;
+constexpr int kLdsLimit = 160 * 1024 - 8192;   // gathered rows of a workgroup, beside the partials
+
+struct NormArgs : RmsNormArgs {
+    int groups, stride;   // four-row groups per workgroup, lanes of each
+    int64_t unit0;        // first 32-row unit of this launch
+    int units;
+};
+
+// the larger of two magnitudes, a NaN if either is one
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// over the eight lanes of an octet, in each of them
+constexpr int kHalfMirror = 0x141;   // DPP control: lane ^ 7
+template <class Op>
+__device__ __forceinline__ float octet(float v, Op &&op) {
+    v = op(v, lane_xchg<kLaneXor1>(v));
+    v = op(v, lane_xchg<kLaneXor2>(v));
+    return op(v, lane_xchg<kHalfMirror>(v));
+}
+
+template <int CTRL>
+__device__ __forceinline__ void pair_exchange(uint32_t &lo, uint32_t &hi, bool b) {
+    const uint32_t plo = lane_xchg<CTRL>(lo), phi = lane_xchg<CTRL>(hi);
+    lo = b ? phi : lo;
+    hi = b ? hi : plo;
+}
+
+// The codes of one chunk column of a quad's four rows (rows rho0 .. rho0 + 3 of unit u) from rotated
+// values and the rows' signed reciprocals: a 16-byte operand piece is the even codes of 16, then the
+// odd, of a lane pair; lane b0 of the pair stores rows b0 and 2 + b0.
+__device__ __forceinline__ void store_codes8(const float (&x)[4][8], const float (&rs)[4], int64_t u, int rho0, int chunk,
+                                             int K, uint8_t *__restrict__ out, bool active) {
+    constexpr float M = Grid<8>::magic;
+    const int lam = chunk & 3;
+    const bool b0 = lam & 1;
+    uint32_t ev[4], od[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(__builtin_fmaf(x[r][e], rs[r], M));
+        ev[r] = low_bytes4(w[0], w[2], w[4], w[6]) ^ 0x80808080u;
+        od[r] = low_bytes4(w[1], w[3], w[5], w[7]) ^ 0x80808080u;
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        pair_exchange<kLaneXor1>(ev[2 * s], ev[2 * s + 1], b0);
+        pair_exchange<kLaneXor1>(od[2 * s], od[2 * s + 1], b0);
+        if (active)
+            *reinterpret_cast<uint4 *>(out + q8_piece_offset(u, rho0 + 2 * s + (lam & 1), chunk >> 2, lam >> 1, K)) =
+                make_uint4(ev[2 * s], ev[2 * s + 1], od[2 * s], od[2 * s + 1]);
+    }
+}
+
+// B: Hadamard block (0: plain result).  RES: the residual (0 none, 1 16-bit, 2 fp32).  NCH: chunks per
+// lane (1: rows of up to 8192 columns, 2: up to 16384).
+template <int B, int RES, int NCH>
+__global__ void __launch_bounds__(kMaxLanes) rms_norm_kernel(NormArgs a)
+{
+    extern __shared__ __align__(16) float gat[];   // gathered inputs: a column's rows side by side
+    __shared__ float4 psum[kMaxLanes / 8], pmax[B ? kMaxLanes / 8 : 1];
+    const int t = threadIdx.x;
+    const int wpu = 8 / a.groups;                   // workgroups per unit
+    const int idx = blockIdx.x >> 3;
+    const int64_t ul = (int64_t)(blockIdx.x & 7) + 8 * (int64_t)(idx / wpu);
+    if (ul >= a.units) return;
+    const int64_t u = a.unit0 + ul;
+    const int K = a.K, cpr = K >> 3;
+    const int gl = t / a.stride, t0 = t - gl * a.stride;
+    const bool glive = gl < a.groups;
+    const int s = (idx % wpu) * a.groups + (glive ? gl : 0);
+    const int64_t row0 = u * 32 + 4 * s;
+    const int lane_c = logical_lane(t0);   // its chunk among the octet's eight
+
+    int64_t row[4];
+    bool rv[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        rv[r] = glive && row0 + r < a.M;
+        row[r] = rv[r] ? row0 + r : 0;
+    }
+    const bool bf16 = a.x_type == MxType::BF16;
+
+    // s w of each chunk, and the rows' sums of squares
+    float x[NCH][4][8], sq[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    {
+        uint4 v[NCH][4];
+        uint4 res[NCH][4][RES == 2 ? 2 : 1];
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int at = min(lane_c + i * a.stride, cpr - 1) * 8;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)   // (unconditional, so that all are in flight)
+                v[i][r] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.X) + row[r] * a.ldx + at);
+            if constexpr (RES == 1) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    res[i][r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.R) + row[r] * a.ldr + at);
+            } else if constexpr (RES == 2) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.R) + row[r] * a.ldr + at);
+                    res[i][r][0] = p[0];
+                    res[i][r][1] = p[1];
+                }
+            }
+        }
+        // (rows of one sample share their weights' load)
+        const uint32_t sr = (uint32_t)a.sample_rows, first = (uint32_t)row[0] / sr;
+        const bool one = (uint32_t)min(row[0] + 3, a.M - 1) / sr == first;
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int chunk = lane_c + i * a.stride, at = min(chunk, cpr - 1) * 8;
+            const bool live = chunk < cpr;
+            float w[8];
+            if (a.W != nullptr) load8(a.W, (int64_t)first * K + at, a.w_type, w);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float(&y)[8] = x[i][r];
+                widen8(v[i][r], bf16, y);
+                if constexpr (RES == 1) {
+                    float q[8];
+                    widen8(res[i][r][0], a.r_type == MxType::BF16, q);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] += q[e];
+                } else if constexpr (RES == 2) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 q = res[i][r][h];
+                        y[4 * h] += __uint_as_float(q.x);
+                        y[4 * h + 1] += __uint_as_float(q.y);
+                        y[4 * h + 2] += __uint_as_float(q.z);
+                        y[4 * h + 3] += __uint_as_float(q.w);
+                    }
+                }
+                if constexpr (RES != 0)
+                    if (rv[r] && live) store8(a.sum, row[r] * a.ld_sum + at, RES == 2 ? MxType::F32 : a.r_type, y);
+                if (!rv[r] || !live) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sq[r] = __builtin_fmaf(y[e], y[e], sq[r]);
+                if (a.W != nullptr) {
+                    if (!one && r > 0) load8(a.W, (int64_t)((uint32_t)row[r] / sr) * K + at, a.w_type, w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = (rv[r] && live) ? y[e] * w[e] : 0.0f;
+                }
+            }
+        }
+    }
+
+    const CrossSigns cs = cross_signs<B ? B : 32>(lane_c);
+    if constexpr (B != 0) {
+        if (a.perm != nullptr) {
+            // P rows of the group at a time, a column's side by side: one LDS read serves them
+            constexpr int P = NCH == 1 ? 4 : 2;
+            float *mine = gat + (int64_t)(glive ? gl : 0) * K * P;
+            float g[NCH][4][8];
+#pragma unroll
+            for (int p0 = 0; p0 < 4; p0 += P) {
+                if (p0 > 0) __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NCH; ++i) {
+                    const int chunk = lane_c + i * a.stride;
+                    if (glive && chunk < cpr) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+#pragma unroll
+                            for (int p = 0; p < P; ++p) mine[(chunk * 8 + e) * P + p] = x[i][p0 + p][e];
+                    }
+                }
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NCH; ++i) {
+                    const int32_t *q = a.perm + min(lane_c + i * a.stride, cpr - 1) * 8;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float *c = mine + (int64_t)q[e] * P;
+#pragma unroll
+                        for (int p = 0; p < P; ++p) g[i][p0 + p][e] = c[p];
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NCH; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[i][r][e] = lane_c + i * a.stride < cpr ? g[i][r][e] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p = x[i][r][e], q = x[i][r][e + 1];
+                    x[i][r][e] = p + q;
+                    x[i][r][e + 1] = p - q;
+                }
+                fwht8_rest(x[i][r]);
+            }
+            cross_stages<B, 4>(x[i], cs);
+        }
+    }
+
+    // the rows' sums and maxima: octet, LDS, octet
+    float m[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [](float p, float q) { return p + q; };
+    auto larger = [](float p, float q) { return max_nan(p, q); };
+    if constexpr (B != 0) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m[r] = max_nan(m[r], fabsf(x[i][r][e]));
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        sq[r] = octet(sq[r], add);
+        if constexpr (B != 0) m[r] = octet(m[r], larger);
+    }
+    if ((t & 7) == 0) {
+        psum[t >> 3] = make_float4(sq[0], sq[1], sq[2], sq[3]);
+        if constexpr (B != 0) pmax[t >> 3] = make_float4(m[0], m[1], m[2], m[3]);
+    }
+    __syncthreads();
+    const int first = (glive ? gl : 0) * (a.stride >> 3);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sq[r] = m[r] = 0.0f;
+    for (int j = t & 7; j < a.stride >> 3; j += 8) {
+        const float4 p = psum[first + j];
+        sq[0] += p.x, sq[1] += p.y, sq[2] += p.z, sq[3] += p.w;
+        if constexpr (B != 0) {
+            const float4 q = pmax[first + j];
+            m[0] = max_nan(m[0], q.x), m[1] = max_nan(m[1], q.y), m[2] = max_nan(m[2], q.z), m[3] = max_nan(m[3], q.w);
+        }
+    }
+    float inv[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        sq[r] = octet(sq[r], add);
+        if constexpr (B != 0) m[r] = octet(m[r], larger);
+        inv[r] = 1.0f / sqrtf(sq[r] / (float)K + a.eps);
+    }
+
+    if constexpr (B == 0) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int chunk = lane_c + i * a.stride;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][r][e] *= inv[r];
+                if (rv[r] && chunk < cpr) store8(a.Y, row[r] * a.ldy + chunk * 8, a.y_type, x[i][r]);
+            }
+        }
+    } else {
+        float rs[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            // (maxima whose reciprocal would overflow count as zeros: eps keeps the factor finite)
+            const float top = m[r] < 0x1p-100f ? 0.0f : m[r];
+            rs[r] = (top == 0.0f ? 0.0f : 127.0f / top) * cs.sign;
+            if (t0 == r && rv[r]) a.x_scale[row[r]] = (top / 127.0f) * inv[r];
+        }
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            const int chunk = lane_c + i * a.stride;
+            store_codes8(x[i], rs, u, 4 * s, chunk, K, a.Xq8, glive && chunk < cpr);
+        }
+    }
+}
+
+// Four-row groups per workgroup: the most live lanes of whole waves, more groups on a tie, but no
+// more than leaves two workgroups per compute unit to the launch.
+int pick_groups(int stride, int64_t total_groups, int cus) {
+    int best = 1;
+    double best_u = 0.0;
+    for (int g = 1; g <= kMaxGroups && g * stride <= kMaxLanes; g <<= 1) {
+        if (g > 1 && g * stride > 64 && total_groups / g < 2 * cus) break;
+        const int waves = (g * stride + 63) / 64;
+        if (g > 1 && waves > 8) break;
+        const double u = (double)(g * stride) * (16 / waves);
+        if (u >= best_u) {
+            best_u = u;
+            best = g;
+        }
+    }
+    return best;
+}
+
+template <int B, int RES, int NCH>
+hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
+    NormArgs a;
+    static_cast<RmsNormArgs &>(a) = args;
+    const int cpr = a.K >> 3;
+    const int64_t units = padded_act_rows(a.M) / 32;
+    constexpr int P = NCH == 1 ? 4 : 2;
+    if constexpr (NCH == 1) {
+        a.stride = (cpr + 7) / 8 * 8;
+        a.groups = pick_groups(a.stride, units * 8, compute_units());
+        while (B != 0 && a.perm != nullptr && a.groups > 1 && (size_t)a.groups * a.K * P * 4 > kLdsLimit) a.groups >>= 1;
+    } else {
+        a.groups = 1;
+        a.stride = ((cpr + 1) / 2 + 63) / 64 * 64;
+    }
+    const int T = (a.groups * a.stride + 63) / 64 * 64;
+    const size_t lds = B != 0 && a.perm != nullptr ? (size_t)a.groups * a.K * P * 4 : 0;
+    if (T > kMaxLanes || lds > kLdsLimit) return hipErrorInvalidConfiguration;
+    if (lds > 65536 - 8192) {
+        hipError_t e = hipFuncSetAttribute((const void *)rms_norm_kernel<B, RES, NCH>,
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, kLdsLimit);
+        if (e != hipSuccess) return e;
+    }
+    // launches of at most 2^31 lanes
+    const int64_t per_unit = (int64_t)(8 / a.groups) * T;
+    const int64_t most = std::max<int64_t>(8, (((int64_t)1 << 31) / per_unit) / 8 * 8);
+    for (a.unit0 = 0; a.unit0 < units; a.unit0 += most) {
+        a.units = (int)std::min<int64_t>(most, units - a.unit0);
+        const int64_t grid = ((int64_t)a.units + 7) / 8 * 8 * (8 / a.groups);
+        hipLaunchKernelGGL((rms_norm_kernel<B, RES, NCH>), dim3((unsigned)grid), dim3(T), lds, stream, a);
+    }
+    return hipGetLastError();
+}
+
+template <int B, int RES>
+hipError_t launch_width(const RmsNormArgs &a, hipStream_t stream) {
+    return a.K <= 8 * kMaxLanes ? launch_norm<B, RES, 1>(a, stream) : launch_norm<B, RES, 2>(a, stream);
+}
+template <int B>
+hipError_t launch_residual(const RmsNormArgs &a, hipStream_t stream) {
+    if (a.R == nullptr) return launch_width<B, 0>(a, stream);
+    return a.r_type == MxType::F32 ? launch_width<B, 2>(a, stream) : launch_width<B, 1>(a, stream);
+}
+
+// One 16-byte operand piece (16 codes of a row) per thread: four threads write a row's 64 codes, sixteen
+// rows a wave read whole 256-byte pieces.
+__global__ void dequantize_act8_kernel(const uint8_t *__restrict__ q8, const float *__restrict__ scale, int64_t M, int K,
+                                       MxType type, void *__restrict__ out, int64_t ldo) {
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int piece = (int)(i & 3), rho = (int)(i >> 2) & 31;
+    const int64_t unit = i >> 7, kus = K >> 6, u = unit / kus, ku = unit - u * kus;
+    const int64_t row = u * 32 + rho;
+    if (row >= M) return;
+    const int h = piece >> 1, q = piece & 1;
+    const uint4 v = *reinterpret_cast<const uint4 *>(q8 + q8_piece_offset(u, rho, 2 * ku + h, q, K));
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const float sc = scale[row];
+    const int64_t at = row * ldo + ku * 64 + h * 32 + q * 16;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {   // (bytes 0 .. 7: even codes, 8 .. 15: odd ones)
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = (float)(int8_t)(w[2 * (e & 1) + half] >> (8 * (e >> 1))) * sc;
+        store8(out, at + 8 * half, type, x);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t stream) {
+    if (a.Y != nullptr) return launch_residual<0>(a, stream);
+    switch (a.block) {
+        case 32: return launch_residual<32>(a, stream);
+        case 64: return launch_residual<64>(a, stream);
+        case 128: return launch_residual<128>(a, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_dequantize_act8(const uint8_t *Xq8, const float *x_scale, int64_t M, int K, MxType type, void *out,
+                                  int64_t ldo, hipStream_t stream) {
+    // units of 32 rows x 64 codes, 128 threads each; launches of at most 2^31 lanes
+    const int64_t units = (padded_act_rows(M) >> 5) * (K >> 6), kus = K >> 6;
+    const int64_t most = (((int64_t)1 << 24) / kus) * kus;   // whole row units
+    for (int64_t u0 = 0; u0 < units; u0 += most) {
+        const int64_t n = std::min(most, units - u0), rows0 = u0 / kus * 32;
+        hipLaunchKernelGGL(dequantize_act8_kernel, dim3((unsigned)((n + 1) / 2)), dim3(256), 0, stream,
+                           Xq8 + u0 * 2048, x_scale + rows0, M - rows0, K, type,
+                           static_cast<uint8_t *>(out) + rows0 * ldo * (type == MxType::F32 ? 4 : 2), ldo);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace clq

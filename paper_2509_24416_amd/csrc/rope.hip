@@ -1,0 +1,189 @@
+// Rotary positions with several axes (time, height, width), on heads that may be normed first:
+// pair i of a head, (a, b) -> (a cos - b sin, b cos + a sin) at the angle
+// position[row, axis(i)] * freq[i].
+//
+// Angles are formed in fp64 as revolutions and reduced there (position * freq / 2 pi less its nearest
+// whole number), so that far positions lose nothing; sine and cosine then take an fp32 argument of half
+// a revolution at most.
+//
+// What bounds it is memory (every value read and written once), and ahead of that the sines: 1 of a head's
+// pairs and rows each, shared by all heads of a row.  So a lane owns the same piece of every head that it
+// works on, an item: eight columns (interleaved pairs), or V columns and their partners (halves paired; V =
+// 8, or 4 where half of the turned columns is no multiple of 8), and computes their angles once.  A wave
+// takes as many heads side by side as its 64 lanes hold, several rows where a row's heads do not fill it.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "block.h"
+
+namespace clq {
+namespace {
+
+struct RopeLaunch : RopeArgs {
+    int items, turned;   // items of a head, those that turn
+    int side;            // heads side by side in a wave
+    int rows;            // rows of a wave
+    int slices;          // waves that share a row's heads
+    int64_t m0, m1;      // rows of this launch
+};
+
+// V 16-bit values
+template <int V>
+__device__ __forceinline__ void load_v(const uint16_t *p, bool bf16, float (&x)[V]) {
+    if constexpr (V == 8) {
+        widen8(*reinterpret_cast<const uint4 *>(p), bf16, x);
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = widen16((uint16_t)((e < 2 ? v.x : v.y) >> (16 * (e & 1))), bf16);
+    }
+}
+template <int V>
+__device__ __forceinline__ void store_v(uint16_t *p, bool bf16, const float (&x)[V]) {
+    if constexpr (V == 8) *reinterpret_cast<uint4 *>(p) = narrow8(x, bf16);
+    else *reinterpret_cast<uint2 *>(p) = make_uint2(narrow2(x[0], x[1], bf16), narrow2(x[2], x[3], bf16));
+}
+__device__ __forceinline__ float weight(const void *W, MxType type, int64_t at) {
+    return type == MxType::F32 ? static_cast<const float *>(W)[at]
+                               : widen16(static_cast<const uint16_t *>(W)[at], type == MxType::BF16);
+}
+
+// PAIRS: interleaved pairs (V = 8 columns an item), otherwise an item's V columns pair with V others.
+template <bool PAIRS, int V, bool NORM>
+__global__ void __launch_bounds__(256) rope_kernel(RopeLaunch a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t rowgroup = wave / a.slices;
+    const int slice = (int)(wave - rowgroup * a.slices);
+    const int hd = lane / a.items, c = lane - hd * a.items;   // head of the wave's, item
+    const int sub = hd / a.side, g = hd - sub * a.side;        // row of the wave's, head of the row's
+    const int64_t m = a.m0 + rowgroup * a.rows + sub;
+    const bool live = sub < a.rows && m < a.m1;
+    const int half = a.ends[3];                               // pairs
+    const bool turns = c < a.turned;
+    // the item's columns: c0 onwards, and (halves paired) half + c0 onwards
+    const int c0 = PAIRS ? 8 * c : turns ? V * c : 2 * half + V * (c - a.turned);
+
+    constexpr int NP = PAIRS ? V / 2 : V;   // its pairs
+    float cs[NP], sn[NP];
+    if (live && turns) {
+        const int64_t token = (uint32_t)m % (uint32_t)a.tokens;
+        const int i0 = PAIRS ? 4 * c : V * c;
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            const int i = i0 + j;
+            const int axis = (i >= a.ends[0]) + (i >= a.ends[1]) + (i >= a.ends[2]);
+            const int64_t at = token * a.axes + axis;
+            const double p = a.float_positions ? (double)static_cast<const float *>(a.positions)[at]
+                                               : (double)static_cast<const int32_t *>(a.positions)[at];
+            double r = p * a.freqs[i] * 0.15915494309189535;
+            r -= rint(r);
+            sincospif(2.0f * (float)r, &sn[j], &cs[j]);
+            if (a.inverse) sn[j] = -sn[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) cs[j] = 1.0f, sn[j] = 0.0f;
+    }
+
+    const uint16_t *xr = a.X + (live ? m : 0) * a.ldx;
+    uint16_t *yr = a.Y + (live ? m : 0) * a.ldy;
+    // (the trip count is the wave's own, so that its lanes meet at the norm's exchanges)
+    for (int h0 = slice * a.side; h0 < a.heads; h0 += a.slices * a.side) {
+        const int h = h0 + g;
+        const bool on = live && h < a.heads;
+        const uint16_t *xp = xr + (on ? h : 0) * a.lhx + c0;
+        float x[V], y[V];
+        if (on) load_v<V>(xp, a.bf16, x);
+        if constexpr (!PAIRS) {
+            if (on && turns) load_v<V>(xp + half, a.bf16, y);
+        }
+        if constexpr (NORM) {
+            float s = 0.0f;
+            if (on) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) s = __builtin_fmaf(x[e], x[e], s);
+                if (!PAIRS && turns) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s = __builtin_fmaf(y[e], y[e], s);
+                }
+            }
+            // the head's items are neighbours: each adds what lies 1, 2, 4, .. items behind it, in a
+            // fixed order, until the first holds the sum
+            for (int off = 1; off < a.items; off <<= 1) {
+                const float o = __shfl(s, lane + off);
+                if (c + off < a.items) s += o;
+            }
+            s = __shfl(s, lane - c);
+            const float inv = 1.0f / sqrtf(s / (float)a.D + a.eps);
+            if (on) {
+                const int64_t w0 = h * a.w_stride + c0;
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[e] = x[e] * inv * weight(a.W, a.w_type, w0 + e);
+                if (!PAIRS && turns) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) y[e] = y[e] * inv * weight(a.W, a.w_type, w0 + half + e);
+                }
+            }
+        }
+        if (!on) continue;
+        uint16_t *yp = yr + h * a.lhy + c0;
+        if (!turns) {
+            store_v<V>(yp, a.bf16, x);
+        } else if constexpr (PAIRS) {
+            float z[V];
+#pragma unroll
+            for (int j = 0; j < NP; ++j) {
+                z[2 * j] = __builtin_fmaf(x[2 * j], cs[j], -(x[2 * j + 1] * sn[j]));
+                z[2 * j + 1] = __builtin_fmaf(x[2 * j + 1], cs[j], x[2 * j] * sn[j]);
+            }
+            store_v<V>(yp, a.bf16, z);
+        } else {
+            float z[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) z[j] = __builtin_fmaf(x[j], cs[j], -(y[j] * sn[j]));
+            store_v<V>(yp, a.bf16, z);
+#pragma unroll
+            for (int j = 0; j < V; ++j) z[j] = __builtin_fmaf(y[j], cs[j], x[j] * sn[j]);
+            store_v<V>(yp + half, a.bf16, z);
+        }
+    }
+}
+
+template <bool PAIRS, int V>
+hipError_t launch(RopeLaunch a, hipStream_t stream) {
+    a.turned = PAIRS ? 2 * a.ends[3] / 8 : a.ends[3] / V;
+    a.items = a.turned + (a.D - 2 * a.ends[3]) / V;
+    if (a.items < 1 || a.items > 64) return hipErrorInvalidValue;
+    const int fit = 64 / a.items;
+    a.side = std::min(fit, a.heads);
+    a.rows = fit / a.side;
+    const int steps = (a.heads + a.side - 1) / a.side;
+    const int64_t groups = (a.M + a.rows - 1) / a.rows;
+    // few rows: their heads to several waves, up to eight waves a compute unit
+    a.slices = (int)std::max<int64_t>(1, std::min<int64_t>(steps, 8 * (int64_t)compute_units() / groups));
+    // launches of at most 2^31 lanes
+    const int64_t most = (((int64_t)1 << 25) / a.slices) * a.rows;
+    for (a.m0 = 0; a.m0 < a.M; a.m0 += most) {
+        a.m1 = std::min(a.M, a.m0 + most);
+        const int64_t waves = (a.m1 - a.m0 + a.rows - 1) / a.rows * a.slices;
+        const dim3 grid((unsigned)((waves + 3) / 4));
+        if (a.W != nullptr) hipLaunchKernelGGL((rope_kernel<PAIRS, V, true>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((rope_kernel<PAIRS, V, false>), grid, dim3(256), 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs &args, hipStream_t stream) {
+    RopeLaunch a;
+    static_cast<RopeArgs &>(a) = args;
+    if (a.interleaved) return launch<true, 8>(a, stream);
+    return a.ends[3] % 8 == 0 && (a.D - 2 * a.ends[3]) % 8 == 0 ? launch<false, 8>(a, stream) : launch<false, 4>(a, stream);
+}
+
+}  // namespace clq

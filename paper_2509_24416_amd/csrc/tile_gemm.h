@@ -32,6 +32,7 @@
 
 #include <type_traits>
 
+#include "block.h"
 #include "clq_internal.h"
 #include "f6_codes.h"
 
@@ -150,7 +151,17 @@ struct Args {
     double *errp;
     int nc;
     int64_t wq_stride, ws_stride, p_stride;
+    // activating epilogue (Epi::F16 and on): residual of the output's type, gate by sample
+    const void *gate, *res;
+    int64_t ldr;
+    int act, sample_rows;
+    bool res_vec;   // the residual's rows are 16-byte aligned
+    MxType bias_type, gate_type;
 };
+
+// What is done with the sums: the epilogue of the entry points without activation, or activation, gate
+// and residual with the result in one of three types.
+enum class Epi { Plain, F16, BF16, F32 };
 
 // a stage's operands of one wave: 4 channel units, 2 token units.  read: from
 // the units' LDS addresses (wa, xa: of lane 0's bytes); wait<VM>: at most VM
@@ -349,6 +360,80 @@ __device__ __forceinline__ void store_fragment(const Args &a, const Acc<F> &x, c
     }
 }
 
+// The tanh form of GELU and SiLU with the hardware's exp2 and reciprocal (1 ulp each): h / (1 + 2^t).
+// Relative errors under 6e-7 for h > -2; below, exp2 scales up its argument's rounding with the argument
+// (1e-5 at -10, where GELU is -1e-37 and SiLU's error 1e-6); absolute errors for negative h under 1e-7.
+__device__ __forceinline__ float activated(float h, int act) {
+    if (act == (int)Act8::None) return h;
+    const float t = act == (int)Act8::Gelu ? h * __builtin_fmaf(-0.10294324f, h * h, -2.3022082f) : h * -1.4426950408889634f;
+    return h * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+}
+
+// store_fragment with activation, gate and residual.
+template <Fmt F, int BN, Epi E>
+__device__ __forceinline__ void store_activated(const Args &a, const Acc<F> &x, const float *ep, int c0, int r0, int n0,
+                                                int m) {
+    if (m >= a.M || n0 >= a.N) return;
+    constexpr MxType T = E == Epi::F16 ? MxType::F16 : E == Epi::BF16 ? MxType::BF16 : MxType::F32;
+    const float xsc = ep[2 * BN + r0] * (1.0f / (float)(1 << FmtInfo<F>::LOG));
+    float y[2][8];
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+        y[v >> 3][v & 7] = activated(__builtin_fmaf((float)x[v] * xsc, ep[c0 + v], ep[BN + c0 + v]), a.act);
+    const bool whole = n0 <= a.N - 16;
+    if (a.gate != nullptr) {
+        const int64_t at = (int64_t)((uint32_t)m / (uint32_t)a.sample_rows) * a.N + n0;
+        if (whole && a.N % 8 == 0) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float g[8];
+                load8(a.gate, at + 8 * h, a.gate_type, g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[h][e] *= g[e];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (n0 + v < a.N)
+                    y[v >> 3][v & 7] *= a.gate_type == MxType::F32
+                                            ? static_cast<const float *>(a.gate)[at + v]
+                                            : clq::widen16(static_cast<const uint16_t *>(a.gate)[at + v], a.gate_type == MxType::BF16);
+        }
+    }
+    if (a.res != nullptr) {
+        const int64_t at = (int64_t)m * a.ldr + n0;
+        if (whole && a.res_vec) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float r[8];
+                load8(a.res, at + 8 * h, T, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[h][e] += r[e];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (n0 + v < a.N) {
+                    if constexpr (T == MxType::F32) y[v >> 3][v & 7] += static_cast<const float *>(a.res)[at + v];
+                    else y[v >> 3][v & 7] += clq::widen16(static_cast<const uint16_t *>(a.res)[at + v], T == MxType::BF16);
+                }
+        }
+    }
+    const int64_t at = (int64_t)m * a.ldy + n0;
+    if (whole) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) store8(a.Y, at + 8 * h, T, y[h]);
+    } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            if (n0 + v < a.N) {
+                const float s = y[v >> 3][v & 7];
+                if constexpr (T == MxType::F32) static_cast<float *>(a.Y)[at + v] = s;
+                else static_cast<uint16_t *>(a.Y)[at + v] = (uint16_t)narrow2(s, s, T == MxType::BF16);
+            }
+    }
+}
+
 // Tile number of this workgroup: workgroups are dealt to the 8 XCDs
 // round-robin, and each XCD takes a contiguous run.
 __device__ __forceinline__ int tile_of_block() {
@@ -397,11 +482,39 @@ struct EpilogueOperands {
     }
 };
 
+// The same for the activating epilogue: biases of either 16-bit type or none, at run time.
+template <int BN, int BM, int NT>
+struct ActivatedOperands {
+    static constexpr int EPN = 2 * BN + BM, EPR = (EPN + NT - 1) / NT;
+    float v[EPR];
+    uint16_t b[EPR];
+    __device__ __forceinline__ void load(const Args &a, int tm, int tn, int tid) {
+#pragma unroll
+        for (int r = 0; r < EPR; ++r) {
+            const int e = min(tid + r * NT, EPN - 1);
+            const int ec = min(tn * BN + (e & (BN - 1)), a.N - 1), er = min(tm * BM + max(e - 2 * BN, 0), a.M - 1);
+            const float *p = e < 2 * BN ? a.ws + ec : a.xs + er;
+            v[r] = *p;
+            // (without a bias: some value of the scales, not used)
+            const uint16_t *q = a.bias != nullptr ? a.bias + ec : reinterpret_cast<const uint16_t *>(a.ws) + ec;
+            b[r] = *q;
+        }
+    }
+    __device__ __forceinline__ void store(const Args &a, float *ep, int tid) const {
+#pragma unroll
+        for (int r = 0; r < EPR; ++r) {
+            const int e = min(tid + r * NT, EPN - 1);
+            const float bias = a.bias != nullptr ? clq::widen16(b[r], a.bias_type == MxType::BF16) : 0.0f;
+            ep[e] = e >= BN && e < 2 * BN ? bias : v[r];
+        }
+    }
+};
+
 // ERR: nothing is stored; the epilogue sums (Y0 - sum * x_scale * w_scale)^2
 // over the tile in fp64 (the integer sum exact) and keeps one partial per wave.
 // A target tile's candidates are neighbours in the tile order, so that one
 // XCD's L2 serves the target and the activation panel to all of them.
-template <class C, bool I32OUT, bool RAGGED, bool BIAS, bool ERR = false>
+template <class C, bool I32OUT, bool RAGGED, bool BIAS, bool ERR = false, Epi E = Epi::Plain>
 __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
 {
     static_assert(!(I32OUT && BIAS), "no bias on the integer output");
@@ -486,7 +599,8 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
     // ---- epilogue operands: loaded ahead of the transfers, held in registers
     // through the k loop, written to LDS after it (an LDS store while transfers
     // into LDS are in flight would wait for all of them)
-    EpilogueOperands<C::BN, C::BM, C::NT, BIAS> eo;
+    std::conditional_t<E == Epi::Plain, EpilogueOperands<C::BN, C::BM, C::NT, BIAS>,
+                       ActivatedOperands<C::BN, C::BM, C::NT>> eo;
     if constexpr (!I32OUT) eo.load(a, tm, tn, tid);
     __builtin_amdgcn_sched_barrier(0);
 
@@ -539,7 +653,8 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
     op[0].template wait<0>();
     op[1].template wait<0>();
     if constexpr (!I32OUT) {
-        eo.store(ep, tid);
+        if constexpr (E == Epi::Plain) eo.store(ep, tid);
+        else eo.store(a, ep, tid);
         __syncthreads();
     }
 
@@ -594,7 +709,9 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
         static_for<0, C::FM>([&](auto mc) {
             constexpr int fn = decltype(fc)::value, fm = decltype(mc)::value;
             const int c0 = fn * 32 + h16, r0 = (wave * C::FM + fm) * 32 + (lane & 31);
-            store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
+            if constexpr (E == Epi::Plain)
+                store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
+            else store_activated<F, C::BN, E>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
         });
     });
 }
@@ -619,7 +736,7 @@ struct SplitCfg {
     static_assert(KS == 2 || KS == 4, "recursive halving over 8 fragments");
 };
 
-template <class C, bool I32OUT, bool RAGGED, bool BIAS>
+template <class C, bool I32OUT, bool RAGGED, bool BIAS, Epi E = Epi::Plain>
 __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
 {
     static_assert(!(I32OUT && BIAS), "no bias on the integer output");
@@ -640,7 +757,8 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
 #pragma unroll
     for (int f = 0; f < 2; ++f) xs[f] = a.Xq + (int64_t)min(tm * 2 + f, xunits - 1) * nks * C::XU;
 
-    EpilogueOperands<C::BN, C::BM, C::NT, BIAS> eo;
+    std::conditional_t<E == Epi::Plain, EpilogueOperands<C::BN, C::BM, C::NT, BIAS>,
+                       ActivatedOperands<C::BN, C::BM, C::NT>> eo;
     if constexpr (!I32OUT) eo.load(a, tm, tn, tid);
     __builtin_amdgcn_sched_barrier(0);
 
@@ -678,7 +796,10 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
     if constexpr (D > 2)
         if (rest > 1) mma(IC<1>{});
 
-    if constexpr (!I32OUT) eo.store(ep, tid);   // (the exchange's barriers publish it)
+    if constexpr (!I32OUT) {   // (the exchange's barriers publish it)
+        if constexpr (E == Epi::Plain) eo.store(ep, tid);
+        else eo.store(a, ep, tid);
+    }
 
     // one step's messages: fragments [fn0, fn0 + nf) x [fm0, fm0 + mf)
     using V4 = std::conditional_t<F == Fmt::F6, v4f, v4i>;
@@ -715,8 +836,10 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
             static_for<0, decltype(mf)::value>([&](auto j) {
                 constexpr int fn = decltype(fn0)::value + decltype(i)::value, fm = decltype(fm0)::value + decltype(j)::value;
                 const int c0 = fn * 32 + h16, r0 = fm * 32 + (lane & 31);
-                store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0,
-                                                              tm * C::BM + r0);
+                if constexpr (E == Epi::Plain)
+                    store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0,
+                                                                  tm * C::BM + r0);
+                else store_activated<F, C::BN, E>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
             });
         });
     };
