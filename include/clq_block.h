@@ -27,7 +27,7 @@ extern "C" {
 
 /* ---- RMS norm ------------------------------------------------------------------------
  *   s = X + R,   n = s / sqrt(mean(s^2) + eps) * W[sample]
- *   X        fp16 or bf16 [M][K], row stride ldx.
+ *   X        fp16, bf16 or fp32 [M][K], row stride ldx.
  *   R        the residual stream, fp16, bf16 or fp32 [M][K], row stride ldr; NULL: none (then sum is
  *            NULL too).
  *   W        fp16, bf16 or fp32 [samples][K], contiguous; NULL: ones (samples 1).
@@ -50,6 +50,11 @@ clq_status clq_rms_norm_act8(const void *X, clq_type x_type, int64_t ldx, const 
                              const void *W, clq_type w_type, int64_t samples, float eps, const int32_t *perm,
                              int64_t M, int64_t K, int32_t block, void *Xq8, float *x_scale, void *sum, int64_t ld_sum,
                              hipStream_t stream);
+
+/* clq_rotate_quant_act8 of fp16, bf16 or fp32 activations (the results of an activating linear, say, that
+ * were not rounded to 16 bits): the same codes and scales for fp16.  Shapes as above. */
+clq_status clq_quantize_act8(const void *X, clq_type x_type, int64_t ldx, const int32_t *perm, int64_t M, int64_t K,
+                             int32_t block, void *Xq8, float *x_scale, hipStream_t stream);
 
 /* The values that 8-bit codes and their scales stand for (still rotated): out [M][K] of `type`, row
  * stride ldo.  64 <= K <= 32768, K % 64 == 0. */

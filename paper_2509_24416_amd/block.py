@@ -6,6 +6,7 @@ Argument marshalling only, in the manner of the package's other entry points:
     clq_rms_norm(X, weight=None, residual=None, eps=1e-6)            -> Y, or (Y, sum)
     clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None)
                                                                      -> (Xq8, x_scale), or (Xq8, x_scale, sum)
+    clq_quantize_act8(X, block, perm=None)                           -> (Xq8, x_scale)
     clq_dequantize_act8(Xq8, x_scale, K, dtype=torch.float16)        -> values
     clq_rope_freqs(axes, theta=10000.0, device="cuda")               -> freqs
     clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, weight=None) -> Y
@@ -28,6 +29,7 @@ _SIGNATURES = {
                             _p]),
     "clq_rms_norm_act8": (_i32, [_p, _i32, _i64, _p, _i32, _i64, _p, _i32, _i64, _f32, _p, _i64, _i64, _i32, _p, _p, _p,
                                  _i64, _p]),
+    "clq_quantize_act8": (_i32, [_p, _i32, _i64, _p, _i64, _i64, _i32, _p, _p, _p]),
     "clq_dequantize_act8": (_i32, [_p, _p, _i64, _i64, _i32, _p, _i64, _p]),
     "clq_rope_axes": (_i32, [_p, _i32, _i64, _i64, _p, _i32, _i64, _p, _p, _i32, _i32, _i32, _p, _i32, _i64, _f32, _i64,
                              _i64, _i64, _p, _i64, _i64, _p]),
@@ -71,7 +73,7 @@ def _in_place(out, t, ld_out, ld):
 def _norm_operands(X, weight, residual, sum_out):
     """Checks what both forms of the norm share; (rows, columns, stride, weight, residual, sum) with the last
     three as the C call takes them."""
-    M, K, ldx = _rows2d(X, "X")
+    M, K, ldx = _rows2d(X, "X", _TYPES)
     device = X.device
     w = _modulation(weight, "weight", K, M, device)
     if residual is None:
@@ -106,7 +108,7 @@ def _norm_inputs(X, weight, residual, M, K, ldx, r):
 
 
 def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, sum_out=None, stream=None):
-    """Y = s / sqrt(mean(s^2) + eps) * weight with s = X + residual, per row.  X: fp16 or bf16 [M, K], any
+    """Y = s / sqrt(mean(s^2) + eps) * weight with s = X + residual, per row.  X: fp16, bf16 or fp32 [M, K], any
     row stride that is a multiple of 8.  weight: [K], or [samples, K] for rows of that many equal samples.
     residual: fp16, bf16 or fp32 [M, K]; the sum comes back too, in its type (sum_out: where, the residual
     itself included).  dtype: of Y (X's by default).  out: where, X itself included."""
@@ -134,27 +136,11 @@ def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, 
     return Y if S is None else (Y, S)
 
 
-def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None, out=None, scale_out=None,
-                      sum_out=None, stream=None):
-    """The norm of clq_rms_norm rotated by blocks of `block` (after gathering its columns by `perm`) and
-    quantized to 8 bits a value with one scale a row, without a rounding in between: what
-    clq_rotate_quant_act8 returns, (Xq8 uint8 [clq_act8_bytes(M, K)], x_scale fp32 [M]), and with a
-    residual the sum."""
-    M, K, ldx, w, r = _norm_operands(X, weight, residual, sum_out)
-    device = X.device
-    g = None if perm is None else _gather(perm, K, device)
-    i = device.index
-    if stream is not None or _current_device() != i:
-        with _elsewhere(device, stream):
-            return clq_rms_norm_act8(X, block, weight, residual, eps, perm, out, scale_out, sum_out)
+def _codes(M, K, device, out, scale_out, reads, where):
+    """Buffers of 8-bit codes and their scales: the caller's, checked against what the call reads, or new ones."""
     n = clq_act8_bytes(M, K)
     if n == 0:
-        raise ClqError(CLQ_ERR_SHAPE, "clq_rms_norm_act8")
-    reads = None
-    if out is not None or scale_out is not None:
-        reads = (_row_bytes(X, M, K, ldx), *_norm_inputs(X, weight, residual, M, K, ldx, r),
-                 *(() if perm is None else (_flat_bytes(perm),)),
-                 *(() if sum_out is None else (_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K),)))
+        raise ClqError(CLQ_ERR_SHAPE, where)
     if out is None:
         out = torch.empty(n, dtype=torch.uint8, device=device)
     else:
@@ -168,12 +154,54 @@ def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None,
         if _dev(scale_out, "scale_out", (torch.float32,)).numel() < M or not scale_out.is_contiguous():
             raise ValueError("the scales' buffer is too small")
         _together(device, "scale_out", scale_out)
-        _apart((scale_out.data_ptr(), 1, 4 * M, 4 * M), (out.data_ptr(), 1, n, n), *(reads or ()))
+        _apart((scale_out.data_ptr(), 1, 4 * M, 4 * M), (out.data_ptr(), 1, n, n), *reads)
+    return out, scale_out
+
+
+def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None, out=None, scale_out=None,
+                      sum_out=None, stream=None):
+    """The norm of clq_rms_norm rotated by blocks of `block` (after gathering its columns by `perm`) and
+    quantized to 8 bits a value with one scale a row, without a rounding in between: what
+    clq_rotate_quant_act8 returns, (Xq8 uint8 [clq_act8_bytes(M, K)], x_scale fp32 [M]), and with a
+    residual the sum."""
+    M, K, ldx, w, r = _norm_operands(X, weight, residual, sum_out)
+    device = X.device
+    g = None if perm is None else _gather(perm, K, device)
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_rms_norm_act8(X, block, weight, residual, eps, perm, out, scale_out, sum_out)
+    if out is None and scale_out is None:
+        q, xs = _codes(M, K, device, None, None, (), "clq_rms_norm_act8")
+    else:
+        q, xs = _codes(M, K, device, out, scale_out,
+                       (_row_bytes(X, M, K, ldx), *_norm_inputs(X, weight, residual, M, K, ldx, r),
+                        *(() if perm is None else (_flat_bytes(perm),)),
+                        *(() if sum_out is None else (_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K),))),
+                       "clq_rms_norm_act8")
     S, lds = (None, 0) if residual is None else _output(sum_out, M, K, residual.dtype, device)
     _check(_lib.clq_rms_norm_act8(X.data_ptr(), _TYPES[X.dtype], ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, g, M, K,
-                                  block, out.data_ptr(), scale_out.data_ptr(), _ptr(S), lds, _raw_stream(i)),
+                                  block, q.data_ptr(), xs.data_ptr(), _ptr(S), lds, _raw_stream(i)),
            "clq_rms_norm_act8")
-    return (out, scale_out) if S is None else (out, scale_out, S)
+    return (q, xs) if S is None else (q, xs, S)
+
+
+def clq_quantize_act8(X, block, perm=None, out=None, scale_out=None, stream=None):
+    """clq_rotate_quant_act8 of fp16, bf16 or fp32 activations [M, K] (any row stride that is a multiple of 8):
+    the same codes and scales for fp16."""
+    M, K, ldx = _rows2d(X, "X", _TYPES)
+    device = X.device
+    g = None if perm is None else _gather(perm, K, device)
+    i = device.index
+    if stream is not None or _current_device() != i:
+        with _elsewhere(device, stream):
+            return clq_quantize_act8(X, block, perm, out, scale_out)
+    q, xs = _codes(M, K, device, out, scale_out,
+                   () if out is None and scale_out is None else (_row_bytes(X, M, K, ldx), *(() if perm is None else (_flat_bytes(perm),))),
+                   "clq_quantize_act8")
+    _check(_lib.clq_quantize_act8(X.data_ptr(), _TYPES[X.dtype], ldx, g, M, K, block, q.data_ptr(), xs.data_ptr(),
+                                  _raw_stream(i)), "clq_quantize_act8")
+    return q, xs
 
 
 def clq_dequantize_act8(Xq8, x_scale, K, dtype=torch.float16, out=None, stream=None):

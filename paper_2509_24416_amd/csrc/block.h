@@ -21,7 +21,8 @@ struct RmsNormArgs {
     void *sum;               // R's type
     // plain result
     void *Y;
-    // 8-bit codes (Y == nullptr)
+    // 8-bit codes (Y == nullptr); norm: false for a quantizer alone
+    bool norm;
     const int32_t *perm;
     int block;
     uint8_t *Xq8;
@@ -61,6 +62,9 @@ struct Act8Args {
     int M, N, K, wbits;
 };
 hipError_t launch_a8_act(const Act8Args &a, hipStream_t stream);
+// by the output's type
+hipError_t launch_a8_act_bf16(const Act8Args &a, hipStream_t stream);
+hipError_t launch_a8_act_f32(const Act8Args &a, hipStream_t stream);
 
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
 __device__ __forceinline__ float widen16(uint16_t h, bool bf16) {

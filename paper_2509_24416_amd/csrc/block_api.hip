@@ -30,7 +30,7 @@ clq_status norm(const void *X, clq_type x_type, int64_t ldx, const void *R, clq_
                 clq_type w_type, int64_t samples, float eps, int64_t M, int64_t K, void *sum, int64_t ld_sum,
                 clq::RmsNormArgs &a) {
     if ((R == nullptr) != (sum == nullptr)) return CLQ_ERR_NULL;
-    if (!is_16bit(x_type) || (R && !is_type(r_type)) || (W && !is_type(w_type)) || !is_eps(eps)) return CLQ_ERR_ARG;
+    if (!is_type(x_type) || (R && !is_type(r_type)) || (W && !is_type(w_type)) || !is_eps(eps)) return CLQ_ERR_ARG;
     clq_status s;
     if ((s = check_rows(M)) != CLQ_OK || (s = check_samples(M, samples)) != CLQ_OK) return s;
     if (K < 8 || K > kMaxNormK || K % 8 != 0 || (!W && samples != 1)) return CLQ_ERR_SHAPE;
@@ -83,6 +83,29 @@ clq_status clq_rms_norm_act8(const void *X, clq_type x_type, int64_t ldx, const 
     clq_status s = norm(X, x_type, ldx, R, r_type, ldr, W, w_type, samples, eps, M, K, sum, ld_sum, a);
     if (s != CLQ_OK || (s = check_k(K)) != CLQ_OK || (s = check_block(K, block)) != CLQ_OK) return s;
     if (!aligned(Xq8, 16) || !aligned(x_scale, 4) || !aligned(perm, 4)) return CLQ_ERR_ALIGN;
+    a.norm = true;
+    a.perm = perm;
+    a.block = block;
+    a.Xq8 = static_cast<uint8_t *>(Xq8);
+    a.x_scale = x_scale;
+    return done(stream, clq::launch_rms_norm(a, stream));
+}
+
+clq_status clq_quantize_act8(const void *X, clq_type x_type, int64_t ldx, const int32_t *perm, int64_t M, int64_t K,
+                             int32_t block, void *Xq8, float *x_scale, hipStream_t stream) {
+    if (!X || !Xq8 || !x_scale) return CLQ_ERR_NULL;
+    if (!is_type(x_type)) return CLQ_ERR_ARG;
+    clq_status s;
+    if ((s = check_rows(M)) != CLQ_OK || (s = check_k(K)) != CLQ_OK || (s = check_block(K, block)) != CLQ_OK) return s;
+    if (K > kMaxNormK || !is_stride(ldx, K)) return CLQ_ERR_SHAPE;
+    if (!aligned(X, 16) || !aligned(Xq8, 16) || !aligned(x_scale, 4) || !aligned(perm, 4)) return CLQ_ERR_ALIGN;
+    clq::RmsNormArgs a = {};
+    a.X = X;
+    a.x_type = mx_type(x_type);
+    a.ldx = ldx;
+    a.M = M;
+    a.sample_rows = M;
+    a.K = (int)K;
     a.perm = perm;
     a.block = block;
     a.Xq8 = static_cast<uint8_t *>(Xq8);

@@ -30,8 +30,7 @@ constexpr int kLdsLimit = 160 * 1024 - 8192;   // gathered rows of a workgroup, 
 
 struct NormArgs : RmsNormArgs {
     int groups, stride;   // four-row groups per workgroup, lanes of each
-    int64_t unit0;        // first 32-row unit of this launch
-    int units;
+    int unit0, units;     // first 32-row unit of this launch, units
 };
 
 // the larger of two magnitudes, a NaN if either is one
@@ -80,99 +79,112 @@ __device__ __forceinline__ void store_codes8(const float (&x)[4][8], const float
     }
 }
 
-// B: Hadamard block (0: plain result).  RES: the residual (0 none, 1 16-bit, 2 fp32).  NCH: chunks per
-// lane (1: rows of up to 8192 columns, 2: up to 16384).
-template <int B, int RES, int NCH>
-__global__ void __launch_bounds__(kMaxLanes) rms_norm_kernel(NormArgs a)
+// Waves a SIMD that the registers are held to (what each form needs by itself, or a few less).
+template <int B, bool XW, int RES, bool NORM, int NCH>
+constexpr int waves_per_simd() {
+    if (NCH == 2) return 4;   // (a workgroup of 16 waves)
+    return NORM ? 7 - (B != 0) - (XW || RES == 2) : 7;
+}
+
+// B: Hadamard block (0: plain result).  XW: X in fp32.  RES: the residual (0 none, 1 16-bit, 2 fp32).  NORM:
+// without it the rows are only rotated and quantized.  MIXED: four rows may be of several samples (a branch
+// for it at run time costs every launch 20 registers).  NCH: chunks per lane (1: rows of up to 8192 columns, 2:
+// up to 16384).
+template <int B, bool XW, int RES, bool NORM, bool MIXED, int NCH>
+__global__ void __launch_bounds__(kMaxLanes) __attribute__((amdgpu_waves_per_eu(waves_per_simd<B, XW, RES, NORM, NCH>())))
+rms_norm_kernel(NormArgs a)
 {
+    static_assert(NORM || (B != 0 && RES == 0), "a quantizer");
     extern __shared__ __align__(16) float gat[];   // gathered inputs: a column's rows side by side
-    __shared__ float4 psum[kMaxLanes / 8], pmax[B ? kMaxLanes / 8 : 1];
+    __shared__ float4 psum[NORM ? kMaxLanes / 8 : 1], pmax[B ? kMaxLanes / 8 : 1];
     const int t = threadIdx.x;
     const int wpu = 8 / a.groups;                   // workgroups per unit
     const int idx = blockIdx.x >> 3;
-    const int64_t ul = (int64_t)(blockIdx.x & 7) + 8 * (int64_t)(idx / wpu);
+    const int ul = (int)(blockIdx.x & 7) + 8 * (idx / wpu);
     if (ul >= a.units) return;
-    const int64_t u = a.unit0 + ul;
+    const int u = a.unit0 + ul;
     const int K = a.K, cpr = K >> 3;
     const int gl = t / a.stride, t0 = t - gl * a.stride;
     const bool glive = gl < a.groups;
     const int s = (idx % wpu) * a.groups + (glive ? gl : 0);
-    const int64_t row0 = u * 32 + 4 * s;
+    const uint32_t row0 = (uint32_t)u * 32 + 4 * s;
     const int lane_c = logical_lane(t0);   // its chunk among the octet's eight
-
-    int64_t row[4];
-    bool rv[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        rv[r] = glive && row0 + r < a.M;
-        row[r] = rv[r] ? row0 + r : 0;
-    }
+    // rows of the four that exist; the others read the first row of all
+    const int rows = glive && row0 < (uint32_t)a.M ? (int)min(4u, (uint32_t)a.M - row0) : 0;
+    auto row_of = [&](int r) { return (int64_t)(r < rows ? row0 + r : 0u); };
     const bool bf16 = a.x_type == MxType::BF16;
 
     // s w of each chunk, and the rows' sums of squares
     float x[NCH][4][8], sq[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     {
-        uint4 v[NCH][4];
+        uint4 v[NCH][4][XW ? 2 : 1];
         uint4 res[NCH][4][RES == 2 ? 2 : 1];
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
             const int at = min(lane_c + i * a.stride, cpr - 1) * 8;
+            // (unconditional, so that all are in flight)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)   // (unconditional, so that all are in flight)
-                v[i][r] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.X) + row[r] * a.ldx + at);
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (XW) {
+                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.X) + row_of(r) * a.ldx + at);
+                    v[i][r][0] = p[0];
+                    v[i][r][1] = p[1];
+                } else {
+                    v[i][r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.X) + row_of(r) * a.ldx + at);
+                }
+            }
             if constexpr (RES == 1) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    res[i][r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.R) + row[r] * a.ldr + at);
+                    res[i][r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.R) + row_of(r) * a.ldr + at);
             } else if constexpr (RES == 2) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.R) + row[r] * a.ldr + at);
+                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.R) + row_of(r) * a.ldr + at);
                     res[i][r][0] = p[0];
                     res[i][r][1] = p[1];
                 }
             }
         }
-        // (rows of one sample share their weights' load)
-        const uint32_t sr = (uint32_t)a.sample_rows, first = (uint32_t)row[0] / sr;
-        const bool one = (uint32_t)min(row[0] + 3, a.M - 1) / sr == first;
+        auto as_floats = [](const uint4 &q, float *f) {
+            f[0] = __uint_as_float(q.x), f[1] = __uint_as_float(q.y), f[2] = __uint_as_float(q.z), f[3] = __uint_as_float(q.w);
+        };
+        const uint32_t sr = (uint32_t)a.sample_rows;
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
             const int chunk = lane_c + i * a.stride, at = min(chunk, cpr - 1) * 8;
             const bool live = chunk < cpr;
             float w[8];
-            if (a.W != nullptr) load8(a.W, (int64_t)first * K + at, a.w_type, w);
+            if constexpr (NORM) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = 1.0f;
+                if (!MIXED && a.W != nullptr) load8(a.W, (int64_t)((uint32_t)row_of(0) / sr) * K + at, a.w_type, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = live ? w[e] : 0.0f;
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float(&y)[8] = x[i][r];
-                widen8(v[i][r], bf16, y);
-                if constexpr (RES == 1) {
+                if constexpr (XW) as_floats(v[i][r][0], y), as_floats(v[i][r][1], y + 4);
+                else widen8(v[i][r][0], bf16, y);
+                if constexpr (RES != 0) {
                     float q[8];
-                    widen8(res[i][r][0], a.r_type == MxType::BF16, q);
+                    if constexpr (RES == 2) as_floats(res[i][r][0], q), as_floats(res[i][r][1], q + 4);
+                    else widen8(res[i][r][0], a.r_type == MxType::BF16, q);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] += q[e];
-                } else if constexpr (RES == 2) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint4 q = res[i][r][h];
-                        y[4 * h] += __uint_as_float(q.x);
-                        y[4 * h + 1] += __uint_as_float(q.y);
-                        y[4 * h + 2] += __uint_as_float(q.z);
-                        y[4 * h + 3] += __uint_as_float(q.w);
-                    }
+                    if (r < rows && live) store8(a.sum, row_of(r) * a.ld_sum + at, RES == 2 ? MxType::F32 : a.r_type, y);
                 }
-                if constexpr (RES != 0)
-                    if (rv[r] && live) store8(a.sum, row[r] * a.ld_sum + at, RES == 2 ? MxType::F32 : a.r_type, y);
-                if (!rv[r] || !live) {
+                if (r >= rows || !live) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] = 0.0f;
                 }
+                if constexpr (NORM) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq[r] = __builtin_fmaf(y[e], y[e], sq[r]);
-                if (a.W != nullptr) {
-                    if (!one && r > 0) load8(a.W, (int64_t)((uint32_t)row[r] / sr) * K + at, a.w_type, w);
+                    for (int e = 0; e < 8; ++e) sq[r] = __builtin_fmaf(y[e], y[e], sq[r]);
+                    if (MIXED && live) load8(a.W, (int64_t)((uint32_t)row_of(r) / sr) * K + at, a.w_type, w);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = (rv[r] && live) ? y[e] * w[e] : 0.0f;
+                    for (int e = 0; e < 8; ++e) y[e] *= w[e];
                 }
             }
         }
@@ -247,11 +259,11 @@ __global__ void __launch_bounds__(kMaxLanes) rms_norm_kernel(NormArgs a)
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        sq[r] = octet(sq[r], add);
+        if constexpr (NORM) sq[r] = octet(sq[r], add);
         if constexpr (B != 0) m[r] = octet(m[r], larger);
     }
     if ((t & 7) == 0) {
-        psum[t >> 3] = make_float4(sq[0], sq[1], sq[2], sq[3]);
+        if constexpr (NORM) psum[t >> 3] = make_float4(sq[0], sq[1], sq[2], sq[3]);
         if constexpr (B != 0) pmax[t >> 3] = make_float4(m[0], m[1], m[2], m[3]);
     }
     __syncthreads();
@@ -259,41 +271,51 @@ __global__ void __launch_bounds__(kMaxLanes) rms_norm_kernel(NormArgs a)
 #pragma unroll
     for (int r = 0; r < 4; ++r) sq[r] = m[r] = 0.0f;
     for (int j = t & 7; j < a.stride >> 3; j += 8) {
-        const float4 p = psum[first + j];
-        sq[0] += p.x, sq[1] += p.y, sq[2] += p.z, sq[3] += p.w;
+        if constexpr (NORM) {
+            const float4 p = psum[first + j];
+            sq[0] += p.x, sq[1] += p.y, sq[2] += p.z, sq[3] += p.w;
+        }
         if constexpr (B != 0) {
             const float4 q = pmax[first + j];
             m[0] = max_nan(m[0], q.x), m[1] = max_nan(m[1], q.y), m[2] = max_nan(m[2], q.z), m[3] = max_nan(m[3], q.w);
         }
     }
-    float inv[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        sq[r] = octet(sq[r], add);
+        if constexpr (NORM) sq[r] = octet(sq[r], add);
         if constexpr (B != 0) m[r] = octet(m[r], larger);
-        inv[r] = 1.0f / sqrtf(sq[r] / (float)K + a.eps);
     }
+    // each lane of a quad works out one of its four rows, the quad shares the results
+    const int mine = t & 3;
+    auto of_mine = [&](const float (&v)[4]) { return mine == 0 ? v[0] : mine == 1 ? v[1] : mine == 2 ? v[2] : v[3]; };
+    const float inv = NORM ? 1.0f / sqrtf(of_mine(sq) / (float)K + a.eps) : 1.0f;
+    auto quad = [](float v, float (&all)[4]) {
+        all[0] = lane_xchg<kQuadLane0>(v), all[1] = lane_xchg<kQuadLane1>(v);
+        all[2] = lane_xchg<kQuadLane2>(v), all[3] = lane_xchg<kQuadLane3>(v);
+    };
 
     if constexpr (B == 0) {
+        float factor[4];
+        quad(inv, factor);
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
             const int chunk = lane_c + i * a.stride;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][r][e] *= inv[r];
-                if (rv[r] && chunk < cpr) store8(a.Y, row[r] * a.ldy + chunk * 8, a.y_type, x[i][r]);
+                for (int e = 0; e < 8; ++e) x[i][r][e] *= factor[r];
+                if (r < rows && chunk < cpr) store8(a.Y, row_of(r) * a.ldy + chunk * 8, a.y_type, x[i][r]);
             }
         }
     } else {
+        // (maxima whose reciprocal would overflow count as zeros: eps keeps the factor finite)
+        float top = of_mine(m);
+        top = top < 0x1p-100f ? 0.0f : top;
+        if (t0 < 4 && mine < rows) a.x_scale[row_of(mine)] = (top / 127.0f) * inv;
         float rs[4];
+        quad(top == 0.0f ? 0.0f : 127.0f / top, rs);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            // (maxima whose reciprocal would overflow count as zeros: eps keeps the factor finite)
-            const float top = m[r] < 0x1p-100f ? 0.0f : m[r];
-            rs[r] = (top == 0.0f ? 0.0f : 127.0f / top) * cs.sign;
-            if (t0 == r && rv[r]) a.x_scale[row[r]] = (top / 127.0f) * inv[r];
-        }
+        for (int r = 0; r < 4; ++r) rs[r] *= cs.sign;
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
             const int chunk = lane_c + i * a.stride;
@@ -304,14 +326,14 @@ __global__ void __launch_bounds__(kMaxLanes) rms_norm_kernel(NormArgs a)
 
 // Four-row groups per workgroup: the most live lanes of whole waves, more groups on a tie, but no
 // more than leaves two workgroups per compute unit to the launch.
-int pick_groups(int stride, int64_t total_groups, int cus) {
+int pick_groups(int stride, int64_t total_groups, int cus, int most_waves) {
     int best = 1;
     double best_u = 0.0;
     for (int g = 1; g <= kMaxGroups && g * stride <= kMaxLanes; g <<= 1) {
         if (g > 1 && g * stride > 64 && total_groups / g < 2 * cus) break;
         const int waves = (g * stride + 63) / 64;
-        if (g > 1 && waves > 8) break;
-        const double u = (double)(g * stride) * (16 / waves);
+        if (g > 1 && waves > most_waves / 2) break;
+        const double u = (double)(g * stride) * (most_waves / waves);
         if (u >= best_u) {
             best_u = u;
             best = g;
@@ -320,7 +342,7 @@ int pick_groups(int stride, int64_t total_groups, int cus) {
     return best;
 }
 
-template <int B, int RES, int NCH>
+template <int B, bool XW, int RES, bool NORM, bool MIXED, int NCH>
 hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
     NormArgs a;
     static_cast<RmsNormArgs &>(a) = args;
@@ -329,7 +351,7 @@ hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
     constexpr int P = NCH == 1 ? 4 : 2;
     if constexpr (NCH == 1) {
         a.stride = (cpr + 7) / 8 * 8;
-        a.groups = pick_groups(a.stride, units * 8, compute_units());
+        a.groups = pick_groups(a.stride, units * 8, compute_units(), 4 * waves_per_simd<B, XW, RES, NORM, NCH>());
         while (B != 0 && a.perm != nullptr && a.groups > 1 && (size_t)a.groups * a.K * P * 4 > kLdsLimit) a.groups >>= 1;
     } else {
         a.groups = 1;
@@ -339,29 +361,41 @@ hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
     const size_t lds = B != 0 && a.perm != nullptr ? (size_t)a.groups * a.K * P * 4 : 0;
     if (T > kMaxLanes || lds > kLdsLimit) return hipErrorInvalidConfiguration;
     if (lds > 65536 - 8192) {
-        hipError_t e = hipFuncSetAttribute((const void *)rms_norm_kernel<B, RES, NCH>,
+        hipError_t e = hipFuncSetAttribute((const void *)rms_norm_kernel<B, XW, RES, NORM, MIXED, NCH>,
                                            hipFuncAttributeMaxDynamicSharedMemorySize, kLdsLimit);
         if (e != hipSuccess) return e;
     }
     // launches of at most 2^31 lanes
     const int64_t per_unit = (int64_t)(8 / a.groups) * T;
     const int64_t most = std::max<int64_t>(8, (((int64_t)1 << 31) / per_unit) / 8 * 8);
-    for (a.unit0 = 0; a.unit0 < units; a.unit0 += most) {
-        a.units = (int)std::min<int64_t>(most, units - a.unit0);
+    for (int64_t u0 = 0; u0 < units; u0 += most) {
+        a.unit0 = (int)u0;
+        a.units = (int)std::min<int64_t>(most, units - u0);
         const int64_t grid = ((int64_t)a.units + 7) / 8 * 8 * (8 / a.groups);
-        hipLaunchKernelGGL((rms_norm_kernel<B, RES, NCH>), dim3((unsigned)grid), dim3(T), lds, stream, a);
+        hipLaunchKernelGGL((rms_norm_kernel<B, XW, RES, NORM, MIXED, NCH>), dim3((unsigned)grid), dim3(T), lds, stream, a);
     }
     return hipGetLastError();
 }
 
-template <int B, int RES>
+template <int B, bool XW, int RES, bool NORM>
 hipError_t launch_width(const RmsNormArgs &a, hipStream_t stream) {
-    return a.K <= 8 * kMaxLanes ? launch_norm<B, RES, 1>(a, stream) : launch_norm<B, RES, 2>(a, stream);
+    if constexpr (NORM)
+        if (a.W != nullptr && a.sample_rows < a.M && a.sample_rows % 4 != 0)
+            return a.K <= 8 * kMaxLanes ? launch_norm<B, XW, RES, NORM, true, 1>(a, stream)
+                                        : launch_norm<B, XW, RES, NORM, true, 2>(a, stream);
+    return a.K <= 8 * kMaxLanes ? launch_norm<B, XW, RES, NORM, false, 1>(a, stream)
+                                : launch_norm<B, XW, RES, NORM, false, 2>(a, stream);
+}
+template <int B, bool XW>
+hipError_t launch_residual(const RmsNormArgs &a, hipStream_t stream) {
+    if constexpr (B != 0)
+        if (!a.norm) return launch_width<B, XW, 0, false>(a, stream);
+    if (a.R == nullptr) return launch_width<B, XW, 0, true>(a, stream);
+    return a.r_type == MxType::F32 ? launch_width<B, XW, 2, true>(a, stream) : launch_width<B, XW, 1, true>(a, stream);
 }
 template <int B>
-hipError_t launch_residual(const RmsNormArgs &a, hipStream_t stream) {
-    if (a.R == nullptr) return launch_width<B, 0>(a, stream);
-    return a.r_type == MxType::F32 ? launch_width<B, 2>(a, stream) : launch_width<B, 1>(a, stream);
+hipError_t launch_type(const RmsNormArgs &a, hipStream_t stream) {
+    return a.x_type == MxType::F32 ? launch_residual<B, true>(a, stream) : launch_residual<B, false>(a, stream);
 }
 
 // One 16-byte operand piece (16 codes of a row) per thread: four threads write a row's 64 codes, sixteen
@@ -391,11 +425,11 @@ __global__ void dequantize_act8_kernel(const uint8_t *__restrict__ q8, const flo
 }  // namespace
 
 hipError_t launch_rms_norm(const RmsNormArgs &a, hipStream_t stream) {
-    if (a.Y != nullptr) return launch_residual<0>(a, stream);
+    if (a.Y != nullptr) return launch_type<0>(a, stream);
     switch (a.block) {
-        case 32: return launch_residual<32>(a, stream);
-        case 64: return launch_residual<64>(a, stream);
-        case 128: return launch_residual<128>(a, stream);
+        case 32: return launch_type<32>(a, stream);
+        case 64: return launch_type<64>(a, stream);
+        case 128: return launch_type<128>(a, stream);
     }
     return hipErrorInvalidValue;
 }

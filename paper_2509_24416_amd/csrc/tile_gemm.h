@@ -151,17 +151,23 @@ struct Args {
     double *errp;
     int nc;
     int64_t wq_stride, ws_stride, p_stride;
-    // activating epilogue (Epi::F16 and on): residual of the output's type, gate by sample
+    // activating epilogue: residual of the output's type, gate by sample
     const void *gate, *res;
     int64_t ldr;
-    int act, sample_rows;
+    int sample_rows;
     bool res_vec;   // the residual's rows are 16-byte aligned
     MxType bias_type, gate_type;
 };
 
-// What is done with the sums: the epilogue of the entry points without activation, or activation, gate
-// and residual with the result in one of three types.
-enum class Epi { Plain, F16, BF16, F32 };
+// What is done with the sums, as a policy of the kernels.  PlainEpi: the epilogue of the entry points without
+// activation, spelt out in them.  Others (act_epilogue.h): kActs, turn bytes of a wave, and
+//   Operands<BN, BM>  load(a, tm, tn, tid) ahead of the k loop, store(a, ep, tid) behind it
+//   finish_tile, finish_split  of a wave's fragments.
+struct PlainEpi {
+    static constexpr bool kActs = false;
+    static constexpr int kTurnBytes = 0;
+    template <int BN, int BM> static constexpr int kOperands = 2 * BN + BM;
+};
 
 // a stage's operands of one wave: 4 channel units, 2 token units.  read: from
 // the units' LDS addresses (wa, xa: of lane 0's bytes); wait<VM>: at most VM
@@ -360,80 +366,6 @@ __device__ __forceinline__ void store_fragment(const Args &a, const Acc<F> &x, c
     }
 }
 
-// The tanh form of GELU and SiLU with the hardware's exp2 and reciprocal (1 ulp each): h / (1 + 2^t).
-// Relative errors under 6e-7 for h > -2; below, exp2 scales up its argument's rounding with the argument
-// (1e-5 at -10, where GELU is -1e-37 and SiLU's error 1e-6); absolute errors for negative h under 1e-7.
-__device__ __forceinline__ float activated(float h, int act) {
-    if (act == (int)Act8::None) return h;
-    const float t = act == (int)Act8::Gelu ? h * __builtin_fmaf(-0.10294324f, h * h, -2.3022082f) : h * -1.4426950408889634f;
-    return h * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
-}
-
-// store_fragment with activation, gate and residual.
-template <Fmt F, int BN, Epi E>
-__device__ __forceinline__ void store_activated(const Args &a, const Acc<F> &x, const float *ep, int c0, int r0, int n0,
-                                                int m) {
-    if (m >= a.M || n0 >= a.N) return;
-    constexpr MxType T = E == Epi::F16 ? MxType::F16 : E == Epi::BF16 ? MxType::BF16 : MxType::F32;
-    const float xsc = ep[2 * BN + r0] * (1.0f / (float)(1 << FmtInfo<F>::LOG));
-    float y[2][8];
-#pragma unroll
-    for (int v = 0; v < 16; ++v)
-        y[v >> 3][v & 7] = activated(__builtin_fmaf((float)x[v] * xsc, ep[c0 + v], ep[BN + c0 + v]), a.act);
-    const bool whole = n0 <= a.N - 16;
-    if (a.gate != nullptr) {
-        const int64_t at = (int64_t)((uint32_t)m / (uint32_t)a.sample_rows) * a.N + n0;
-        if (whole && a.N % 8 == 0) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float g[8];
-                load8(a.gate, at + 8 * h, a.gate_type, g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[h][e] *= g[e];
-            }
-        } else {
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-                if (n0 + v < a.N)
-                    y[v >> 3][v & 7] *= a.gate_type == MxType::F32
-                                            ? static_cast<const float *>(a.gate)[at + v]
-                                            : clq::widen16(static_cast<const uint16_t *>(a.gate)[at + v], a.gate_type == MxType::BF16);
-        }
-    }
-    if (a.res != nullptr) {
-        const int64_t at = (int64_t)m * a.ldr + n0;
-        if (whole && a.res_vec) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float r[8];
-                load8(a.res, at + 8 * h, T, r);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[h][e] += r[e];
-            }
-        } else {
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-                if (n0 + v < a.N) {
-                    if constexpr (T == MxType::F32) y[v >> 3][v & 7] += static_cast<const float *>(a.res)[at + v];
-                    else y[v >> 3][v & 7] += clq::widen16(static_cast<const uint16_t *>(a.res)[at + v], T == MxType::BF16);
-                }
-        }
-    }
-    const int64_t at = (int64_t)m * a.ldy + n0;
-    if (whole) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) store8(a.Y, at + 8 * h, T, y[h]);
-    } else {
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-            if (n0 + v < a.N) {
-                const float s = y[v >> 3][v & 7];
-                if constexpr (T == MxType::F32) static_cast<float *>(a.Y)[at + v] = s;
-                else static_cast<uint16_t *>(a.Y)[at + v] = (uint16_t)narrow2(s, s, T == MxType::BF16);
-            }
-    }
-}
-
 // Tile number of this workgroup: workgroups are dealt to the 8 XCDs
 // round-robin, and each XCD takes a contiguous run.
 __device__ __forceinline__ int tile_of_block() {
@@ -482,47 +414,24 @@ struct EpilogueOperands {
     }
 };
 
-// The same for the activating epilogue: biases of either 16-bit type or none, at run time.
-template <int BN, int BM, int NT>
-struct ActivatedOperands {
-    static constexpr int EPN = 2 * BN + BM, EPR = (EPN + NT - 1) / NT;
-    float v[EPR];
-    uint16_t b[EPR];
-    __device__ __forceinline__ void load(const Args &a, int tm, int tn, int tid) {
-#pragma unroll
-        for (int r = 0; r < EPR; ++r) {
-            const int e = min(tid + r * NT, EPN - 1);
-            const int ec = min(tn * BN + (e & (BN - 1)), a.N - 1), er = min(tm * BM + max(e - 2 * BN, 0), a.M - 1);
-            const float *p = e < 2 * BN ? a.ws + ec : a.xs + er;
-            v[r] = *p;
-            // (without a bias: some value of the scales, not used)
-            const uint16_t *q = a.bias != nullptr ? a.bias + ec : reinterpret_cast<const uint16_t *>(a.ws) + ec;
-            b[r] = *q;
-        }
-    }
-    __device__ __forceinline__ void store(const Args &a, float *ep, int tid) const {
-#pragma unroll
-        for (int r = 0; r < EPR; ++r) {
-            const int e = min(tid + r * NT, EPN - 1);
-            const float bias = a.bias != nullptr ? clq::widen16(b[r], a.bias_type == MxType::BF16) : 0.0f;
-            ep[e] = e >= BN && e < 2 * BN ? bias : v[r];
-        }
-    }
-};
+template <class E, int BN, int BM, int NT, bool BIAS>
+struct EpilogueOf { using type = typename E::template Operands<BN, BM>; };
+template <int BN, int BM, int NT, bool BIAS>
+struct EpilogueOf<PlainEpi, BN, BM, NT, BIAS> { using type = EpilogueOperands<BN, BM, NT, BIAS>; };
 
 // ERR: nothing is stored; the epilogue sums (Y0 - sum * x_scale * w_scale)^2
 // over the tile in fp64 (the integer sum exact) and keeps one partial per wave.
 // A target tile's candidates are neighbours in the tile order, so that one
 // XCD's L2 serves the target and the activation panel to all of them.
-template <class C, bool I32OUT, bool RAGGED, bool BIAS, bool ERR = false, Epi E = Epi::Plain>
+template <class C, bool I32OUT, bool RAGGED, bool BIAS, bool ERR = false, class E = PlainEpi>
 __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
 {
     static_assert(!(I32OUT && BIAS), "no bias on the integer output");
     static_assert(!ERR || (!I32OUT && !BIAS), "the error mode has no output and no bias");
     constexpr Fmt F = C::fmt;
     constexpr int NS = C::NS;
-    __shared__ __align__(16) uint8_t pool[C::POOL];
-    __shared__ float ep[C::EPN];   // channel scales, biases (fp16 widened), token scales
+    __shared__ __align__(16) uint8_t pool[C::POOL > C::WM * E::kTurnBytes ? C::POOL : C::WM * E::kTurnBytes];
+    __shared__ __align__(16) float ep[E::template kOperands<C::BN, C::BM>];   // channel scales, biases, token scales
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int M = a.M, N = a.N, nks = a.K >> 6;
@@ -599,8 +508,7 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
     // ---- epilogue operands: loaded ahead of the transfers, held in registers
     // through the k loop, written to LDS after it (an LDS store while transfers
     // into LDS are in flight would wait for all of them)
-    std::conditional_t<E == Epi::Plain, EpilogueOperands<C::BN, C::BM, C::NT, BIAS>,
-                       ActivatedOperands<C::BN, C::BM, C::NT>> eo;
+    typename EpilogueOf<E, C::BN, C::BM, C::NT, BIAS>::type eo;
     if constexpr (!I32OUT) eo.load(a, tm, tn, tid);
     __builtin_amdgcn_sched_barrier(0);
 
@@ -653,11 +561,15 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
     op[0].template wait<0>();
     op[1].template wait<0>();
     if constexpr (!I32OUT) {
-        if constexpr (E == Epi::Plain) eo.store(ep, tid);
-        else eo.store(a, ep, tid);
+        if constexpr (E::kActs) eo.store(a, ep, tid);
+        else eo.store(ep, tid);
         __syncthreads();
     }
 
+    if constexpr (E::kActs) {
+        E::template finish_tile<F, 4>(a, acc, pool + wave * E::kTurnBytes, ep, C::BM, tm, tn, wave, lane);
+        return;
+    }
     // ---- epilogue: lane owns token m and 16 consecutive channels ----------------
     const int h16 = (lane >> 5) * 16;
     if constexpr (ERR) {
@@ -709,9 +621,7 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
         static_for<0, C::FM>([&](auto mc) {
             constexpr int fn = decltype(fc)::value, fm = decltype(mc)::value;
             const int c0 = fn * 32 + h16, r0 = (wave * C::FM + fm) * 32 + (lane & 31);
-            if constexpr (E == Epi::Plain)
-                store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
-            else store_activated<F, C::BN, E>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
+            store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
         });
     });
 }
@@ -736,14 +646,15 @@ struct SplitCfg {
     static_assert(KS == 2 || KS == 4, "recursive halving over 8 fragments");
 };
 
-template <class C, bool I32OUT, bool RAGGED, bool BIAS, Epi E = Epi::Plain>
+template <class C, bool I32OUT, bool RAGGED, bool BIAS, class E = PlainEpi>
 __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
 {
     static_assert(!(I32OUT && BIAS), "no bias on the integer output");
     constexpr Fmt F = C::fmt;
     constexpr int KS = C::KS, D = C::kDepth;
-    __shared__ __align__(16) uint8_t exch[KS * 16384];   // a step: 16 KB a wave at most
-    __shared__ float ep[C::EPN];
+    constexpr int kSlot = 16384 > E::kTurnBytes ? 16384 : E::kTurnBytes;   // a step: 16 KB a wave at most
+    __shared__ __align__(16) uint8_t exch[KS * kSlot];
+    __shared__ __align__(16) float ep[E::template kOperands<C::BN, C::BM>];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nks = a.K >> 6;
@@ -757,8 +668,7 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
 #pragma unroll
     for (int f = 0; f < 2; ++f) xs[f] = a.Xq + (int64_t)min(tm * 2 + f, xunits - 1) * nks * C::XU;
 
-    std::conditional_t<E == Epi::Plain, EpilogueOperands<C::BN, C::BM, C::NT, BIAS>,
-                       ActivatedOperands<C::BN, C::BM, C::NT>> eo;
+    typename EpilogueOf<E, C::BN, C::BM, C::NT, BIAS>::type eo;
     if constexpr (!I32OUT) eo.load(a, tm, tn, tid);
     __builtin_amdgcn_sched_barrier(0);
 
@@ -797,14 +707,14 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
         if (rest > 1) mma(IC<1>{});
 
     if constexpr (!I32OUT) {   // (the exchange's barriers publish it)
-        if constexpr (E == Epi::Plain) eo.store(ep, tid);
-        else eo.store(a, ep, tid);
+        if constexpr (E::kActs) eo.store(a, ep, tid);
+        else eo.store(ep, tid);
     }
 
     // one step's messages: fragments [fn0, fn0 + nf) x [fm0, fm0 + mf)
     using V4 = std::conditional_t<F == Fmt::F6, v4f, v4i>;
     auto send = [&](auto fn0, auto nf, auto fm0, auto mf, int to) __attribute__((always_inline)) {
-        V4 *out = reinterpret_cast<V4 *>(exch + to * 16384) + lane;
+        V4 *out = reinterpret_cast<V4 *>(exch + to * kSlot) + lane;
         static_for<0, decltype(nf)::value>([&](auto i) {
             static_for<0, decltype(mf)::value>([&](auto j) {
                 const Acc<F> &x = acc[decltype(fn0)::value + decltype(i)::value][decltype(fm0)::value + decltype(j)::value];
@@ -816,7 +726,7 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
         });
     };
     auto receive = [&](auto fn0, auto nf, auto fm0, auto mf) __attribute__((always_inline)) {
-        const V4 *in = reinterpret_cast<const V4 *>(exch + wave * 16384) + lane;
+        const V4 *in = reinterpret_cast<const V4 *>(exch + wave * kSlot) + lane;
         static_for<0, decltype(nf)::value>([&](auto i) {
             static_for<0, decltype(mf)::value>([&](auto j) {
                 Acc<F> &x = acc[decltype(fn0)::value + decltype(i)::value][decltype(fm0)::value + decltype(j)::value];
@@ -832,14 +742,17 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
     const int h16 = (lane >> 5) * 16;
     // the wave's summed fragments [fn0, fn0 + nf) x [fm0, fm0 + mf)
     auto finish = [&](auto fn0, auto nf, auto fm0, auto mf) __attribute__((always_inline)) {
+        if constexpr (E::kActs) {
+            E::template finish_unit<F, decltype(fn0)::value, decltype(nf)::value, decltype(fm0)::value>(
+                a, acc, exch + wave * kSlot, ep, C::BM, tm, tn, decltype(fm0)::value * 32, lane);
+            return;
+        }
         static_for<0, decltype(nf)::value>([&](auto i) {
             static_for<0, decltype(mf)::value>([&](auto j) {
                 constexpr int fn = decltype(fn0)::value + decltype(i)::value, fm = decltype(fm0)::value + decltype(j)::value;
                 const int c0 = fn * 32 + h16, r0 = fm * 32 + (lane & 31);
-                if constexpr (E == Epi::Plain)
-                    store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0,
-                                                                  tm * C::BM + r0);
-                else store_activated<F, C::BN, E>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0, tm * C::BM + r0);
+                store_fragment<F, C::BN, I32OUT, RAGGED, BIAS>(a, acc[fn][fm], ep, c0, r0, tn * C::BN + c0,
+                                                              tm * C::BM + r0);
             });
         });
     };

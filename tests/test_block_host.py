@@ -42,7 +42,7 @@ def norm8(X=A, xt=0, ldx=1152, R=None, rt=0, ldr=1152, W=None, wt=0, samples=1, 
     return L.clq_rms_norm_act8(X, xt, ldx, R, rt, ldr, W, wt, samples, eps, perm, M, K, block, q, xs, S, lds, None)
 
 
-COMMON = [(dict(X=None), NULL), (dict(R=A), NULL), (dict(S=A), NULL), (dict(xt=2), ARG), (dict(xt=-1), ARG),
+COMMON = [(dict(X=None), NULL), (dict(R=A), NULL), (dict(S=A), NULL), (dict(xt=3), ARG), (dict(xt=-1), ARG),
           (dict(R=A, S=A, rt=3), ARG), (dict(W=A, wt=5), ARG), (dict(eps=0.0), ARG), (dict(eps=-1.0), ARG),
           (dict(eps=math.inf), ARG), (dict(eps=math.nan), ARG), (dict(M=0), SHAPE), (dict(M=2 ** 31), SHAPE),
           (dict(samples=2), SHAPE), (dict(W=A, samples=3), SHAPE), (dict(W=A, samples=8), SHAPE), (dict(W=A, samples=0), SHAPE),
@@ -62,6 +62,17 @@ def test_norm_refusals(kw, want):
                                      (dict(q=MIS), ALIGN), (dict(xs=MIS), ALIGN), (dict(perm=MIS), ALIGN)])
 def test_norm_act8_refusals(kw, want):
     assert norm8(**kw) == want
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(X=None), NULL), (dict(q=None), NULL), (dict(xs=None), NULL), (dict(t=3), ARG), (dict(M=0), SHAPE), (dict(K=72, ldx=72), SHAPE),
+    (dict(K=16448, ldx=16448), SHAPE), (dict(ldx=1148), SHAPE), (dict(block=0), BLOCK), (dict(K=192, ldx=192, block=128), BLOCK),
+    (dict(X=MIS), ALIGN), (dict(q=MIS), ALIGN), (dict(xs=MIS), ALIGN), (dict(perm=MIS), ALIGN)])
+def test_quantize_act8_refusals(kw, want):
+    def call(X=A, t=0, ldx=1152, perm=None, M=4, K=1152, block=64, q=A, xs=A):
+        return L.clq_quantize_act8(X, t, ldx, perm, M, K, block, q, xs, None)
+
+    assert call(**kw) == want
 
 
 @pytest.mark.parametrize("kw,want", [

@@ -78,7 +78,7 @@ NORM = 28 * U
 @pytest.mark.parametrize("M,K,xt,rt,wt,samples", [
     (1, 64, F16, None, None, 1), (1, 1152, F16, F16, F16, 1), (2, 8, BF16, None, F32, 2), (3, 72, F16, F32, F16, 3),
     (31, 1160, BF16, BF16, BF16, 1), (33, 520, F16, BF16, F32, 3), (100, 4096, BF16, None, F16, 2), (6, 8192, F16, F32, BF16, 2),
-    (5, 8200, BF16, F16, F16, 1), (3, 16384, F16, BF16, None, 1), (70, 16376, BF16, F32, F32, 7), (1030, 136, F16, F16, F16, 2)])
+    (5, 8200, BF16, F16, F16, 1), (9, 1152, F32, F32, F32, 3), (64, 200, F32, F16, None, 1), (12, 9216, F32, None, BF16, 2), (3, 16384, F16, BF16, None, 1), (70, 16376, BF16, F32, F32, 7), (1030, 136, F16, F16, F16, 2)])
 def test_norm(clq, M, K, xt, rt, wt, samples):
     g = gen(M * K)
     x = strided(randn(g, M, K, dtype=xt, scale=3))
@@ -149,7 +149,8 @@ def check_codes(clq, q, xs, n, perm, block, K, what=""):
 @pytest.mark.parametrize("M,K,block,xt,rt,wt,samples,perm", [
     (1, 64, 64, F16, None, None, 1, False), (1, 1152, 64, F16, F16, F16, 1, False), (2, 1152, 128, BF16, F32, F32, 2, True),
     (45, 1216, 32, BF16, F32, BF16, 1, True), (33, 64, 32, F16, BF16, F16, 3, True), (600, 4096, 128, BF16, None, F16, 2, False),
-    (9, 8192, 64, F16, F32, F16, 1, True), (5, 8256, 64, F16, F16, F16, 5, True), (40, 12288, 128, BF16, BF16, None, 1, False),
+    (9, 8192, 64, F16, F32, F16, 1, True), (66, 1152, 64, F32, F32, F32, 6, True), (40, 320, 32, F32, F16, F16, 10, False),
+    (33, 8320, 128, F32, None, F32, 3, False), (5, 8256, 64, F16, F16, F16, 5, True), (40, 12288, 128, BF16, BF16, None, 1, False),
     (3, 16384, 32, F16, F32, F32, 1, True), (2049, 320, 64, F16, F16, F16, 1, True), (1030, 2048, 32, BF16, None, None, 1, False)])
 def test_norm_act8(clq, M, K, block, xt, rt, wt, samples, perm):
     g = gen(M + K)
@@ -174,6 +175,32 @@ def test_norm_act8(clq, M, K, block, xt, rt, wt, samples, perm):
         close(d, codes * xs.double().unsqueeze(1), codes.abs() * xs.double().unsqueeze(1) * U, f"dequantized to {t}")
     q2, xs2 = clq.clq_rms_norm_act8(x, block, w, r, EPS, perm=p, out=torch.full_like(q, 77), scale_out=torch.empty_like(xs))[:2]
     assert torch.equal(q2, q) and torch.equal(xs2, xs)
+
+
+@pytest.mark.parametrize("perm", [False, True])
+@pytest.mark.parametrize("M,K,block", [(1, 64, 64), (1, 4608, 64), (45, 1216, 32), (600, 1152, 128), (70, 8192, 32), (40, 12288, 64)])
+def test_quantizer(clq, M, K, block, perm):
+    """fp16: bit for bit clq_rotate_quant_act8.  bf16 and fp32: the values' exact rotation within the roundings of
+    its stages."""
+    g = gen(M + K)
+    p = torch.randperm(K, device="cuda", generator=g).to(torch.int32) if perm else None
+    x = strided(randn(g, M, K, dtype=F16, scale=3))
+    q, xs = clq.clq_quantize_act8(x, block, p)
+    want, scales = clq.clq_rotate_quant_act8(x.contiguous(), block, p)
+    assert torch.equal(q, want) and torch.equal(xs, scales)
+    for t in (BF16, F32):
+        x = strided(randn(g, M, K, dtype=t, scale=3))
+        x[0] = 0
+        q, xs = clq.clq_quantize_act8(x, block, p)
+        assert xs[0] == 0 and (clq.clq_unswizzle_act8(q, M, K)[0] == 0).all()
+        check_codes(clq, q, xs, x.double(), p, block, K, str(t))
+        rows = (M + 31) // 32 * 32
+        assert (clq.clq_unswizzle_act8(q, rows, K)[M:] == 0).all()
+        q2, xs2 = clq.clq_quantize_act8(x, block, p, out=torch.full_like(q, 5), scale_out=torch.empty_like(xs))
+        assert torch.equal(q2, q) and torch.equal(xs2, xs)
+    x = randn(g, M, K)
+    x[M - 1, 3] = math.nan
+    assert clq.clq_quantize_act8(x, block)[1][M - 1].isnan()
 
 
 def test_norm_of_zeros_infinities_and_nans(clq):
@@ -397,8 +424,8 @@ def test_linear_act_far_from_zero(clq):
 
 def mlp(clq, x, r, n, w1, b1, w2, b2, gate):
     q, xs, s = clq.clq_rms_norm_act8(x, 64, n, r)
-    h = clq.clq_a8_linear_act(q, xs, w1, b1, act="gelu")
-    q, xs = clq.clq_rotate_quant_act8(h, 64)
+    h = clq.clq_a8_linear_act(q, xs, w1, b1, act="gelu", dtype=F32)
+    q, xs = clq.clq_quantize_act8(h, 64)
     return clq.clq_a8_linear_act(q, xs, w2, b2, gate=gate, residual=s), s
 
 
@@ -438,8 +465,9 @@ def test_a_block_step_by_step(clq):
         return (clq.clq_unswizzle_act8(q, M, qw.K).double() @ clq.clq_unswizzle_weights8(qw).double().t()) * \
             xs.double().unsqueeze(1) * qw.w_scale.double()
 
-    h = check_linear(clq, q, xs, w1, product(q, xs, w1), b1, "gelu", None, None, F16)
-    q, xs = clq.clq_rotate_quant_act8(h, 64)
+    h = check_linear(clq, q, xs, w1, product(q, xs, w1), b1, "gelu", None, None, F32)
+    q, xs = clq.clq_quantize_act8(h, 64)
+    check_codes(clq, q, xs, h.double(), None, 64, h.shape[1])
     last = check_linear(clq, q, xs, w2, product(q, xs, w2), b2, None, gate, s, F16, gate_tensor=gate)
     assert torch.equal(last, y)
     qkv = attention_inputs(clq, y, w, b, pos, freqs, axes, heads, hw)
@@ -507,7 +535,7 @@ def test_binding_refusals(clq):
     r = randn(g, 8, 128)
     flat = torch.empty(4096, dtype=F16, device="cuda")
     with pytest.raises(TypeError, match="X"):
-        clq.clq_rms_norm(r)
+        clq.clq_rms_norm(r.double())
     for bad, kw in (("weight", dict(weight=wide[0, :64])), ("samples", dict(weight=wide[:3])), ("residual", dict(residual=r[:4])),
                     ("without a residual", dict(sum_out=r)), ("sum_out", dict(residual=r, sum_out=r[:4])),
                     ("overlaps", dict(out=wide[4:12], residual=wide[8:])), ("overlaps", dict(residual=wide[:8], sum_out=wide[4:12])),
