@@ -31,7 +31,7 @@ extern "C" {
  *   R        the residual stream, fp16, bf16 or fp32 [M][K], row stride ldr; NULL: none (then sum is
  *            NULL too).
  *   W        fp16, bf16 or fp32 [samples][K], contiguous; NULL: ones (samples 1).
- *   eps      finite, > 0.
+ *   eps      finite, 2^-126 at least.
  *   sum      out, s rounded to R's type, row stride ld_sum; may be R, in place.  The norm is that of s
  *            before this rounding.
  * A row that holds a NaN or an infinity gives NaN where s / infinity is one and, in the 8-bit form, a
@@ -74,7 +74,7 @@ clq_status clq_dequantize_act8(const void *Xq8, const float *x_scale, int64_t M,
  *   interleaved  1: pair i is columns 2i, 2i + 1; 0: columns i, i + P.
  *   inverse  1: by the opposite angle (the transpose).
  *   W        NULL, or fp16, bf16 or fp32 weights of an RMS norm of each head (all D columns) ahead of the
- *            turn, [D] (weight_heads 1) or [heads][D] (weight_heads = heads), contiguous; eps finite, > 0.
+ *            turn, [D] (weight_heads 1) or [heads][D] (weight_heads = heads), contiguous; eps as for the norm.
  *   Y        out, X's type, strides ldy and lhy, no value of it in two places of the head's rows; may be X,
  *            in place. */
 clq_status clq_rope_axes(const void *X, clq_type type, int64_t ldx, int64_t lhx, const void *positions,
@@ -85,7 +85,8 @@ clq_status clq_rope_axes(const void *X, clq_type type, int64_t ldx, int64_t lhx,
 
 /* ---- 8-bit linear with epilogue ----------------------------------------------------------
  *   Y = R + gate[sample] * act(dequant(Xq8 . Wq^T) + bias)
- * on the operands of clq_a8_linear (wbits 4 or 8, 64 <= K <= 32768, K % 64 == 0).
+ * on the operands of clq_a8_linear (wbits 4 or 8, 64 <= K <= 32768, K % 64 == 0; fewer than 2^24 tiles of
+ * 256 tokens x 128 channels).
  *   bias     fp16 or bf16 [N], or NULL.
  *   act      CLQ_ACT_NONE, CLQ_ACT_GELU (tanh form) or CLQ_ACT_SILU; ARG for CLQ_ACT_SWIGLU.
  *   gate     fp16, bf16 or fp32 [samples][N], contiguous, or NULL (samples 1).

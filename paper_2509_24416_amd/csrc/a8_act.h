@@ -1,12 +1,11 @@
 // Launches of the 8-bit linear with activation, gate and residual, for one output type (each type is a source
-// file of its own, so that they compile side by side).  The kernels are tile_gemm.h's behind
-// act_epilogue.h's epilogue; the rule that picks one is the same.
+// file of its own, so that they compile side by side).
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-#include <stdlib.h>
 
+#include "a8_rows.h"
 #include "a8_tile.h"
 #include "act_epilogue.h"
 #include "block.h"
@@ -16,14 +15,6 @@
 namespace clq {
 namespace {
 
-template <class C, class E>
-hipError_t launch_act_tile(tg::Args a, hipStream_t stream) {
-    a.tiles_m = (int)tg::tile_count(a.M, C::BM);
-    a.tiles_n = (int)tg::tile_count(a.N, C::BN);
-    hipLaunchKernelGGL((tg::tile_gemm_kernel<C, false, false, true, false, E>), dim3((unsigned)(a.tiles_m * a.tiles_n)),
-                       dim3(C::NT), 0, stream, a);
-    return hipGetLastError();
-}
 template <class C, class E>
 hipError_t launch_act_split(tg::Args a, hipStream_t stream) {
     a.tiles_m = (int)tg::tile_count(a.M, C::BM);
@@ -41,30 +32,41 @@ hipError_t launch_act_direct(tg::Args a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <tg::Fmt F, class E>
+template <tg::Fmt F, Act8 A, MxType T>
+hipError_t launch_act_rows(tg::Args a, hipStream_t stream) {
+    a.tiles_m = (int)tg::tile_count(a.M, 32);
+    a.tiles_n = (int)tg::tile_count(a.N, 32);
+    hipLaunchKernelGGL((a8::a8_rows_kernel<F, A, T>), dim3((unsigned)(a.tiles_m * a.tiles_n)), dim3(a8::kRowWaves * 64), 0,
+                       stream, a);
+    return hipGetLastError();
+}
+
+// The kernel of a shape, c compute units (us: 8-bit weights, GELU, replayed from a graph):
+//   few tiles of 32 x 32     the rows kernel up to 2 c of them (one token x 4608 -> 1152 5.7, on 64 x 128 tiles with
+//                            the k loop over four waves 10.8; 300 x 1152 -> 1152, 1.4 c, 6.3 / 7.8; 128 x 1152 -> 4608,
+//                            2.25 c, 8.2 / 7.8);
+//   t = M / 64 x N / 128     k over four waves up to t = 2 c, where they have a stage each (3072 x 4608 -> 1152,
+//   (rounded up)             1.7 c, 26.1, 96-channel tiles 27.8; 4096 x 4608 -> 1152, 2.25 c, 37.7 / 31.5);
+//   otherwise                256-token tiles, of 96 channels where these are resident at once and no more to a
+//                            compute unit than those of 128 (8192 x 4608 -> 1152: 384 and 288 of them, two a unit,
+//                            51.8 / 57.8; 12000 x 4608 -> 1152: 564 and 423, 77.5 / 65.8; 6144: 288 and 216, 48.0 /
+//                            38.4).
+// Tiles of 128 tokens and the k loop over two waves won nowhere by more than 3%.
+template <tg::Fmt F, Act8 A, MxType T>
 hipError_t launch_act_shape(const tg::Args &a, hipStream_t stream) {
-    if (const char *v = getenv("CLQ_V")) switch (atoi(v)) {
-        case 1: return launch_act_direct<F, 4, 4, E>(a, stream);
-        case 2: return launch_act_direct<F, 2, 4, E>(a, stream);
-        case 3: return launch_act_direct<F, 4, 3, E>(a, stream);
-        case 4: return launch_act_direct<F, 2, 3, E>(a, stream);
-        case 5: return launch_act_split<tg::SplitCfg<F, 4>, E>(a, stream);
-        case 6: return launch_act_split<tg::SplitCfg<F, 2>, E>(a, stream);
-    }
-    switch (tg::pick_variant<F>(a.M, a.N, a.K, compute_units())) {
-        case tg::kTile256: return launch_act_direct<F, 4, 4, E>(a, stream);
-        case tg::kTile128: return launch_act_direct<F, 2, 4, E>(a, stream);
-        case tg::kSplit4: return launch_act_split<tg::SplitCfg<F, 4>, E>(a, stream);
-        case tg::kSplit2: return launch_act_split<tg::SplitCfg<F, 2>, E>(a, stream);
-        case tg::kVariants: break;
-    }
-    return hipErrorInvalidValue;
+    using E = ActEpi<A, T>;
+    const int64_t c = compute_units(), M = a.M, N = a.N;
+    if (tg::tile_count(M, 32) * tg::tile_count(N, 32) <= 2 * c) return launch_act_rows<F, A, T>(a, stream);
+    if (tg::tile_count(M, 64) * tg::tile_count(N, 128) <= 2 * c && (a.K >> 6) >= tg::SplitCfg<F, 4>::KS)
+        return launch_act_split<tg::SplitCfg<F, 4>, E>(a, stream);
+    const int64_t t128 = tg::tile_count(M, 256) * tg::tile_count(N, 128), t96 = tg::tile_count(M, 256) * tg::tile_count(N, 96);
+    if (t96 <= 2 * c && (t96 + c - 1) / c <= (t128 + c - 1) / c) return launch_act_direct<F, 4, 3, E>(a, stream);
+    return launch_act_direct<F, 4, 4, E>(a, stream);
 }
 
 template <Act8 A, MxType T>
 hipError_t launch_act_format(const tg::Args &a, int wbits, hipStream_t stream) {
-    return wbits == 4 ? launch_act_shape<tg::Fmt::W4A8, ActEpi<A, T>>(a, stream)
-                      : launch_act_shape<tg::Fmt::W8A8, ActEpi<A, T>>(a, stream);
+    return wbits == 4 ? launch_act_shape<tg::Fmt::W4A8, A, T>(a, stream) : launch_act_shape<tg::Fmt::W8A8, A, T>(a, stream);
 }
 
 template <MxType T>

@@ -74,7 +74,7 @@ template <Fmt F, int NW, int FN, class E>
 __global__ void __launch_bounds__(NW * 64, 2) a8_tile_kernel(tg::Args a)
 {
     static_assert(F == Fmt::W4A8 || F == Fmt::W8A8, "8-bit activations");
-    static_assert(NW == 2 || NW == 4, "a stage's four pieces split evenly");
+    static_assert(NW == 4, "a piece of a stage each");
     constexpr int NS = kStages, PPW = 4 / NW, BN = 32 * FN, BM = 64 * NW;
     constexpr int H = F == Fmt::W4A8 ? 2 : 1;             // matrix instructions a fragment and stage
     constexpr int FETCH = PPW + 2 * H;                    // transfers and loads of a wave and stage
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(NW * 64, 2) a8_tile_kernel(tg::Args a)
         if constexpr (Q < kDepth) load_x(qc, Q);
         __builtin_amdgcn_sched_barrier(0);
     });
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 1) * PPW + kDepth * 2 * H - 2 * H) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 1) * PPW + (kDepth - 1) * 2 * H) : "memory");
     tg::Acc<F> acc[FN][2];
     static_for<0, FN>([&](auto fn) {
         static_for<0, 2>([&](auto fm) { acc[decltype(fn)::value][decltype(fm)::value] = tg::Acc<F>{}; });

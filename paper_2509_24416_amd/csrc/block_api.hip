@@ -1,6 +1,7 @@
 // C ABI of the operators around the 8-bit linears (clq_block.h): host-side checks and
 // launches, as in clq_api.hip.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -18,7 +19,7 @@ constexpr int64_t kMaxNormK = 16384, kMaxHead = 256;
 bool is_16bit(clq_type t) { return t == CLQ_F16 || t == CLQ_BF16; }
 bool is_type(clq_type t) { return is_16bit(t) || t == CLQ_F32; }
 clq::MxType mx_type(clq_type t) { return t == CLQ_F16 ? clq::MxType::F16 : t == CLQ_BF16 ? clq::MxType::BF16 : clq::MxType::F32; }
-bool is_eps(float eps) { return isfinite(eps) && eps > 0.0f; }
+bool is_eps(float eps) { return isfinite(eps) && eps >= FLT_MIN; }
 
 bool is_stride(int64_t ld, int64_t n) { return ld >= n && ld % 8 == 0; }
 clq_status check_samples(int64_t M, int64_t samples) {
@@ -190,6 +191,8 @@ clq_status clq_a8_linear_act(const void *Xq8, const float *x_scale, const void *
     if ((s = check_rows(M)) != CLQ_OK || (s = check_rows(N)) != CLQ_OK || (s = check_k(K)) != CLQ_OK ||
         (s = check_samples(M, samples)) != CLQ_OK)
         return s;
+    // (a launch has fewer than 2^32 lanes)
+    if (((M + 255) / 256) * ((N + 127) / 128) >= (int64_t)1 << 24) return CLQ_ERR_SHAPE;
     if ((!gate && samples != 1) || !is_stride(ldy, N) || (R && ldr < N)) return CLQ_ERR_SHAPE;
     if (!aligned(Xq8, 16) || !aligned(Wq, 16) || !aligned(Y, 16) || !aligned(R, type == CLQ_F32 ? 4 : 2) || !aligned(gate, 16) ||
         !aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 2))

@@ -159,10 +159,10 @@ struct Args {
     MxType bias_type, gate_type;
 };
 
-// What is done with the sums, as a policy of the kernels.  PlainEpi: the epilogue of the entry points without
-// activation, spelt out in them.  Others (act_epilogue.h): kActs, turn bytes of a wave, and
+// What split_gemm_kernel does with the sums.  PlainEpi: the epilogue of the entry points without activation,
+// spelt out there.  Others (act_epilogue.h): kActs, turn bytes of a wave, and
 //   Operands<BN, BM>  load(a, tm, tn, tid) ahead of the k loop, store(a, ep, tid) behind it
-//   finish_tile, finish_split  of a wave's fragments.
+//   finish_unit       of a wave's fragments.
 struct PlainEpi {
     static constexpr bool kActs = false;
     static constexpr int kTurnBytes = 0;
@@ -423,15 +423,15 @@ struct EpilogueOf<PlainEpi, BN, BM, NT, BIAS> { using type = EpilogueOperands<BN
 // over the tile in fp64 (the integer sum exact) and keeps one partial per wave.
 // A target tile's candidates are neighbours in the tile order, so that one
 // XCD's L2 serves the target and the activation panel to all of them.
-template <class C, bool I32OUT, bool RAGGED, bool BIAS, bool ERR = false, class E = PlainEpi>
+template <class C, bool I32OUT, bool RAGGED, bool BIAS, bool ERR = false>
 __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
 {
     static_assert(!(I32OUT && BIAS), "no bias on the integer output");
     static_assert(!ERR || (!I32OUT && !BIAS), "the error mode has no output and no bias");
     constexpr Fmt F = C::fmt;
     constexpr int NS = C::NS;
-    __shared__ __align__(16) uint8_t pool[C::POOL > C::WM * E::kTurnBytes ? C::POOL : C::WM * E::kTurnBytes];
-    __shared__ __align__(16) float ep[E::template kOperands<C::BN, C::BM>];   // channel scales, biases, token scales
+    __shared__ __align__(16) uint8_t pool[C::POOL];
+    __shared__ float ep[C::EPN];   // channel scales, biases (fp16 widened), token scales
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int M = a.M, N = a.N, nks = a.K >> 6;
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
     // ---- epilogue operands: loaded ahead of the transfers, held in registers
     // through the k loop, written to LDS after it (an LDS store while transfers
     // into LDS are in flight would wait for all of them)
-    typename EpilogueOf<E, C::BN, C::BM, C::NT, BIAS>::type eo;
+    EpilogueOperands<C::BN, C::BM, C::NT, BIAS> eo;
     if constexpr (!I32OUT) eo.load(a, tm, tn, tid);
     __builtin_amdgcn_sched_barrier(0);
 
@@ -561,15 +561,10 @@ __global__ void __launch_bounds__(C::NT, 2) tile_gemm_kernel(Args a)
     op[0].template wait<0>();
     op[1].template wait<0>();
     if constexpr (!I32OUT) {
-        if constexpr (E::kActs) eo.store(a, ep, tid);
-        else eo.store(ep, tid);
+        eo.store(ep, tid);
         __syncthreads();
     }
 
-    if constexpr (E::kActs) {
-        E::template finish_tile<F, 4>(a, acc, pool + wave * E::kTurnBytes, ep, C::BM, tm, tn, wave, lane);
-        return;
-    }
     // ---- epilogue: lane owns token m and 16 consecutive channels ----------------
     const int h16 = (lane >> 5) * 16;
     if constexpr (ERR) {

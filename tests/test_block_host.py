@@ -43,7 +43,7 @@ def norm8(X=A, xt=0, ldx=1152, R=None, rt=0, ldr=1152, W=None, wt=0, samples=1, 
 
 
 COMMON = [(dict(X=None), NULL), (dict(R=A), NULL), (dict(S=A), NULL), (dict(xt=3), ARG), (dict(xt=-1), ARG),
-          (dict(R=A, S=A, rt=3), ARG), (dict(W=A, wt=5), ARG), (dict(eps=0.0), ARG), (dict(eps=-1.0), ARG),
+          (dict(R=A, S=A, rt=3), ARG), (dict(W=A, wt=5), ARG), (dict(eps=0.0), ARG), (dict(eps=1e-39), ARG), (dict(eps=-1.0), ARG),
           (dict(eps=math.inf), ARG), (dict(eps=math.nan), ARG), (dict(M=0), SHAPE), (dict(M=2 ** 31), SHAPE),
           (dict(samples=2), SHAPE), (dict(W=A, samples=3), SHAPE), (dict(W=A, samples=8), SHAPE), (dict(W=A, samples=0), SHAPE),
           (dict(K=0), SHAPE), (dict(K=16448, ldx=16448), SHAPE), (dict(ldx=1144), SHAPE), (dict(ldx=1156), SHAPE),
@@ -115,7 +115,7 @@ def lin(Xq=A, xs=A, Wq=A, ws=A, bits=8, b=None, bt=0, act=0, g=None, gt=0, sampl
     (dict(bits=6), ARG), (dict(act=2), ARG), (dict(act=4), ARG), (dict(t=3), ARG), (dict(b=A, bt=2), ARG), (dict(g=A, gt=3), ARG),
     (dict(M=0), SHAPE), (dict(N=0), SHAPE), (dict(K=32), SHAPE), (dict(K=96), SHAPE), (dict(K=65536), SHAPE), (dict(samples=2), SHAPE),
     (dict(g=A, samples=3), SHAPE), (dict(g=A, samples=0), SHAPE), (dict(ldy=56), SHAPE), (dict(ldy=68), SHAPE),
-    (dict(R=A, ldr=63), SHAPE), (dict(Xq=MIS), ALIGN), (dict(xs=MIS), ALIGN), (dict(Wq=MIS), ALIGN), (dict(ws=MIS), ALIGN),
+    (dict(R=A, ldr=63), SHAPE), (dict(M=2 ** 31 - 1, N=2 ** 16, ldy=2 ** 16), SHAPE), (dict(Xq=MIS), ALIGN), (dict(xs=MIS), ALIGN), (dict(Wq=MIS), ALIGN), (dict(ws=MIS), ALIGN),
     (dict(Y=MIS), ALIGN), (dict(b=0x10001), ALIGN), (dict(g=MIS), ALIGN), (dict(R=0x10001), ALIGN), (dict(R=MIS, t=2), ALIGN)])
 def test_linear_act_refusals(kw, want):
     assert lin(**kw) == want

@@ -369,7 +369,9 @@ def gate_arg(kw):
     (1300, 640, 1304, 8, F16, "gelu", F16, 13, True, F16), (2048, 1152, 1152, 4, F16, None, F16, 2, True, F16),
     (5000, 320, 1160, 8, F16, "silu", F32, 2, True, BF16), (8192, 256, 4608, 4, BF16, "gelu", None, 1, False, BF16),
     (6000, 64, 2000, 8, F16, "gelu", BF16, 6, True, F32), (2304, 1152, 3456, 8, F16, None, None, 1, False, F16),
-    (4100, 128, 1152, 4, F16, None, F32, 4, True, F32)])
+    (4100, 128, 1152, 4, F16, None, F32, 4, True, F32), (3000, 192, 3456, 4, F16, "gelu", F16, 3, True, F16),
+    (4200, 320, 1100, 4, BF16, "silu", F16, 7, True, BF16), (4200, 448, 1101, 8, F16, "gelu", BF16, 4200, True, F32),
+    (32, 2048, 512, 8, F16, None, F32, 32, True, BF16), (31, 64, 33, 4, None, "silu", F16, 31, True, F32)])
 def test_linear_act(clq, M, K, N, bits, bt, act, gt, samples, res, dtype):
     g = gen(M + N)
     q, xs, qw, p = operands(clq, g, M, K, N, bits)
