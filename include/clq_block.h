@@ -67,7 +67,7 @@ clq_status clq_dequantize_act8(const void *Xq8, const float *x_scale, int64_t M,
  * axis(i) the first axis a with i < pair_ends[a]:
  *   (a, b) -> (a cos - b sin, b cos + a sin).
  *   X        fp16 or bf16 [M][heads][D], strides ldx (row) and lhx (head), multiples of 8; D % 8 == 0,
- *            D <= 256.  Heads may be columns of a wider row (queries and keys of one projection).
+ *            D <= 256, heads <= 2^20.  Heads may be columns of a wider row (queries and keys of one projection).
  *   positions  int32 or fp32 [tokens][axes] (position_type: 0 int32, 1 fp32), M % tokens == 0.
  *   freqs    fp64 [P], radians a position.  Angles are formed and reduced in fp64.
  *   pair_ends  host int32 [axes], 1 <= axes <= 4, ascending, the last a multiple of 4, 2 P <= D.

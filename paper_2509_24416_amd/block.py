@@ -16,12 +16,12 @@ Every call enqueues on the current stream, or on `stream`; what it allocates bel
 to that stream.  Nothing here has a gradient of its own: the package is post-training quantization.
 """
 import ctypes
+import functools
 
 import torch
 
-from . import (CLQ_ERR_ARG, CLQ_ERR_SHAPE, ClqError, _check, _check_xq8, _lib, _ptr, _raw_stream, clq_act8_bytes,
-               clq_weight8_bytes, clq_weight_bytes)
-from .mx4 import _HALF, _TYPES, _apart, _current_device, _dev, _elsewhere, _gather, _output, _row_bytes, _rows2d, _together
+from . import CLQ_ERR_ARG, CLQ_ERR_SHAPE, ClqError, _check, _lib, _raw_stream
+from .mx4 import _HALF, _TYPES, _current_device, _dev, _elsewhere, _gather, _meet, _output, _row_bytes, _rows2d, _together
 
 _i64, _i32, _f32, _p = ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
 _SIGNATURES = {
@@ -43,6 +43,9 @@ for _name, (_res, _args) in _SIGNATURES.items():
 BLOCK_EXPORTS = tuple(_SIGNATURES)
 __all__ = ["BLOCK_EXPORTS", "clq_rope_freqs", *BLOCK_EXPORTS]
 
+_POSITIONS = {torch.int32: 0, torch.float32: 1}
+_F64, _F32, _U8 = (torch.float64,), (torch.float32,), (torch.uint8,)
+_NONE = (None, 0, 1)
 _ACTS = {None: 0, "none": 0, "gelu": 1, "silu": 3}
 
 
@@ -51,18 +54,34 @@ def _flat_bytes(t):
     return t.data_ptr(), 1, n, n
 
 
-def _modulation(w, name, K, M, device, types=_TYPES):
+def _apart(out, *inputs):
+    """An output of the caller's must not lie in what the launch reads: pieces at one distance are compared
+    piece by piece, others by the spans they lie in."""
+    for x in inputs:
+        a, b = ((p[0], 1, 1, p[1] * p[3]) if p[1] == 1 or p[2] == p[3] else p for p in (out, x))
+        if a[1] == 1 or b[1] == 1 or a[2] == b[2]:
+            bad = _meet(a, b)
+        else:
+            (lo, hi), (lo2, hi2) = ((p[0], p[0] + (p[1] - 1) * p[2] + p[3]) for p in (a, b))
+            bad = lo < hi2 and lo2 < hi
+        if bad:
+            raise ValueError("the output overlaps an input")
+
+
+def _modulation(w, name, K, M, device):
     """Pointer, type and samples of a [K] or [samples, K] matrix (None: none)."""
     if w is None:
-        return None, 0, 1
-    _dev(w, name, types)
-    if w.dim() not in (1, 2) or w.shape[-1] != K or not w.is_contiguous():
+        return _NONE
+    t = _dev(w, name, _TYPES).dtype
+    shape = w.shape
+    samples = 1 if len(shape) == 1 else shape[0]
+    if len(shape) not in (1, 2) or shape[-1] != K or not w.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [{K}] or [samples, {K}] tensor")
-    samples = 1 if w.dim() == 1 else w.shape[0]
     if samples < 1 or M % samples:
         raise ValueError(f"{name} has {samples} samples, which do not divide {M} rows")
-    _together(device, name, w)
-    return w.data_ptr(), _TYPES[w.dtype], samples
+    if w.device != device:
+        _together(device, name, w)
+    return w.data_ptr(), _TYPES[t], samples
 
 
 def _in_place(out, t, ld_out, ld):
@@ -81,15 +100,16 @@ def _norm_operands(X, weight, residual, sum_out):
             raise ValueError("there is no sum without a residual")
         return M, K, ldx, w, (None, 0, 0)
     r, k, ldr = _rows2d(residual, "residual", _TYPES)
-    if (r, k) != (M, K):
+    if r != M or k != K:
         raise ValueError(f"residual must be [{M}, {K}]")
-    _together(device, "residual", residual)
+    if residual.device != device:
+        _together(device, "residual", residual)
     if sum_out is not None:
-        _sum_rows(X, residual, sum_out, M, K, ldx, ldr, weight)
+        _check_sum(X, residual, sum_out, M, K, ldx, ldr, weight)
     return M, K, ldx, w, (residual.data_ptr(), _TYPES[residual.dtype], ldr)
 
 
-def _sum_rows(X, residual, sum_out, M, K, ldx, ldr, weight):
+def _check_sum(X, residual, sum_out, M, K, ldx, ldr, weight):
     s, n, lds = _rows2d(sum_out, "sum_out", (residual.dtype,))
     if (s, n) != (M, K):
         raise ValueError(f"sum_out must be [{M}, {K}]")
@@ -98,7 +118,6 @@ def _sum_rows(X, residual, sum_out, M, K, ldx, ldr, weight):
     if not _in_place(sum_out, residual, lds, ldr):
         _apart(at, _row_bytes(residual, M, K, ldr))
     _apart(at, _row_bytes(X, M, K, ldx), *(() if weight is None else (_flat_bytes(weight),)))
-    return lds
 
 
 def _norm_inputs(X, weight, residual, M, K, ldx, r):
@@ -132,15 +151,15 @@ def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, 
         if out is not None and sum_out is not None:
             _apart(_row_bytes(S, M, K, lds), _row_bytes(Y, M, K, ldy))
     _check(_lib.clq_rms_norm(X.data_ptr(), _TYPES[X.dtype], ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, M, K,
-                             Y.data_ptr(), _TYPES[dtype], ldy, _ptr(S), lds, _raw_stream(i)), "clq_rms_norm")
+                             Y.data_ptr(), _TYPES[dtype], ldy, None if S is None else S.data_ptr(), lds, _raw_stream(i)), "clq_rms_norm")
     return Y if S is None else (Y, S)
 
 
 def _codes(M, K, device, out, scale_out, reads, where):
     """Buffers of 8-bit codes and their scales: the caller's, checked against what the call reads, or new ones."""
-    n = clq_act8_bytes(M, K)
-    if n == 0:
+    if not 0 < M < 2147483648 or not 64 <= K <= 16384 or K & 63:
         raise ClqError(CLQ_ERR_SHAPE, where)
+    n = (M + 31) // 32 * 32 * K
     if out is None:
         out = torch.empty(n, dtype=torch.uint8, device=device)
     else:
@@ -181,7 +200,7 @@ def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None,
                        "clq_rms_norm_act8")
     S, lds = (None, 0) if residual is None else _output(sum_out, M, K, residual.dtype, device)
     _check(_lib.clq_rms_norm_act8(X.data_ptr(), _TYPES[X.dtype], ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, g, M, K,
-                                  block, q.data_ptr(), xs.data_ptr(), _ptr(S), lds, _raw_stream(i)),
+                                  block, q.data_ptr(), xs.data_ptr(), None if S is None else S.data_ptr(), lds, _raw_stream(i)),
            "clq_rms_norm_act8")
     return (q, xs) if S is None else (q, xs, S)
 
@@ -204,14 +223,25 @@ def clq_quantize_act8(X, block, perm=None, out=None, scale_out=None, stream=None
     return q, xs
 
 
+def _rows8(Xq8, x_scale, K):
+    """Rows of 8-bit activations, checked."""
+    _dev(Xq8, "Xq8", _U8)
+    _dev(x_scale, "x_scale", _F32)
+    M = x_scale.shape[0] if x_scale.dim() == 1 else 0
+    if M < 1 or not x_scale.is_contiguous():
+        raise ValueError("x_scale must be a contiguous [M] tensor")
+    if Xq8.numel() < (M + 31) // 32 * 32 * K or not Xq8.is_contiguous():
+        raise ValueError("Xq8 must be the contiguous buffer of 8-bit codes of these rows and K")
+    if x_scale.device != Xq8.device:
+        _together(Xq8.device, "x_scale", x_scale)
+    return M
+
+
 def clq_dequantize_act8(Xq8, x_scale, K, dtype=torch.float16, out=None, stream=None):
     """The values that 8-bit activations stand for (still rotated): fp16, bf16 or fp32 [M, K], M =
     len(x_scale)."""
-    M = _check_xq8(Xq8, x_scale, K)
+    M = _rows8(Xq8, x_scale, K)
     device = Xq8.device
-    _together(device, "x_scale", x_scale)
-    if x_scale.dim() != 1 or not x_scale.is_contiguous():
-        raise ValueError("x_scale must be a contiguous [M] tensor")
     i = device.index
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
@@ -224,22 +254,22 @@ def clq_dequantize_act8(Xq8, x_scale, K, dtype=torch.float16, out=None, stream=N
     return o
 
 
+@functools.lru_cache(maxsize=64)
 def _pair_ends(axes):
-    """Pairs of the axes so far, from the columns each axis turns."""
-    axes = tuple(axes)
+    """Pairs of the axes so far, from the columns each axis turns (a tuple)."""
     if not 1 <= len(axes) <= 4 or any(int(d) != d or d < 2 or d % 2 for d in axes):
         raise ValueError("axes must be one to four positive even numbers of columns")
     ends, n = (_i32 * len(axes))(), 0
     for j, d in enumerate(axes):
         n += int(d) // 2
         ends[j] = n
-    return ends, n
+    return ends, n, ctypes.addressof(ends), len(axes)
 
 
 def clq_rope_freqs(axes, theta=10000.0, device="cuda"):
     """Radians a position for each pair: an axis of d columns has theta^(-2 j / d), j = 0 .. d / 2 - 1
     (fp64 [sum(axes) / 2])."""
-    _pair_ends(axes)
+    _pair_ends(tuple(axes))
     return torch.cat([float(theta) ** (-torch.arange(0, d, 2, dtype=torch.float64, device=device) / d) for d in axes])
 
 
@@ -272,20 +302,20 @@ def clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, we
     [heads, D] of an RMS norm of each head ahead of the turn.  out: where, X itself included."""
     M, H, D, ldx, lhx = _head_strides(X, "X", _HALF)
     device = X.device
-    ends, n = _pair_ends(axes)
-    _dev(positions, "positions", (torch.int32, torch.float32))
-    if positions.dim() != 2 or positions.shape[1] != len(ends) or not positions.is_contiguous():
-        raise ValueError(f"positions must be a contiguous [tokens, {len(ends)}] tensor")
-    tokens = positions.shape[0]
+    _, n, ends, na = _pair_ends(tuple(axes))
+    pt = _dev(positions, "positions", _POSITIONS).dtype
+    shape = positions.shape
+    if len(shape) != 2 or shape[1] != na or not positions.is_contiguous():
+        raise ValueError(f"positions must be a contiguous [tokens, {na}] tensor")
+    tokens = shape[0]
     if tokens < 1 or M % tokens:
         raise ValueError(f"positions of {tokens} tokens do not repeat over {M} rows")
-    _dev(freqs, "freqs", (torch.float64,))
-    if freqs.shape != (n,) or not freqs.is_contiguous():
+    if _dev(freqs, "freqs", _F64).shape != (n,) or not freqs.is_contiguous():
         raise ValueError(f"freqs must be a contiguous fp64 [{n}] tensor")
     if 2 * n > D:
         raise ValueError(f"the axes turn {2 * n} columns, a head has {D}")
-    for t, name in ((positions, "positions"), (freqs, "freqs")):
-        _together(device, name, t)
+    if positions.device != device or freqs.device != device:
+        raise ValueError(f"positions and freqs are on {positions.device} and {freqs.device}, not on {device}")
     w, wt, wh = None, 0, 1
     if weight is not None:
         _dev(weight, "weight", _TYPES)
@@ -309,8 +339,8 @@ def clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, we
             _apart(at, _head_bytes(X, M, H, D, ldx, lhx))
         _apart(at, _flat_bytes(positions), _flat_bytes(freqs), *(() if weight is None else (_flat_bytes(weight),)))
     _check(_lib.clq_rope_axes(X.data_ptr(), _TYPES[X.dtype], ldx, lhx, positions.data_ptr(),
-                              int(positions.dtype is torch.float32), tokens, freqs.data_ptr(), ends, len(ends),
-                              int(bool(interleaved)), int(bool(inverse)), w, wt, wh, eps, M, H, D, Y.data_ptr(), ldy, lhy,
+                              _POSITIONS[pt], tokens, freqs.data_ptr(), ends, na, 1 if interleaved else 0,
+                              1 if inverse else 0, w, wt, wh, eps, M, H, D, Y.data_ptr(), ldy, lhy,
                               _raw_stream(i)), "clq_rope_axes")
     return Y
 
@@ -320,25 +350,24 @@ def clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual
     once.  act: None, "gelu" (tanh form) or "silu".  gate: [N], or [samples, N] for rows of that many equal
     samples.  residual: of Y's type [M, N].  dtype: of Y (by default that of `out`, of the residual, or fp16).
     out: where, the residual itself included."""
-    M = _check_xq8(Xq8, x_scale, qw.K)
-    N, K, device = qw.N, qw.K, Xq8.device
-    if x_scale.dim() != 1 or not x_scale.is_contiguous():
-        raise ValueError("x_scale must be a contiguous [M] tensor")
-    if qw.bits not in (4, 8):
+    N, K, bits, wq, ws, device = qw.N, qw.K, qw.bits, qw.wq, qw.w_scale, Xq8.device
+    M = _rows8(Xq8, x_scale, K)
+    if bits not in (4, 8):
         raise ClqError(CLQ_ERR_ARG, "clq_a8_linear_act")
-    if qw.wq.numel() < (clq_weight_bytes if qw.bits == 4 else clq_weight8_bytes)(N, K) or qw.w_scale.numel() < N:
+    if wq.numel() * 8 < N * K * bits or ws.numel() < N or not wq.is_contiguous() or not ws.is_contiguous():
         raise ValueError("the weights' buffers are too small for their N and K")
     if act not in _ACTS:
         raise ValueError(f"act must be None, 'gelu' or 'silu', not {act!r}")
-    for t, name in ((x_scale, "x_scale"), (qw.wq, "weights"), (qw.w_scale, "weights")):
-        _together(device, name, t)
+    if wq.device != device or ws.device != device:
+        raise ValueError(f"weights are on {wq.device}, not on {device}")
     b, bt = None, 0
     if bias is not None:
-        _dev(bias, "bias", _HALF)
+        bt = _TYPES[_dev(bias, "bias", _HALF).dtype]
         if bias.shape != (N,) or not bias.is_contiguous():
             raise ValueError(f"bias must be a contiguous [{N}] tensor")
-        _together(device, "bias", bias)
-        b, bt = bias.data_ptr(), _TYPES[bias.dtype]
+        if bias.device != device:
+            _together(device, "bias", bias)
+        b = bias.data_ptr()
     g, gt, samples = _modulation(gate, "gate", N, M, device)
     if dtype is None:
         dtype = out.dtype if out is not None else residual.dtype if residual is not None else torch.float16
@@ -358,8 +387,8 @@ def clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual
         at = _row_bytes(Y, M, N, ld)
         if residual is not None and not _in_place(Y, residual, ld, ldr):
             _apart(at, _row_bytes(residual, M, N, ldr))
-        _apart(at, *(_flat_bytes(t) for t in (Xq8, x_scale, qw.wq, qw.w_scale, bias, gate) if t is not None))
-    _check(_lib.clq_a8_linear_act(Xq8.data_ptr(), x_scale.data_ptr(), qw.wq.data_ptr(), qw.w_scale.data_ptr(), qw.bits, b,
-                                  bt, _ACTS[act], g, gt, samples, r, ldr, M, N, K, _TYPES[dtype], Y.data_ptr(), ld,
+        _apart(at, *(_flat_bytes(t) for t in (Xq8, x_scale, wq, ws, bias, gate) if t is not None))
+    _check(_lib.clq_a8_linear_act(Xq8.data_ptr(), x_scale.data_ptr(), wq.data_ptr(), ws.data_ptr(), bits, b, bt,
+                                  _ACTS[act], g, gt, samples, r, ldr, M, N, K, _TYPES[dtype], Y.data_ptr(), ld,
                                   _raw_stream(i)), "clq_a8_linear_act")
     return Y

@@ -15,6 +15,12 @@
 // with stage s + NS.  The loop runs over whole groups of kDepth stages, each of which fetches the same
 // (past the end the last stage again); the up to three stages behind it fetch nothing, and their waits count
 // that.
+//
+// What bounds it: on long k loops the power limit (43200 x 4608 -> 1152 on int8 weights: 214 us, 2.15 POP/s at 1.7 of
+// 2.4 GHz, matrix cores 63% busy at that clock; with gate and residual, 100 MB more, 235); on short ones a tile's
+// prologue and epilogue beside its 18 stages of 64 codes (8192 x 1152 -> 4608, GELU: 62 us, 2.16 GHz, matrix cores 31%
+// busy, 1152 tiles on 512 slots).  Wave priorities (by wave slot or workgroup, so that one workgroup of a
+// compute unit runs ahead of the other) made it 0 to 10% slower.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -33,6 +39,7 @@ using tg::static_for;
 using tg::v4i;
 using tg::v4u;
 
+// (6 and 8 stages ahead took the same time on int8 weights: 43200 x 4608 -> 1152 214 to 216 us)
 constexpr int kDepth = 4, kStages = kDepth + 1, kStageBytes = 4096;
 
 // Buffer transfers into LDS, 16 bytes a lane from byte lane_off + off of a buffer: the compiler counts
@@ -146,8 +153,7 @@ __global__ void __launch_bounds__(NW * 64, 2) a8_tile_kernel(tg::Args a)
     auto stage = [&](auto pc, auto bc) __attribute__((always_inline)) {
         constexpr int P = decltype(pc)::value, R = P & 1;
         constexpr bool BEHIND = decltype(bc)::value;
-        static_assert(NS == 5, "three stages between a transfer and the wait for it");
-        wait_stage<BEHIND ? (3 - P) * FETCH : 3 * FETCH>(op[R]);
+        wait_stage<BEHIND ? (kDepth - 1 - P) * FETCH : (kDepth - 1) * FETCH>(op[R]);
         const uint32_t nxt = cur == (uint32_t)((NS - 1) * kStageBytes) ? 0u : cur + kStageBytes;
         op[1 - R].read(wl + nxt);
         if constexpr (!BEHIND) produce(cur, k + NS);

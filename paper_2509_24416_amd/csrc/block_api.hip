@@ -14,7 +14,7 @@ using namespace clq::api;
 
 namespace {
 
-constexpr int64_t kMaxNormK = 16384, kMaxHead = 256;
+constexpr int64_t kMaxNormK = 16384, kMaxHead = 256, kMaxHeads = 1 << 20;
 
 bool is_16bit(clq_type t) { return t == CLQ_F16 || t == CLQ_BF16; }
 bool is_type(clq_type t) { return is_16bit(t) || t == CLQ_F32; }
@@ -138,6 +138,7 @@ clq_status clq_rope_axes(const void *X, clq_type type, int64_t ldx, int64_t lhx,
     if (W && (!is_type(w_type) || !is_eps(eps))) return CLQ_ERR_ARG;
     clq_status s;
     if ((s = check_rows(M)) != CLQ_OK || (s = check_rows(heads)) != CLQ_OK) return s;
+    if (heads > kMaxHeads) return CLQ_ERR_SHAPE;
     if (tokens < 1 || tokens > M || M % tokens != 0) return CLQ_ERR_SHAPE;
     if (D < 8 || D > kMaxHead || D % 8 != 0) return CLQ_ERR_SHAPE;
     if (W && weight_heads != 1 && weight_heads != heads) return CLQ_ERR_SHAPE;

@@ -95,7 +95,7 @@ def rope(X=A, t=0, ldx=1152, lhx=72, pos=A, pt=0, tokens=4, f=A, ends=(12, 24, 3
 @pytest.mark.parametrize("kw,want", [
     (dict(X=None), NULL), (dict(Y=None), NULL), (dict(pos=None), NULL), (dict(f=None), NULL), (dict(ends=None, axes=1), NULL),
     (dict(t=2), ARG), (dict(pt=2), ARG), (dict(axes=0), ARG), (dict(axes=5), ARG), (dict(inter=2), ARG), (dict(inv=-1), ARG),
-    (dict(W=A, wt=3), ARG), (dict(W=A, eps=0.0), ARG), (dict(M=0), SHAPE), (dict(H=0), SHAPE), (dict(tokens=3), SHAPE),
+    (dict(W=A, wt=3), ARG), (dict(W=A, eps=0.0), ARG), (dict(M=0), SHAPE), (dict(H=0), SHAPE), (dict(H=2 ** 20 + 1), SHAPE), (dict(tokens=3), SHAPE),
     (dict(tokens=0), SHAPE), (dict(tokens=8), SHAPE), (dict(D=0), SHAPE), (dict(D=70), SHAPE), (dict(D=264, ldx=4224), SHAPE),
     (dict(W=A, wh=2), SHAPE), (dict(ends=(12, 12, 36)), SHAPE), (dict(ends=(0, 12, 36)), SHAPE), (dict(ends=(12, 24, 40)), SHAPE),
     (dict(ends=(12, 24, 34)), SHAPE), (dict(ldx=64), SHAPE), (dict(lhx=64), SHAPE), (dict(lhx=76), SHAPE), (dict(ldy=1148), SHAPE),
@@ -119,6 +119,20 @@ def lin(Xq=A, xs=A, Wq=A, ws=A, bits=8, b=None, bt=0, act=0, g=None, gt=0, sampl
     (dict(Y=MIS), ALIGN), (dict(b=0x10001), ALIGN), (dict(g=MIS), ALIGN), (dict(R=0x10001), ALIGN), (dict(R=MIS, t=2), ALIGN)])
 def test_linear_act_refusals(kw, want):
     assert lin(**kw) == want
+
+
+def test_rows_that_overlap():
+    """Outputs of other spacing than an input are compared by the spans of both."""
+    from paper_2509_24416_amd.block import _apart
+    a = (1000, 5, 100, 40)                       # five pieces of 40 bytes, 100 apart
+    for other, bad in (((1040, 5, 100, 60), False), ((1040, 5, 100, 61), True), ((900, 5, 100, 100), True), ((900, 1, 1, 100), False),
+                       ((1050, 3, 200, 10), True), ((1440, 3, 200, 10), False), ((500, 5, 100, 40), False), ((500, 6, 100, 40), True), ((0, 11, 104, 40), True),
+                       ((1440, 1, 1, 5), False), ((1439, 1, 1, 5), True)):
+        if bad:
+            with pytest.raises(ValueError, match="overlaps"):
+                _apart(a, (0, 1, 1, 8), other)
+        else:
+            _apart(a, (0, 1, 1, 8), other)
 
 
 def test_freqs():

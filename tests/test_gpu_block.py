@@ -104,16 +104,14 @@ def test_norm_in_place_and_given_buffers(clq):
     y2, s2 = clq.clq_rms_norm(x2, w, r2, out=x2, sum_out=r2)
     assert y2 is x2 and s2 is r2 and torch.equal(y2, y) and torch.equal(s2, s)
     out, total = strided(torch.empty_like(x)), strided(torch.empty_like(r), 24)
-    tail = out.untyped_storage(), total.untyped_storage()
     y3, s3 = clq.clq_rms_norm(x, w, r, out=out, sum_out=total)
     assert torch.equal(y3, y) and torch.equal(s3, s)
     for t, pad in ((out, 8), (total, 24)):   # the columns behind a row stay what they were
         wide = t.as_strided((77, 1152 + pad), (1152 + pad, 1))
-        assert wide[:76, 1152:].isnan().all()
+        assert wide[:, 1152:].isnan().all()
     r4 = r.clone()
     q, xs, s4 = clq.clq_rms_norm_act8(x, 64, w, r4, sum_out=r4)
     assert s4 is r4 and torch.equal(s4, s)
-    assert len(tail) == 2
 
 
 def hadamard(b):
@@ -530,6 +528,46 @@ def test_streams(clq):
     assert torch.equal(y, clq.clq_rms_norm(x, n, r)[0]) and torch.equal(z.view_as(x), x)
 
 
+def test_offsets_past_32_bits(clq):
+    """Rows whose elements lie past 2^31 of their matrix's start (and past 2^32 bytes)."""
+    g = gen(16)
+    M, ld = 70000, 32768
+    big = torch.empty(M, ld, dtype=F16, device="cuda")
+    x, r, y = big[:, :64], big[:, 1024:1088], big[:, 2048:2112]
+    x.copy_(randn(g, M, 64, dtype=F16))
+    r.copy_(randn(g, M, 64, dtype=F16))
+    want64 = norm64(x, r, None)[1]
+    want, total = clq.clq_rms_norm(x.contiguous(), None, r.contiguous())
+    got, s = clq.clq_rms_norm(x, None, r, out=y, sum_out=big[:, 4096:4160])
+    assert torch.equal(got, want) and torch.equal(s, total)
+    q, xs, _ = clq.clq_rms_norm_act8(x, 64, None, r, sum_out=r)
+    d = clq.clq_dequantize_act8(q, xs, 64, out=big[:, 8192:8256])
+    assert torch.equal(d, clq.clq_dequantize_act8(q, xs, 64)) and torch.equal(r, total)
+    check_codes(clq, q, xs, want64, None, 64, 64)
+    pos, f = torch.arange(M, dtype=torch.int32, device="cuda").unsqueeze(1), clq.clq_rope_freqs((64,))
+    turned = clq.clq_rope_axes(x.unsqueeze(1), pos, f, (64,), out=big[:, 16384:16448].unsqueeze(1))
+    assert torch.equal(turned, clq.clq_rope_axes(x.contiguous().unsqueeze(1), pos, f, (64,)))
+    W = clq.clq_quantize_weights8(randn(g, 64, 64, dtype=F16), 64)
+    lin = clq.clq_a8_linear_act(q, xs, W, residual=r, out=big[:, 30000:30064])
+    assert torch.equal(lin, clq.clq_a8_linear_act(q, xs, W, residual=total))
+
+
+def test_captured_with_gathered_rows(clq):
+    """Gathered rows need more LDS than a launch has by itself: set up in a capture as well."""
+    g = gen(17)
+    x, p = randn(g, 40, 8192, dtype=F16), torch.randperm(8192, device="cuda", generator=g).to(torch.int32)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q, xs = clq.clq_rms_norm_act8(x, 128, perm=p)
+    for seed in range(3):
+        x.copy_(randn(gen(seed), 40, 8192, dtype=F16))
+        want = clq.clq_rms_norm_act8(x, 128, perm=p)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(q, want[0]) and torch.equal(xs, want[1])
+
+
 def test_binding_refusals(clq):
     g = gen(15)
     x = randn(g, 8, 128, dtype=F16)
@@ -541,6 +579,7 @@ def test_binding_refusals(clq):
     for bad, kw in (("weight", dict(weight=wide[0, :64])), ("samples", dict(weight=wide[:3])), ("residual", dict(residual=r[:4])),
                     ("without a residual", dict(sum_out=r)), ("sum_out", dict(residual=r, sum_out=r[:4])),
                     ("overlaps", dict(out=wide[4:12], residual=wide[8:])), ("overlaps", dict(residual=wide[:8], sum_out=wide[4:12])),
+                    ("overlaps", dict(out=flat[:1024].view(8, 128), residual=flat.as_strided((8, 128), (256, 1), 512))),
                     ("overlaps", dict(weight=flat[512:640], out=flat[:1024].view(8, 128)))):
         with pytest.raises(ValueError, match=bad):
             clq.clq_rms_norm(x, **kw)
