@@ -45,7 +45,7 @@ __all__ = ["BLOCK_EXPORTS", "clq_rope_freqs", *BLOCK_EXPORTS]
 
 _POSITIONS = {torch.int32: 0, torch.float32: 1}
 _F64, _F32, _U8 = (torch.float64,), (torch.float32,), (torch.uint8,)
-_NONE = (None, 0, 1)
+_NONE, _NO_RESIDUAL = (None, 0, 1), (None, 0, 0)
 _ACTS = {None: 0, "none": 0, "gelu": 1, "silu": 3}
 
 
@@ -66,6 +66,16 @@ def _apart(out, *inputs):
             bad = lo < hi2 and lo2 < hi
         if bad:
             raise ValueError("the output overlaps an input")
+
+
+def _matrix(X, name):
+    """_rows2d of any of the three types, and the type as the C calls take it."""
+    if not isinstance(X, torch.Tensor) or not X.is_cuda or X.dtype not in _TYPES or X.dim() != 2:
+        return *_rows2d(X, name, _TYPES), None   # (which says what is wrong)
+    (M, K), (ld, step) = X.shape, X.stride()
+    if step != 1:
+        raise ValueError(f"{name} must be 2-D with unit column stride")
+    return M, K, ld if M > 1 else (K + 7) & ~7, _TYPES[X.dtype]   # (a single row has no stride of its own)
 
 
 def _modulation(w, name, K, M, device):
@@ -90,23 +100,23 @@ def _in_place(out, t, ld_out, ld):
 
 
 def _norm_operands(X, weight, residual, sum_out):
-    """Checks what both forms of the norm share; (rows, columns, stride, weight, residual, sum) with the last
-    three as the C call takes them."""
-    M, K, ldx = _rows2d(X, "X", _TYPES)
+    """Checks what both forms of the norm share; (rows, columns, stride, type, device, weight, residual), the
+    last two as the C call takes them."""
+    M, K, ldx, xt = _matrix(X, "X")
     device = X.device
-    w = _modulation(weight, "weight", K, M, device)
+    w = _NONE if weight is None else _modulation(weight, "weight", K, M, device)
     if residual is None:
         if sum_out is not None:
             raise ValueError("there is no sum without a residual")
-        return M, K, ldx, w, (None, 0, 0)
-    r, k, ldr = _rows2d(residual, "residual", _TYPES)
+        return M, K, ldx, xt, device, w, _NO_RESIDUAL
+    r, k, ldr, rt = _matrix(residual, "residual")
     if r != M or k != K:
         raise ValueError(f"residual must be [{M}, {K}]")
     if residual.device != device:
         _together(device, "residual", residual)
     if sum_out is not None:
         _check_sum(X, residual, sum_out, M, K, ldx, ldr, weight)
-    return M, K, ldx, w, (residual.data_ptr(), _TYPES[residual.dtype], ldr)
+    return M, K, ldx, xt, device, w, (residual.data_ptr(), rt, ldr)
 
 
 def _check_sum(X, residual, sum_out, M, K, ldx, ldr, weight):
@@ -131,28 +141,39 @@ def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, 
     row stride that is a multiple of 8.  weight: [K], or [samples, K] for rows of that many equal samples.
     residual: fp16, bf16 or fp32 [M, K]; the sum comes back too, in its type (sum_out: where, the residual
     itself included).  dtype: of Y (X's by default).  out: where, X itself included."""
-    M, K, ldx, w, r = _norm_operands(X, weight, residual, sum_out)
-    device = X.device
+    M, K, ldx, xt, device, w, r = _norm_operands(X, weight, residual, sum_out)
     i = device.index
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
             return clq_rms_norm(X, weight, residual, eps, dtype, out, sum_out)
     if dtype is None:
         dtype = X.dtype if out is None else out.dtype
-    Y, ldy = _output(out, M, K, dtype, device)
-    if out is not None:
+    if out is None and dtype in _TYPES:
+        Y, ldy = torch.empty(M, K, dtype=dtype, device=device), K
+    else:
+        Y, ldy = _output(out, M, K, dtype, device)
         at = _row_bytes(Y, M, K, ldy)
         if not _in_place(Y, X, ldy, ldx):
             _apart(at, _row_bytes(X, M, K, ldx))
         _apart(at, *_norm_inputs(X, weight, residual, M, K, ldx, r))
-    S, lds = None, 0
-    if residual is not None:
-        S, lds = _output(sum_out, M, K, residual.dtype, device)
-        if out is not None and sum_out is not None:
-            _apart(_row_bytes(S, M, K, lds), _row_bytes(Y, M, K, ldy))
-    _check(_lib.clq_rms_norm(X.data_ptr(), _TYPES[X.dtype], ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, M, K,
-                             Y.data_ptr(), _TYPES[dtype], ldy, None if S is None else S.data_ptr(), lds, _raw_stream(i)), "clq_rms_norm")
+    S, s, lds = _sum(residual, sum_out, M, K, device)
+    if out is not None and sum_out is not None:
+        _apart(_row_bytes(S, M, K, lds), _row_bytes(Y, M, K, ldy))
+    status = _lib.clq_rms_norm(X.data_ptr(), xt, ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, M, K, Y.data_ptr(),
+                               _TYPES[dtype], ldy, s, lds, _raw_stream(i))
+    if status:
+        _check(status, "clq_rms_norm")
     return Y if S is None else (Y, S)
+
+
+def _sum(residual, sum_out, M, K, device):
+    """Where the sum goes: a tensor, its address and row stride."""
+    if residual is None:
+        return None, None, 0
+    if sum_out is None:
+        S = torch.empty(M, K, dtype=residual.dtype, device=device)
+        return S, S.data_ptr(), K
+    return sum_out, sum_out.data_ptr(), sum_out.stride(0) if M > 1 else K
 
 
 def _codes(M, K, device, out, scale_out, reads, where):
@@ -170,9 +191,10 @@ def _codes(M, K, device, out, scale_out, reads, where):
     if scale_out is None:
         scale_out = torch.empty(M, dtype=torch.float32, device=device)
     else:
-        if _dev(scale_out, "scale_out", (torch.float32,)).numel() < M or not scale_out.is_contiguous():
-            raise ValueError("the scales' buffer is too small")
+        if _dev(scale_out, "scale_out", _F32).dim() != 1 or scale_out.numel() < M or not scale_out.is_contiguous():
+            raise ValueError(f"scale_out must be a contiguous tensor of at least {M} scales")
         _together(device, "scale_out", scale_out)
+        scale_out = scale_out if scale_out.numel() == M else scale_out[:M]
         _apart((scale_out.data_ptr(), 1, 4 * M, 4 * M), (out.data_ptr(), 1, n, n), *reads)
     return out, scale_out
 
@@ -183,8 +205,7 @@ def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None,
     quantized to 8 bits a value with one scale a row, without a rounding in between: what
     clq_rotate_quant_act8 returns, (Xq8 uint8 [clq_act8_bytes(M, K)], x_scale fp32 [M]), and with a
     residual the sum."""
-    M, K, ldx, w, r = _norm_operands(X, weight, residual, sum_out)
-    device = X.device
+    M, K, ldx, xt, device, w, r = _norm_operands(X, weight, residual, sum_out)
     g = None if perm is None else _gather(perm, K, device)
     i = device.index
     if stream is not None or _current_device() != i:
@@ -198,17 +219,18 @@ def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None,
                         *(() if perm is None else (_flat_bytes(perm),)),
                         *(() if sum_out is None else (_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K),))),
                        "clq_rms_norm_act8")
-    S, lds = (None, 0) if residual is None else _output(sum_out, M, K, residual.dtype, device)
-    _check(_lib.clq_rms_norm_act8(X.data_ptr(), _TYPES[X.dtype], ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, g, M, K,
-                                  block, q.data_ptr(), xs.data_ptr(), None if S is None else S.data_ptr(), lds, _raw_stream(i)),
-           "clq_rms_norm_act8")
+    S, s, lds = _sum(residual, sum_out, M, K, device)
+    status = _lib.clq_rms_norm_act8(X.data_ptr(), xt, ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, g, M, K, block,
+                                    q.data_ptr(), xs.data_ptr(), s, lds, _raw_stream(i))
+    if status:
+        _check(status, "clq_rms_norm_act8")
     return (q, xs) if S is None else (q, xs, S)
 
 
 def clq_quantize_act8(X, block, perm=None, out=None, scale_out=None, stream=None):
     """clq_rotate_quant_act8 of fp16, bf16 or fp32 activations [M, K] (any row stride that is a multiple of 8):
     the same codes and scales for fp16."""
-    M, K, ldx = _rows2d(X, "X", _TYPES)
+    M, K, ldx, xt = _matrix(X, "X")
     device = X.device
     g = None if perm is None else _gather(perm, K, device)
     i = device.index
@@ -218,8 +240,9 @@ def clq_quantize_act8(X, block, perm=None, out=None, scale_out=None, stream=None
     q, xs = _codes(M, K, device, out, scale_out,
                    () if out is None and scale_out is None else (_row_bytes(X, M, K, ldx), *(() if perm is None else (_flat_bytes(perm),))),
                    "clq_quantize_act8")
-    _check(_lib.clq_quantize_act8(X.data_ptr(), _TYPES[X.dtype], ldx, g, M, K, block, q.data_ptr(), xs.data_ptr(),
-                                  _raw_stream(i)), "clq_quantize_act8")
+    status = _lib.clq_quantize_act8(X.data_ptr(), xt, ldx, g, M, K, block, q.data_ptr(), xs.data_ptr(), _raw_stream(i))
+    if status:
+        _check(status, "clq_quantize_act8")
     return q, xs
 
 
@@ -246,11 +269,14 @@ def clq_dequantize_act8(Xq8, x_scale, K, dtype=torch.float16, out=None, stream=N
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
             return clq_dequantize_act8(Xq8, x_scale, K, dtype, out)
-    o, ld = _output(out, M, K, dtype, device)
-    if out is not None:
+    if out is None and dtype in _TYPES and not K & 7:
+        o, ld = torch.empty(M, K, dtype=dtype, device=device), K
+    else:
+        o, ld = _output(out, M, K, dtype, device)
         _apart(_row_bytes(o, M, K, ld), _flat_bytes(Xq8), _flat_bytes(x_scale))
-    _check(_lib.clq_dequantize_act8(Xq8.data_ptr(), x_scale.data_ptr(), M, K, _TYPES[dtype], o.data_ptr(), ld,
-                                    _raw_stream(i)), "clq_dequantize_act8")
+    status = _lib.clq_dequantize_act8(Xq8.data_ptr(), x_scale.data_ptr(), M, K, _TYPES[dtype], o.data_ptr(), ld, _raw_stream(i))
+    if status:
+        _check(status, "clq_dequantize_act8")
     return o
 
 
@@ -338,10 +364,11 @@ def clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, we
         if not (_in_place(Y, X, ldy, ldx) and lhy == lhx):
             _apart(at, _head_bytes(X, M, H, D, ldx, lhx))
         _apart(at, _flat_bytes(positions), _flat_bytes(freqs), *(() if weight is None else (_flat_bytes(weight),)))
-    _check(_lib.clq_rope_axes(X.data_ptr(), _TYPES[X.dtype], ldx, lhx, positions.data_ptr(),
-                              _POSITIONS[pt], tokens, freqs.data_ptr(), ends, na, 1 if interleaved else 0,
-                              1 if inverse else 0, w, wt, wh, eps, M, H, D, Y.data_ptr(), ldy, lhy,
-                              _raw_stream(i)), "clq_rope_axes")
+    status = _lib.clq_rope_axes(X.data_ptr(), _TYPES[X.dtype], ldx, lhx, positions.data_ptr(), _POSITIONS[pt], tokens,
+                                freqs.data_ptr(), ends, na, 1 if interleaved else 0, 1 if inverse else 0, w, wt, wh, eps, M,
+                                H, D, Y.data_ptr(), ldy, lhy, _raw_stream(i))
+    if status:
+        _check(status, "clq_rope_axes")
     return Y
 
 
@@ -388,7 +415,8 @@ def clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual
         if residual is not None and not _in_place(Y, residual, ld, ldr):
             _apart(at, _row_bytes(residual, M, N, ldr))
         _apart(at, *(_flat_bytes(t) for t in (Xq8, x_scale, wq, ws, bias, gate) if t is not None))
-    _check(_lib.clq_a8_linear_act(Xq8.data_ptr(), x_scale.data_ptr(), wq.data_ptr(), ws.data_ptr(), bits, b, bt,
-                                  _ACTS[act], g, gt, samples, r, ldr, M, N, K, _TYPES[dtype], Y.data_ptr(), ld,
-                                  _raw_stream(i)), "clq_a8_linear_act")
+    status = _lib.clq_a8_linear_act(Xq8.data_ptr(), x_scale.data_ptr(), wq.data_ptr(), ws.data_ptr(), bits, b, bt, _ACTS[act],
+                                    g, gt, samples, r, ldr, M, N, K, _TYPES[dtype], Y.data_ptr(), ld, _raw_stream(i))
+    if status:
+        _check(status, "clq_a8_linear_act")
     return Y

@@ -576,6 +576,14 @@ def test_binding_refusals(clq):
     flat = torch.empty(4096, dtype=F16, device="cuda")
     with pytest.raises(TypeError, match="X"):
         clq.clq_rms_norm(r.double())
+    with pytest.raises(TypeError, match="X"):
+        clq.clq_rms_norm([1.0])
+    for bad in (x.t(), x[0], x.unsqueeze(0)):
+        with pytest.raises(ValueError, match="2-D"):
+            clq.clq_rms_norm(bad)
+    for f in (lambda **k: clq.clq_rms_norm(x, **k), lambda **k: clq.clq_dequantize_act8(*clq.clq_quantize_act8(x, 64), 128, **k)):
+        with pytest.raises(TypeError, match="dtype"):
+            f(dtype=torch.float64)
     for bad, kw in (("weight", dict(weight=wide[0, :64])), ("samples", dict(weight=wide[:3])), ("residual", dict(residual=r[:4])),
                     ("without a residual", dict(sum_out=r)), ("sum_out", dict(residual=r, sum_out=r[:4])),
                     ("overlaps", dict(out=wide[4:12], residual=wide[8:])), ("overlaps", dict(residual=wide[:8], sum_out=wide[4:12])),
@@ -595,8 +603,9 @@ def test_binding_refusals(clq):
         clq.clq_rms_norm_act8(x, 64, perm=torch.arange(64, dtype=torch.int32, device="cuda"))
     with pytest.raises(ValueError, match="too small"):
         clq.clq_rms_norm_act8(x, 64, out=torch.empty(64, dtype=torch.uint8, device="cuda"))
-    with pytest.raises(ValueError, match="too small"):
+    with pytest.raises(ValueError, match="scale_out"):
         clq.clq_rms_norm_act8(x, 64, scale_out=torch.empty(4, device="cuda"))
+    assert clq.clq_rms_norm_act8(x, 64, scale_out=torch.empty(20, device="cuda"))[1].shape == (8,)
     with pytest.raises(ValueError, match="overlaps"):
         clq.clq_rms_norm_act8(flat[:1024].view(8, 128), 64, out=flat.view(torch.uint8))
     h, f = x.view(8, 2, 64), clq.clq_rope_freqs((64,))
