@@ -47,10 +47,10 @@ hipError_t launch_act_rows(tg::Args a, hipStream_t stream) {
 //                            2.25 c, 8.2 / 7.8);
 //   t = M / 64 x N / 128     k over four waves up to t = 2 c, where they have a stage each (3072 x 4608 -> 1152,
 //   (rounded up)             1.7 c, 26.1, 96-channel tiles 27.8; 4096 x 4608 -> 1152, 2.25 c, 37.7 / 31.5);
-//   otherwise                256-token tiles, of 96 channels where these are resident at once and no more to a
-//                            compute unit than those of 128 (8192 x 4608 -> 1152: 384 and 288 of them, two a unit,
-//                            51.8 / 57.8; 12000 x 4608 -> 1152: 564 and 423, 77.5 / 65.8; 6144: 288 and 216, 48.0 /
-//                            38.4).
+//   otherwise                256-token tiles, of 96 channels where these are no more to a compute unit than those
+//                            of 128 (8192 x 4608 -> 1152: 384 and 288 of them, two a unit, 51.8 / 57.8; 4096 x 1152 ->
+//                            4608: 768 and 576, three a unit, 36.0 / 37.4; 12000 x 4608 -> 1152: 564 and 423, 77.5 /
+//                            65.8; 6144: 288 and 216, 48.0 / 38.4; 8192 x 1152 -> 4608: 1536 and 1152, 63.6 / 61.7).
 // Tiles of 128 tokens and the k loop over two waves won nowhere by more than 3%.
 template <tg::Fmt F, Act8 A, MxType T>
 hipError_t launch_act_shape(const tg::Args &a, hipStream_t stream) {
@@ -60,7 +60,7 @@ hipError_t launch_act_shape(const tg::Args &a, hipStream_t stream) {
     if (tg::tile_count(M, 64) * tg::tile_count(N, 128) <= 2 * c && (a.K >> 6) >= tg::SplitCfg<F, 4>::KS)
         return launch_act_split<tg::SplitCfg<F, 4>, E>(a, stream);
     const int64_t t128 = tg::tile_count(M, 256) * tg::tile_count(N, 128), t96 = tg::tile_count(M, 256) * tg::tile_count(N, 96);
-    if (t96 <= 2 * c && (t96 + c - 1) / c <= (t128 + c - 1) / c) return launch_act_direct<F, 4, 3, E>(a, stream);
+    if ((t96 + c - 1) / c <= (t128 + c - 1) / c) return launch_act_direct<F, 4, 3, E>(a, stream);
     return launch_act_direct<F, 4, 4, E>(a, stream);
 }
 

@@ -17,10 +17,11 @@
 // that.
 //
 // What bounds it: on long k loops the power limit (43200 x 4608 -> 1152 on int8 weights: 214 us, 2.15 POP/s at 1.7 of
-// 2.4 GHz, matrix cores 63% busy at that clock; with gate and residual, 100 MB more, 235); on short ones a tile's
-// prologue and epilogue beside its 18 stages of 64 codes (8192 x 1152 -> 4608, GELU: 62 us, 2.16 GHz, matrix cores 31%
-// busy, 1152 tiles on 512 slots).  Wave priorities (by wave slot or workgroup, so that one workgroup of a
-// compute unit runs ahead of the other) made it 0 to 10% slower.
+// 2.4 GHz, matrix cores 63% busy at that clock; with gate and residual, 100 MB more, 235).  On short ones loop,
+// epilogue and stores add up, at a clock that is held down as well (43200 x 1152 -> 4608 with GELU 279 us, 244 without
+// the stores, 185 without the epilogue; 8192 rows 60 us at 2.16 GHz, 1152 tiles on 512 slots).  That the two workgroups
+// of a compute unit are in step is not why: a later start of every other one changed nothing, and wave
+// priorities (by wave slot or workgroup) made it 0 to 10% slower.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -7,7 +7,8 @@
 // So a wave turns 32 tokens at a time in its own part of LDS (the sums themselves, before any arithmetic);
 // each lane then owns the same eight channels of all its tokens, holds their scale, bias and gate in
 // registers, and rows are read and stored in whole 256-byte pieces.  The residual is on its way before the
-// turn: its loads are the longest wait of the epilogue.
+// turn: its loads are the longest wait of the epilogue.  (fp32 rows: the eight channels are four and four, half a
+// tile apart, so that a store's lanes lie next to each other: 8192 x 1152 -> 4608 76 -> 65 us.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -65,6 +66,13 @@ struct ActEpi {
         }
     };
 
+    // Channel e of lane c's eight, of 32 NF.
+    template <int NF>
+    __device__ static __forceinline__ int channel(int c, int e) {
+        if constexpr (T == MxType::F32) return 4 * c + (e & 3) + (e < 4 ? 0 : 16 * NF);
+        return 8 * c + e;
+    }
+
     // The residual of 32 tokens x 32 NF channels, as the turned lanes take it.
     template <int NF>
     struct Residual {
@@ -72,16 +80,19 @@ struct ActEpi {
                               PASSES = 32 / RPP, W = T == MxType::F32 ? 2 : 1;
         uint4 v[PASSES][W];
         __device__ __forceinline__ void load(const tg::Args &a, int m0, int n0, int lane) {
-            if (a.res == nullptr || !a.res_vec) return;
-            const int n = min(n0 + 8 * min(lane & (LPR - 1), 4 * NF - 1), max(a.N - 8, 0) & ~7);
-            if (a.N < 8) return;
+            if (a.res == nullptr || !a.res_vec || a.N < 8) return;
+            constexpr int E = 8 / W;   // values of a load
+            const int c = min(lane & (LPR - 1), 4 * NF - 1);
 #pragma unroll
             for (int p = 0; p < PASSES; ++p) {
-                const int64_t at = (int64_t)min(m0 + p * RPP + lane / LPR, a.M - 1) * a.ldr + n;
-                const uint4 *q = T == MxType::F32 ? reinterpret_cast<const uint4 *>(static_cast<const float *>(a.res) + at)
-                                                  : reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.res) + at);
+                const int64_t row = (int64_t)min(m0 + p * RPP + lane / LPR, a.M - 1) * a.ldr;
 #pragma unroll
-                for (int h = 0; h < W; ++h) v[p][h] = q[h];
+                for (int h = 0; h < W; ++h) {
+                    const int64_t at = row + min(n0 + channel<NF>(c, E * h), (a.N - E) & ~(E - 1));
+                    v[p][h] = *reinterpret_cast<const uint4 *>(T == MxType::F32
+                                                                   ? static_cast<const void *>(static_cast<const float *>(a.res) + at)
+                                                                   : static_cast<const uint16_t *>(a.res) + at);
+                }
             }
         }
         __device__ __forceinline__ void widen(int p, float (&r)[8]) const {
@@ -108,6 +119,20 @@ struct ActEpi {
     __device__ static __forceinline__ void finish(const tg::Args &a, const tg::Acc<F> (&acc)[FN][2], const Residual<NF> &res,
                                                   uint8_t *turn, const float *ep, int BM, int m0, int r0, int tn, int lane) {
         constexpr int BN = 32 * FN, LPR = Residual<NF>::LPR, RPP = Residual<NF>::RPP;
+        const int c = lane & (LPR - 1), rs = lane / LPR, n0 = tn * BN + FN0 * 32;
+        const bool some = c < 4 * NF && n0 + channel<NF>(c, 0) < a.N;
+        float w[8], b[8], g[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int ch = FN0 * 32 + channel<NF>(min(c, 4 * NF - 1), e);
+            w[e] = ep[ch], b[e] = ep[BN + ch], g[e] = ep[2 * BN + ch];
+        }
+        const bool whole = n0 + channel<NF>(c, 7) < a.N;
+        // (tiles whose tokens are of several samples look their gates up row by row)
+        const bool one = a.gate == nullptr || (uint32_t)(m0 - r0) / (uint32_t)a.sample_rows ==
+                                                  (uint32_t)min(m0 - r0 + BM - 1, a.M - 1) / (uint32_t)a.sample_rows;
+        const bool gated = a.gate != nullptr, vec = a.res != nullptr && a.res_vec && whole;
+        constexpr float kDown = 1.0f / (float)(1 << tg::FmtInfo<F>::LOG);
         uint8_t *mine = turn + (lane & 31) * kPitch + (lane >> 5) * 64;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses stay in order)
         tg::static_for<0, NF>([&](auto fc) {
@@ -118,22 +143,13 @@ struct ActEpi {
                     tg::v4i{(int)x[4 * q], (int)x[4 * q + 1], (int)x[4 * q + 2], (int)x[4 * q + 3]};
         });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const int c = lane & (LPR - 1), rs = lane / LPR, ch = FN0 * 32 + 8 * c, n = tn * BN + ch;
-        if (c >= 4 * NF || n >= a.N) return;
-        float w[8], b[8], g[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = ep[ch + e], b[e] = ep[BN + ch + e], g[e] = ep[2 * BN + ch + e];
-        const bool whole = n <= a.N - 8;
-        // (tiles whose tokens are of several samples look their gates up row by row)
-        const bool one = a.gate == nullptr || (uint32_t)(m0 - r0) / (uint32_t)a.sample_rows ==
-                                                  (uint32_t)min(m0 - r0 + BM - 1, a.M - 1) / (uint32_t)a.sample_rows;
-        const bool gated = a.gate != nullptr, vec = a.res != nullptr && a.res_vec && whole;
-        constexpr float kDown = 1.0f / (float)(1 << tg::FmtInfo<F>::LOG);
+        if (!some) return;
 #pragma unroll
         for (int p = 0; p < Residual<NF>::PASSES; ++p) {
             const int r = p * RPP + rs, m = m0 + r;
-            const int4 *q = reinterpret_cast<const int4 *>(turn + r * kPitch + c * 32);
-            const int4 lo = q[0], hi = q[1];
+            const uint8_t *row = turn + r * kPitch;
+            const int4 lo = *reinterpret_cast<const int4 *>(row + channel<NF>(c, 0) * 4);
+            const int4 hi = *reinterpret_cast<const int4 *>(row + channel<NF>(c, 4) * 4);
             const int s[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             const float xs = ep[3 * BN + r0 + r] * kDown;
             float y[8];
@@ -145,13 +161,15 @@ struct ActEpi {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] *= g[e];
                 } else {
-                    const int64_t at = (int64_t)((uint32_t)m / (uint32_t)a.sample_rows) * a.N + n;
+                    const int64_t at = (int64_t)((uint32_t)m / (uint32_t)a.sample_rows) * a.N;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (n + e < a.N)
+                    for (int e = 0; e < 8; ++e) {
+                        const int n = n0 + channel<NF>(c, e);
+                        if (n < a.N)
                             y[e] *= a.gate_type == MxType::F32
-                                        ? static_cast<const float *>(a.gate)[at + e]
-                                        : clq::widen16(static_cast<const uint16_t *>(a.gate)[at + e], a.gate_type == MxType::BF16);
+                                        ? static_cast<const float *>(a.gate)[at + n]
+                                        : clq::widen16(static_cast<const uint16_t *>(a.gate)[at + n], a.gate_type == MxType::BF16);
+                    }
                 }
             }
             if (vec) {
@@ -161,19 +179,29 @@ struct ActEpi {
                 for (int e = 0; e < 8; ++e) y[e] += t[e];
             } else if (a.res != nullptr) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < a.N) y[e] += element(a.res, (int64_t)m * a.ldr + n + e);
+                for (int e = 0; e < 8; ++e) {
+                    const int n = n0 + channel<NF>(c, e);
+                    if (n < a.N) y[e] += element(a.res, (int64_t)m * a.ldr + n);
+                }
             }
-            const int64_t at = (int64_t)m * a.ldy + n;
+            const int64_t at = (int64_t)m * a.ldy + n0;
             if (whole) {
-                store8(a.Y, at, T, y);
+                if constexpr (T == MxType::F32) {
+                    float *dst = static_cast<float *>(a.Y) + at;
+                    *reinterpret_cast<float4 *>(dst + channel<NF>(c, 0)) = make_float4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<float4 *>(dst + channel<NF>(c, 4)) = make_float4(y[4], y[5], y[6], y[7]);
+                } else {
+                    store8(a.Y, at + channel<NF>(c, 0), T, y);
+                }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < a.N) {
-                        if constexpr (T == MxType::F32) static_cast<float *>(a.Y)[at + e] = y[e];
-                        else static_cast<uint16_t *>(a.Y)[at + e] = (uint16_t)narrow2(y[e], y[e], T == MxType::BF16);
+                for (int e = 0; e < 8; ++e) {
+                    const int n = channel<NF>(c, e);
+                    if (n0 + n < a.N) {
+                        if constexpr (T == MxType::F32) static_cast<float *>(a.Y)[at + n] = y[e];
+                        else static_cast<uint16_t *>(a.Y)[at + n] = (uint16_t)narrow2(y[e], y[e], T == MxType::BF16);
                     }
+                }
             }
         }
     }
