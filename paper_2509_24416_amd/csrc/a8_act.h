@@ -45,8 +45,8 @@ hipError_t launch_act_rows(tg::Args a, hipStream_t stream) {
 //   few tiles of 32 x 32     the rows kernel up to 2 c of them (one token x 4608 -> 1152 5.7, on 64 x 128 tiles with
 //                            the k loop over four waves 10.8; 300 x 1152 -> 1152, 1.4 c, 6.3 / 7.8; 128 x 1152 -> 4608,
 //                            2.25 c, 8.2 / 7.8);
-//   t = M / 64 x N / 128     k over four waves up to t = 2 c, where they have a stage each (3072 x 4608 -> 1152,
-//   (rounded up)             1.7 c, 26.1, 96-channel tiles 27.8; 4096 x 4608 -> 1152, 2.25 c, 37.7 / 31.5);
+//   t = M / 64 x N / 128     k over four waves up to t = 2 c, where they have a stage each (2560 x 4608 -> 1152,
+//   (rounded up)             1.4 c, 26.0, 96-channel tiles 27.8; 4096 x 4608 -> 1152, 2.25 c, 37.7 / 31.5);
 //   otherwise                256-token tiles, of 96 channels where these are no more to a compute unit than those
 //                            of 128 (8192 x 4608 -> 1152: 384 and 288 of them, two a unit, 51.8 / 57.8; 4096 x 1152 ->
 //                            4608: 768 and 576, three a unit, 36.0 / 37.4; 12000 x 4608 -> 1152: 564 and 423, 77.5 /

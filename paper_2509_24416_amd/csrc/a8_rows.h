@@ -2,7 +2,8 @@
 // idle and a launch takes the length of one wave's k loop.  Here a workgroup computes 32 tokens x 32 channels,
 // its eight waves an eighth of the k loop each, with operands straight from memory (nothing is shared between
 // them), kAhead stages of 64 codes ahead.  The partial sums, exact integers, meet in LDS; each thread then
-// finishes two channels of a token.
+// finishes two channels of a token.  What bounds it is latency: one token x 1152 -> 4608 4.4 us, x 4608 -> 1152 5.7 (weights of
+// 5.3 MB, 0.9 TB/s), 300 tokens x 1152 -> 1152 6.3.
 #pragma once
 
 #include <hip/hip_runtime.h>

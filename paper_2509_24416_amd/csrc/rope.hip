@@ -11,6 +11,10 @@
 // pairs), or V columns and their partners (halves paired; V = 8, or 4 where half of the turned columns is no
 // multiple of 8), and a wave takes as many heads side by side as its 64 lanes hold, several rows where a row's
 // heads do not fill it.  Its lanes work out the angles of its rows together and take their items' from LDS.
+//
+// Measured: 43200 rows of 32 heads of 72 columns, pairs 70 to 78 us (5.1 to 5.7 TB/s), halves (8 bytes a lane) 96, heads
+// normed 90 (one set of weights) and 96; 4608 rows of 48 heads of 128, halves, normed 24 to 27 (from the cache in part); 20000 rows of
+// 8 heads of 64 13 to 14.  With the angles worked out by each lane for itself 84, 100, 98 and 104; 29; 17 to 18.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

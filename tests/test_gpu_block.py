@@ -627,6 +627,8 @@ def test_binding_refusals(clq):
                     ("overlaps", dict(out=flat[:512].view(8, 64), residual=flat[64:576].view(8, 64)))):
         with pytest.raises(ValueError, match=bad):
             clq.clq_a8_linear_act(q, xs, qw, **kw)
+    with pytest.raises(clq.ClqError):
+        clq.clq_a8_linear_act(q, xs, clq.clq_qweight_f6(clq.clq_quantize_weights(randn(g, 64, 128, dtype=F16), 64)))
     with pytest.raises(TypeError, match="residual"):
         clq.clq_a8_linear_act(q, xs, qw, residual=res, dtype=F32)
     with pytest.raises(ValueError, match="Xq8"):
