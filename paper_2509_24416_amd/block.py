@@ -381,8 +381,9 @@ def clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual
     M = _rows8(Xq8, x_scale, K)
     if bits not in (4, 8):
         raise ClqError(CLQ_ERR_ARG, "clq_a8_linear_act")
-    if wq.numel() * 8 < N * K * bits or ws.numel() < N or not wq.is_contiguous() or not ws.is_contiguous():
-        raise ValueError("the weights' buffers are too small for their N and K")
+    if wq.dtype != torch.uint8 or ws.dtype != torch.float32 or not wq.is_contiguous() or not ws.is_contiguous() or \
+            wq.numel() < (N + 63) // 64 * 64 * K * bits // 8 or ws.numel() < N:   # (rows are padded to 64)
+        raise ValueError("the weights' buffers are not those of their N and K")
     if act not in _ACTS:
         raise ValueError(f"act must be None, 'gelu' or 'silu', not {act!r}")
     if wq.device != device or ws.device != device:

@@ -2,6 +2,7 @@
 
 Tolerances are sums of roundings: half a step of the output's type, plus what the fp32 arithmetic of each
 formula can lose (U = 2^-24, one fp32 rounding; each test says how many it counts)."""
+import dataclasses
 import math
 
 import pytest
@@ -629,6 +630,13 @@ def test_binding_refusals(clq):
             clq.clq_a8_linear_act(q, xs, qw, **kw)
     with pytest.raises(clq.ClqError):
         clq.clq_a8_linear_act(q, xs, clq.clq_qweight_f6(clq.clq_quantize_weights(randn(g, 64, 128, dtype=F16), 64)))
+    for bits in (4, 8):   # buffers without the rows that pad them to 64, of another type
+        _, _, odd, _ = operands(clq, g, 8, 128, 40, bits)
+        assert clq.clq_a8_linear_act(q, xs, odd).shape == (8, 40)
+        for change in (dict(wq=odd.wq[:40 * 128 * bits // 8]), dict(wq=odd.wq.view(torch.int32)), dict(w_scale=odd.w_scale[:39]),
+                       dict(w_scale=odd.w_scale.half())):
+            with pytest.raises(ValueError, match="weights"):
+                clq.clq_a8_linear_act(q, xs, dataclasses.replace(odd, **change))
     with pytest.raises(TypeError, match="residual"):
         clq.clq_a8_linear_act(q, xs, qw, residual=res, dtype=F32)
     with pytest.raises(ValueError, match="Xq8"):
