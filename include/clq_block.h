@@ -35,7 +35,8 @@ extern "C" {
  *   sum      out, s rounded to R's type, row stride ld_sum; may be R, in place.  The norm is that of s
  *            before this rounding.
  * A row that holds a NaN or an infinity gives NaN where s / infinity is one and, in the 8-bit form, a
- * NaN scale.  Squares are summed in fp32: of values past 2^62 they overflow. */
+ * NaN scale.  Squares are summed in fp32: of values past 2^62 they overflow.  In the 8-bit form rows whose
+ * rotated s W stays under 2^-119 are zeros. */
 
 /* Y = n in fp16, bf16 or fp32, row stride ldy; may be X, in place.  8 <= K <= 16384, K % 8 == 0. */
 clq_status clq_rms_norm(const void *X, clq_type x_type, int64_t ldx, const void *R, clq_type r_type, int64_t ldr,
@@ -52,7 +53,9 @@ clq_status clq_rms_norm_act8(const void *X, clq_type x_type, int64_t ldx, const 
                              hipStream_t stream);
 
 /* clq_rotate_quant_act8 of fp16, bf16 or fp32 activations (the results of an activating linear, say, that
- * were not rounded to 16 bits): the same codes and scales for fp16.  Shapes as above. */
+ * were not rounded to 16 bits): the same codes and scales for finite fp16 values.  A NaN in a row, and an
+ * infinity with its opposite or another in one block, give a NaN scale, a lone infinity an infinite one; rows
+ * whose rotation stays under 2^-119 are zeros.  Shapes as above. */
 clq_status clq_quantize_act8(const void *X, clq_type x_type, int64_t ldx, const int32_t *perm, int64_t M, int64_t K,
                              int32_t block, void *Xq8, float *x_scale, hipStream_t stream);
 

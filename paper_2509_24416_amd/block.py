@@ -229,7 +229,7 @@ def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None,
 
 def clq_quantize_act8(X, block, perm=None, out=None, scale_out=None, stream=None):
     """clq_rotate_quant_act8 of fp16, bf16 or fp32 activations [M, K] (any row stride that is a multiple of 8):
-    the same codes and scales for fp16."""
+    the same codes and scales for finite fp16 values."""
     M, K, ldx, xt = _matrix(X, "X")
     device = X.device
     g = None if perm is None else _gather(perm, K, device)

@@ -315,9 +315,9 @@ rms_norm_kernel(NormArgs a)
             }
         }
     } else {
-        // (maxima whose reciprocal would overflow count as zeros: eps keeps the factor finite)
+        // (maxima whose 127 / m would overflow count as zeros: eps keeps the factor finite)
         float top = of_mine(m);
-        top = top < 0x1p-100f ? 0.0f : top;
+        top = top < 0x1p-119f ? 0.0f : top;
         if (t0 < 4 && mine < rows) a.x_scale[row_of(mine)] = (top / 127.0f) * inv;
         float rs[4];
         quad(top == 0.0f ? 0.0f : 127.0f / top, rs);

@@ -229,6 +229,22 @@ def test_norm_of_zeros_infinities_and_nans(clq):
         assert ((clq.clq_dequantize_act8(q, xs, 256, dtype=F32)[rest].double() - v).abs() <= 0.51 * xs[rest].double().unsqueeze(1)).all()
 
 
+@pytest.mark.parametrize("t", [BF16, F32])
+def test_rows_of_tiny_values(clq, t):
+    """8-bit rows down to a maximum of 2^-119; smaller ones are zeros."""
+    g = gen(17)
+    x = randn(g, 6, 256)
+    for row, power in enumerate((-60, -99, -105, -112, -128, -140)):
+        x[row] = x[row].clamp(-4, 4) * 2.0 ** power
+    x = x.to(t)
+    for q, xs, n in ((*clq.clq_quantize_act8(x, 64), x.double()),
+                     (*clq.clq_rms_norm_act8(x, 64, eps=2.0 ** -126), norm64(x, None, None, 2.0 ** -126)[1])):
+        codes = clq.clq_unswizzle_act8(q, 6, 256)
+        assert (xs[4:] == 0).all() and (codes[4:] == 0).all()
+        assert (xs[:4] > 0).all() and (codes[:4].abs().amax(1) == 127).all()
+        check_codes(clq, q, xs[:4], n[:4], None, 64, 256, str(t))
+
+
 def rope64(x, pos, freqs, axes, interleaved, inverse, w, eps=EPS):
     v, n = x.double(), freqs.numel()
     if w is not None:
