@@ -84,9 +84,9 @@ def _modulation(w, name, K, M, device):
         return _NONE
     t = _dev(w, name, _TYPES).dtype
     shape = w.shape
-    samples = 1 if len(shape) == 1 else shape[0]
     if len(shape) not in (1, 2) or shape[-1] != K or not w.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [{K}] or [samples, {K}] tensor")
+    samples = 1 if len(shape) == 1 else shape[0]
     if samples < 1 or M % samples:
         raise ValueError(f"{name} has {samples} samples, which do not divide {M} rows")
     if w.device != device:
@@ -207,6 +207,8 @@ def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None,
     residual the sum."""
     M, K, ldx, xt, device, w, r = _norm_operands(X, weight, residual, sum_out)
     g = None if perm is None else _gather(perm, K, device)
+    if perm is not None and sum_out is not None:
+        _apart(_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K), _flat_bytes(perm))
     i = device.index
     if stream is not None or _current_device() != i:
         with _elsewhere(device, stream):
@@ -296,6 +298,8 @@ def clq_rope_freqs(axes, theta=10000.0, device="cuda"):
     """Radians a position for each pair: an axis of d columns has theta^(-2 j / d), j = 0 .. d / 2 - 1
     (fp64 [sum(axes) / 2])."""
     _pair_ends(tuple(axes))
+    if not 0 < theta < float("inf"):
+        raise ValueError(f"theta must be positive and finite, not {theta}")
     return torch.cat([float(theta) ** (-torch.arange(0, d, 2, dtype=torch.float64, device=device) / d) for d in axes])
 
 

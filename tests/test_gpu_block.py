@@ -601,7 +601,7 @@ def test_binding_refusals(clq):
     for f in (lambda **k: clq.clq_rms_norm(x, **k), lambda **k: clq.clq_dequantize_act8(*clq.clq_quantize_act8(x, 64), 128, **k)):
         with pytest.raises(TypeError, match="dtype"):
             f(dtype=torch.float64)
-    for bad, kw in (("weight", dict(weight=wide[0, :64])), ("samples", dict(weight=wide[:3])), ("residual", dict(residual=r[:4])),
+    for bad, kw in (("weight", dict(weight=wide[0, :64])), ("weight", dict(weight=wide[0, 0])), ("samples", dict(weight=wide[:3])), ("residual", dict(residual=r[:4])),
                     ("without a residual", dict(sum_out=r)), ("sum_out", dict(residual=r, sum_out=r[:4])),
                     ("overlaps", dict(out=wide[4:12], residual=wide[8:])), ("overlaps", dict(residual=wide[:8], sum_out=wide[4:12])),
                     ("overlaps", dict(out=flat[:1024].view(8, 128), residual=flat.as_strided((8, 128), (256, 1), 512))),
@@ -625,6 +625,12 @@ def test_binding_refusals(clq):
     assert clq.clq_rms_norm_act8(x, 64, scale_out=torch.empty(20, device="cuda"))[1].shape == (8,)
     with pytest.raises(ValueError, match="overlaps"):
         clq.clq_rms_norm_act8(flat[:1024].view(8, 128), 64, out=flat.view(torch.uint8))
+    total = torch.zeros(8, 128, device="cuda")   # (zeros: a gather of column 0)
+    with pytest.raises(ValueError, match="overlaps"):
+        clq.clq_rms_norm_act8(x, 64, residual=r, sum_out=total, perm=total[7].view(torch.int32))
+    for theta in (0.0, -2.0, math.inf, math.nan):
+        with pytest.raises(ValueError, match="theta"):
+            clq.clq_rope_freqs((64,), theta)
     h, f = x.view(8, 2, 64), clq.clq_rope_freqs((64,))
     pos = torch.zeros(8, 1, dtype=torch.int32, device="cuda")
     for bad, args in (("positions", (pos.repeat(1, 2), f, (64,))), ("repeat", (pos[:3], f, (64,))), ("freqs", (pos, f[:16], (64,))),
