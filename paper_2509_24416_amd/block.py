@@ -55,16 +55,15 @@ def _flat_bytes(t):
 
 
 def _apart(out, *inputs):
-    """An output of the caller's must not lie in what the launch reads: pieces at one distance are compared
-    piece by piece, others by the spans they lie in."""
+    """An output of the caller's must not lie in what the launch reads: where the spans they lie in meet, pieces
+    at one distance are compared piece by piece."""
+    at, n, pitch, width = out
+    end = at + (n - 1) * pitch + width
     for x in inputs:
+        if x[0] >= end or x[0] + (x[1] - 1) * x[2] + x[3] <= at:
+            continue
         a, b = ((p[0], 1, 1, p[1] * p[3]) if p[1] == 1 or p[2] == p[3] else p for p in (out, x))
-        if a[1] == 1 or b[1] == 1 or a[2] == b[2]:
-            bad = _meet(a, b)
-        else:
-            (lo, hi), (lo2, hi2) = ((p[0], p[0] + (p[1] - 1) * p[2] + p[3]) for p in (a, b))
-            bad = lo < hi2 and lo2 < hi
-        if bad:
+        if a[1] != 1 and b[1] != 1 and a[2] != b[2] or _meet(a, b):
             raise ValueError("the output overlaps an input")
 
 
@@ -121,19 +120,26 @@ def _norm_operands(X, weight, residual, sum_out):
 
 def _check_sum(X, residual, sum_out, M, K, ldx, ldr, weight):
     s, n, lds = _rows2d(sum_out, "sum_out", (residual.dtype,))
-    if (s, n) != (M, K):
+    if s != M or n != K:
         raise ValueError(f"sum_out must be [{M}, {K}]")
-    _together(X.device, "sum_out", sum_out)
-    at = _row_bytes(sum_out, M, K, lds)
+    if sum_out.device != X.device:
+        _together(X.device, "sum_out", sum_out)
+    at, reads = _row_bytes(sum_out, M, K, lds), [_row_bytes(X, M, K, ldx)]
     if not _in_place(sum_out, residual, lds, ldr):
-        _apart(at, _row_bytes(residual, M, K, ldr))
-    _apart(at, _row_bytes(X, M, K, ldx), *(() if weight is None else (_flat_bytes(weight),)))
+        reads.append(_row_bytes(residual, M, K, ldr))
+    if weight is not None:
+        reads.append(_flat_bytes(weight))
+    _apart(at, *reads)
 
 
-def _norm_inputs(X, weight, residual, M, K, ldx, r):
+def _norm_inputs(weight, residual, M, K, ldr):
     """What a norm's output must not lie in, X apart."""
-    return (*(() if weight is None else (_flat_bytes(weight),)),
-            *(() if residual is None else (_row_bytes(residual, M, K, r[2]),)))
+    reads = []
+    if weight is not None:
+        reads.append(_flat_bytes(weight))
+    if residual is not None:
+        reads.append(_row_bytes(residual, M, K, ldr))
+    return reads
 
 
 def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, sum_out=None, stream=None):
@@ -152,13 +158,13 @@ def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, 
         Y, ldy = torch.empty(M, K, dtype=dtype, device=device), K
     else:
         Y, ldy = _output(out, M, K, dtype, device)
-        at = _row_bytes(Y, M, K, ldy)
+        reads = _norm_inputs(weight, residual, M, K, r[2])
         if not _in_place(Y, X, ldy, ldx):
-            _apart(at, _row_bytes(X, M, K, ldx))
-        _apart(at, *_norm_inputs(X, weight, residual, M, K, ldx, r))
+            reads.append(_row_bytes(X, M, K, ldx))
+        if sum_out is not None:
+            reads.append(_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K))
+        _apart(_row_bytes(Y, M, K, ldy), *reads)
     S, s, lds = _sum(residual, sum_out, M, K, device)
-    if out is not None and sum_out is not None:
-        _apart(_row_bytes(S, M, K, lds), _row_bytes(Y, M, K, ldy))
     status = _lib.clq_rms_norm(X.data_ptr(), xt, ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, M, K, Y.data_ptr(),
                                _TYPES[dtype], ldy, s, lds, _raw_stream(i))
     if status:
@@ -216,11 +222,13 @@ def clq_rms_norm_act8(X, block, weight=None, residual=None, eps=1e-6, perm=None,
     if out is None and scale_out is None:
         q, xs = _codes(M, K, device, None, None, (), "clq_rms_norm_act8")
     else:
-        q, xs = _codes(M, K, device, out, scale_out,
-                       (_row_bytes(X, M, K, ldx), *_norm_inputs(X, weight, residual, M, K, ldx, r),
-                        *(() if perm is None else (_flat_bytes(perm),)),
-                        *(() if sum_out is None else (_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K),))),
-                       "clq_rms_norm_act8")
+        reads = _norm_inputs(weight, residual, M, K, r[2])
+        reads.append(_row_bytes(X, M, K, ldx))
+        if perm is not None:
+            reads.append(_flat_bytes(perm))
+        if sum_out is not None:
+            reads.append(_row_bytes(sum_out, M, K, sum_out.stride(0) if M > 1 else K))
+        q, xs = _codes(M, K, device, out, scale_out, reads, "clq_rms_norm_act8")
     S, s, lds = _sum(residual, sum_out, M, K, device)
     status = _lib.clq_rms_norm_act8(X.data_ptr(), xt, ldx, r[0], r[1], r[2], w[0], w[1], w[2], eps, g, M, K, block,
                                     q.data_ptr(), xs.data_ptr(), s, lds, _raw_stream(i))

@@ -117,8 +117,8 @@ __device__ __forceinline__ void store8(void *p, int64_t at, MxType type, const f
         float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + at);
         q[0] = make_float4(x[0], x[1], x[2], x[3]);
         q[1] = make_float4(x[4], x[5], x[6], x[7]);
-    } else {
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + at) = narrow8(x, type == MxType::BF16);
+    } else {   // (one branch for the eight)
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + at) = type == MxType::BF16 ? narrow8(x, true) : narrow8(x, false);
     }
 }
 #endif

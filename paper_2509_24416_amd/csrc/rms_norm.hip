@@ -15,8 +15,9 @@
 // so that results do not depend on the order in which waves arrive.
 //
 // Measured (a copy reaches 5.2 to 5.7 TB/s): 43200 x 1152 with a 16-bit residual to 8 bits 67 to 75 us (4.6 to 5.2
-// TB/s, vector issue 63% busy), with an fp32 one 105 (5.2), without one 40 (3.7: vector instructions); plain with residual
-// 78 (5.1); 8192 x 4608 plain 55 to 59 (5.1 to 5.5); fp32 rows of 43200 x 1152 quantized 45 (5.6).
+// TB/s), with an fp32 one 105 (5.2), without one 40 (3.7: vector instructions); plain with residual 77 (5.2); 8192 x 4608
+// plain with residual 53 (5.7); 3000 x 12288 59 (5.1), to 8 bits 86 (3.0: two chunks a lane spill); fp32 rows of 43200 x
+// 1152 quantized 45 (5.6).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -84,22 +85,26 @@ __device__ __forceinline__ void store_codes8(const float (&x)[4][8], const float
     }
 }
 
+enum class Res { None, F16, BF16, F32 };
+
 // Waves a SIMD that the registers are held to (what each form needs by itself, or a few less).
-template <int B, bool XW, int RES, bool NORM, int NCH>
+template <int B, MxType XT, Res RT, bool NORM, int NCH>
 constexpr int waves_per_simd() {
     if (NCH == 2) return 4;   // (a workgroup of 16 waves)
-    return NORM ? 7 - (B != 0) - (XW || RES == 2) : 7;
+    return NORM ? 7 - (B != 0) - (XT == MxType::F32 || RT == Res::F32) : 7;
 }
 
-// B: Hadamard block (0: plain result).  XW: X in fp32.  RES: the residual (0 none, 1 16-bit, 2 fp32).  NORM:
-// without it the rows are only rotated and quantized.  MIXED: four rows may be of several samples (a branch
-// for it at run time costs every launch 20 registers).  NCH: chunks per lane (1: rows of up to 8192 columns, 2:
-// up to 16384).
-template <int B, bool XW, int RES, bool NORM, bool MIXED, int NCH>
-__global__ void __launch_bounds__(kMaxLanes) __attribute__((amdgpu_waves_per_eu(waves_per_simd<B, XW, RES, NORM, NCH>())))
+// B: Hadamard block (0: plain result).  XT, RT: types of X and the residual (as branches at run time they cost
+// 8192 x 4608 with a residual 58.7 instead of 52.8 us, to 8 bits 59.4 instead of 55.0).  NORM: without it the rows
+// are only rotated and quantized.  MIXED: four rows may be of several samples (a branch for it at run time costs
+// every launch 20 registers).  NCH: chunks per lane (1: rows of up to 8192 columns, 2: up to 16384).
+template <int B, MxType XT, Res RT, bool NORM, bool MIXED, int NCH>
+__global__ void __launch_bounds__(kMaxLanes) __attribute__((amdgpu_waves_per_eu(waves_per_simd<B, XT, RT, NORM, NCH>())))
 rms_norm_kernel(NormArgs a)
 {
-    static_assert(NORM || (B != 0 && RES == 0), "a quantizer");
+    constexpr bool XW = XT == MxType::F32;
+    constexpr MxType kSum = RT == Res::F32 ? MxType::F32 : RT == Res::BF16 ? MxType::BF16 : MxType::F16;
+    static_assert(NORM || (B != 0 && RT == Res::None), "a quantizer");
     extern __shared__ __align__(16) float gat[];   // gathered inputs: a column's rows side by side
     __shared__ float4 psum[NORM ? kMaxLanes / 8 : 1], pmax[B ? kMaxLanes / 8 : 1];
     const int t = threadIdx.x;
@@ -118,40 +123,10 @@ rms_norm_kernel(NormArgs a)
     // rows of the four that exist; the others read the last of all
     const int rows = glive && row0 < (uint32_t)a.M ? (int)min(4u, (uint32_t)a.M - row0) : 0;
     auto row_of = [&](int r) { return (int64_t)min(row0 + r, (uint32_t)a.M - 1); };
-    const bool bf16 = a.x_type == MxType::BF16;
 
     // s w of each chunk, and the rows' sums of squares
     float x[NCH][4][8], sq[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     {
-        uint4 v[NCH][4][XW ? 2 : 1];
-        uint4 res[NCH][4][RES == 2 ? 2 : 1];
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int at = min(lane_c + i * a.stride, cpr - 1) * 8;
-            // (unconditional, so that all are in flight)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if constexpr (XW) {
-                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.X) + row_of(r) * a.ldx + at);
-                    v[i][r][0] = p[0];
-                    v[i][r][1] = p[1];
-                } else {
-                    v[i][r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.X) + row_of(r) * a.ldx + at);
-                }
-            }
-            if constexpr (RES == 1) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    res[i][r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.R) + row_of(r) * a.ldr + at);
-            } else if constexpr (RES == 2) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.R) + row_of(r) * a.ldr + at);
-                    res[i][r][0] = p[0];
-                    res[i][r][1] = p[1];
-                }
-            }
-        }
         auto as_floats = [](const uint4 &q, float *f) {
             f[0] = __uint_as_float(q.x), f[1] = __uint_as_float(q.y), f[2] = __uint_as_float(q.z), f[3] = __uint_as_float(q.w);
         };
@@ -160,6 +135,30 @@ rms_norm_kernel(NormArgs a)
         for (int i = 0; i < NCH; ++i) {
             const int chunk = lane_c + i * a.stride, at = min(chunk, cpr - 1) * 8;
             const bool live = chunk < cpr;
+            uint4 v[4][XW ? 2 : 1], res[4][RT == Res::F32 ? 2 : 1];
+            // (unconditional, so that all of a chunk are in flight)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (XW) {
+                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.X) + row_of(r) * a.ldx + at);
+                    v[r][0] = p[0];
+                    v[r][1] = p[1];
+                } else {
+                    v[r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.X) + row_of(r) * a.ldx + at);
+                }
+            }
+            if constexpr (RT == Res::F16 || RT == Res::BF16) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    res[r][0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.R) + row_of(r) * a.ldr + at);
+            } else if constexpr (RT == Res::F32) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.R) + row_of(r) * a.ldr + at);
+                    res[r][0] = p[0];
+                    res[r][1] = p[1];
+                }
+            }
             float w[8];
             if constexpr (NORM) {
 #pragma unroll
@@ -171,15 +170,15 @@ rms_norm_kernel(NormArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float(&y)[8] = x[i][r];
-                if constexpr (XW) as_floats(v[i][r][0], y), as_floats(v[i][r][1], y + 4);
-                else widen8(v[i][r][0], bf16, y);
-                if constexpr (RES != 0) {
+                if constexpr (XW) as_floats(v[r][0], y), as_floats(v[r][1], y + 4);
+                else widen8(v[r][0], XT == MxType::BF16, y);
+                if constexpr (RT != Res::None) {
                     float q[8];
-                    if constexpr (RES == 2) as_floats(res[i][r][0], q), as_floats(res[i][r][1], q + 4);
-                    else widen8(res[i][r][0], a.r_type == MxType::BF16, q);
+                    if constexpr (RT == Res::F32) as_floats(res[r][0], q), as_floats(res[r][1], q + 4);
+                    else widen8(res[r][0], RT == Res::BF16, q);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] += q[e];
-                    if (r < rows && live) store8(a.sum, row_of(r) * a.ld_sum + at, RES == 2 ? MxType::F32 : a.r_type, y);
+                    if (r < rows && live) store8(a.sum, row_of(r) * a.ld_sum + at, kSum, y);
                 }
                 if (r >= rows || !live) {
 #pragma unroll
@@ -193,6 +192,7 @@ rms_norm_kernel(NormArgs a)
                     for (int e = 0; e < 8; ++e) y[e] *= w[e];
                 }
             }
+            if (i + 1 < NCH) __builtin_amdgcn_sched_barrier(0);   // (both chunks' loads in flight: registers spill)
         }
     }
 
@@ -351,7 +351,7 @@ int pick_groups(int stride, int64_t total_groups, int cus, int most_waves) {
     return best;
 }
 
-template <int B, bool XW, int RES, bool NORM, bool MIXED, int NCH>
+template <int B, MxType XT, Res RT, bool NORM, bool MIXED, int NCH>
 hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
     NormArgs a;
     static_cast<RmsNormArgs &>(a) = args;
@@ -361,7 +361,7 @@ hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
     constexpr int P = NCH == 1 ? 4 : 2;
     if constexpr (NCH == 1) {
         a.stride = (cpr + 7) / 8 * 8;
-        a.groups = pick_groups(a.stride, units * 8, compute_units(), 4 * waves_per_simd<B, XW, RES, NORM, NCH>());
+        a.groups = pick_groups(a.stride, units * 8, compute_units(), 4 * waves_per_simd<B, XT, RT, NORM, NCH>());
         while (B != 0 && a.perm != nullptr && a.groups > 1 && (size_t)a.groups * a.K * P * 4 > kLdsLimit) a.groups >>= 1;
     } else {
         a.groups = 1;
@@ -371,7 +371,7 @@ hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
     const size_t lds = B != 0 && a.perm != nullptr ? (size_t)a.groups * a.K * P * 4 : 0;
     if (T > kMaxLanes || lds > kLdsLimit) return hipErrorInvalidConfiguration;
     if (lds > 65536 - 8192) {
-        hipError_t e = hipFuncSetAttribute((const void *)rms_norm_kernel<B, XW, RES, NORM, MIXED, NCH>,
+        hipError_t e = hipFuncSetAttribute((const void *)rms_norm_kernel<B, XT, RT, NORM, MIXED, NCH>,
                                            hipFuncAttributeMaxDynamicSharedMemorySize, kLdsLimit);
         if (e != hipSuccess) return e;
     }
@@ -382,30 +382,38 @@ hipError_t launch_norm(const RmsNormArgs &args, hipStream_t stream) {
         a.unit0 = (int)u0;
         a.units = (int)std::min<int64_t>(most, units - u0);
         const int64_t grid = ((int64_t)a.units + 7) / 8 * 8 * (8 / a.groups);
-        hipLaunchKernelGGL((rms_norm_kernel<B, XW, RES, NORM, MIXED, NCH>), dim3((unsigned)grid), dim3(T), lds, stream, a);
+        hipLaunchKernelGGL((rms_norm_kernel<B, XT, RT, NORM, MIXED, NCH>), dim3((unsigned)grid), dim3(T), lds, stream, a);
     }
     return hipGetLastError();
 }
 
-template <int B, bool XW, int RES, bool NORM>
+template <int B, MxType XT, Res RT, bool NORM>
 hipError_t launch_width(const RmsNormArgs &a, hipStream_t stream) {
     if constexpr (NORM)
         if (a.W != nullptr && a.sample_rows < a.M && a.sample_rows % 4 != 0)
-            return a.K <= 8 * kMaxLanes ? launch_norm<B, XW, RES, NORM, true, 1>(a, stream)
-                                        : launch_norm<B, XW, RES, NORM, true, 2>(a, stream);
-    return a.K <= 8 * kMaxLanes ? launch_norm<B, XW, RES, NORM, false, 1>(a, stream)
-                                : launch_norm<B, XW, RES, NORM, false, 2>(a, stream);
+            return a.K <= 8 * kMaxLanes ? launch_norm<B, XT, RT, NORM, true, 1>(a, stream)
+                                        : launch_norm<B, XT, RT, NORM, true, 2>(a, stream);
+    return a.K <= 8 * kMaxLanes ? launch_norm<B, XT, RT, NORM, false, 1>(a, stream)
+                                : launch_norm<B, XT, RT, NORM, false, 2>(a, stream);
 }
-template <int B, bool XW>
+template <int B, MxType XT>
 hipError_t launch_residual(const RmsNormArgs &a, hipStream_t stream) {
     if constexpr (B != 0)
-        if (!a.norm) return launch_width<B, XW, 0, false>(a, stream);
-    if (a.R == nullptr) return launch_width<B, XW, 0, true>(a, stream);
-    return a.r_type == MxType::F32 ? launch_width<B, XW, 2, true>(a, stream) : launch_width<B, XW, 1, true>(a, stream);
+        if (!a.norm) return launch_width<B, XT, Res::None, false>(a, stream);
+    if (a.R == nullptr) return launch_width<B, XT, Res::None, true>(a, stream);
+    switch (a.r_type) {
+        case MxType::F16: return launch_width<B, XT, Res::F16, true>(a, stream);
+        case MxType::BF16: return launch_width<B, XT, Res::BF16, true>(a, stream);
+        default: return launch_width<B, XT, Res::F32, true>(a, stream);
+    }
 }
 template <int B>
 hipError_t launch_type(const RmsNormArgs &a, hipStream_t stream) {
-    return a.x_type == MxType::F32 ? launch_residual<B, true>(a, stream) : launch_residual<B, false>(a, stream);
+    switch (a.x_type) {
+        case MxType::F16: return launch_residual<B, MxType::F16>(a, stream);
+        case MxType::BF16: return launch_residual<B, MxType::BF16>(a, stream);
+        default: return launch_residual<B, MxType::F32>(a, stream);
+    }
 }
 
 // One 16-byte operand piece (16 codes of a row) per thread: four threads write a row's 64 codes, sixteen
