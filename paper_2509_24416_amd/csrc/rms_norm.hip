@@ -16,7 +16,7 @@
 //
 // Measured (a copy reaches 5.2 to 5.7 TB/s): 43200 x 1152 with a 16-bit residual to 8 bits 67 to 75 us (4.6 to 5.2
 // TB/s), with an fp32 one 105 (5.2), without one 40 (3.7: vector instructions); plain with residual 77 (5.2); 8192 x 4608
-// plain with residual 53 (5.7); 3000 x 12288 59 (5.1), to 8 bits 86 (3.0: two chunks a lane spill); fp32 rows of 43200 x
+// plain with residual 53 (5.7); 3000 x 12288 57 (5.2), to 8 bits 65 (3.9: two chunks a lane), gathered 76; fp32 rows of 43200 x
 // 1152 quantized 45 (5.6).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -108,18 +108,19 @@ rms_norm_kernel(NormArgs a)
     extern __shared__ __align__(16) float gat[];   // gathered inputs: a column's rows side by side
     __shared__ float4 psum[NORM ? kMaxLanes / 8 : 1], pmax[B ? kMaxLanes / 8 : 1];
     const int t = threadIdx.x;
-    const int wpu = 8 / a.groups;                   // workgroups per unit
+    const int groups = NCH == 2 ? 1 : a.groups, wpu = 8 / groups;   // workgroups per unit
     const int idx = blockIdx.x >> 3;
     const int ul = (int)(blockIdx.x & 7) + 8 * (idx / wpu);
     if (ul >= a.units) return;
     const int u = a.unit0 + ul;
     const int K = a.K, cpr = K >> 3;
-    const int gl = t / a.stride, t0 = t - gl * a.stride;
-    const bool glive = gl < a.groups;
-    const int s = (idx % wpu) * a.groups + (glive ? gl : 0);
+    // (a workgroup of wide rows has one group: its rows' addresses are scalars)
+    const int gl = NCH == 2 ? 0 : t / a.stride, t0 = t - gl * a.stride;
+    const bool glive = NCH == 2 || gl < a.groups;
+    const int s = (idx % wpu) * groups + (glive ? gl : 0);
     const uint32_t row0 = (uint32_t)u * 32 + 4 * s;
     const int lane_c = logical_lane(t0);   // its chunk among the octet's eight
-    if (B == 0 && (uint32_t)u * 32 + 4 * ((idx % wpu) * a.groups) >= (uint32_t)a.M) return;   // (codes are written to the unit's end)
+    if (B == 0 && (uint32_t)u * 32 + 4 * ((idx % wpu) * groups) >= (uint32_t)a.M) return;   // (codes are written to the unit's end)
     // rows of the four that exist; the others read the last of all
     const int rows = glive && row0 < (uint32_t)a.M ? (int)min(4u, (uint32_t)a.M - row0) : 0;
     auto row_of = [&](int r) { return (int64_t)min(row0 + r, (uint32_t)a.M - 1); };
@@ -202,7 +203,6 @@ rms_norm_kernel(NormArgs a)
             // P rows of the group at a time, a column's side by side: one LDS read serves them
             constexpr int P = NCH == 1 ? 4 : 2;
             float *mine = gat + (int64_t)(glive ? gl : 0) * K * P;
-            float g[NCH][4][8];
 #pragma unroll
             for (int p0 = 0; p0 < 4; p0 += P) {
                 if (p0 > 0) __syncthreads();
@@ -220,20 +220,20 @@ rms_norm_kernel(NormArgs a)
 #pragma unroll
                 for (int i = 0; i < NCH; ++i) {
                     const int32_t *q = a.perm + min(lane_c + i * a.stride, cpr - 1) * 8;
+                    float g[P][8];   // (read by all lanes: a condition around the reads costs 10 of 82 us)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float *c = mine + (int64_t)q[e] * P;
 #pragma unroll
-                        for (int p = 0; p < P; ++p) g[i][p0 + p][e] = c[p];
+                        for (int p = 0; p < P; ++p) g[p][e] = c[p];
                     }
+                    const bool live = lane_c + i * a.stride < cpr;
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[i][p0 + p][e] = live ? g[p][e] : 0.0f;
                 }
             }
-#pragma unroll
-            for (int i = 0; i < NCH; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[i][r][e] = lane_c + i * a.stride < cpr ? g[i][r][e] : 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
