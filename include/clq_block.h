@@ -93,8 +93,7 @@ clq_status clq_rope_axes(const void *X, clq_type type, int64_t ldx, int64_t lhx,
  *   bias     fp16 or bf16 [N], or NULL.
  *   act      CLQ_ACT_NONE, CLQ_ACT_GELU (tanh form) or CLQ_ACT_SILU; ARG for CLQ_ACT_SWIGLU.
  *   gate     fp16, bf16 or fp32 [samples][N], contiguous, or NULL (samples 1).
- *   R        the residual stream, of the output's type [M][N], row stride ldr >= N, or NULL.  Rows that are
- *            16-byte aligned (ldr % 8 == 0) are read 16 bytes at a time.
+ *   R        the residual stream, of the output's type [M][N], row stride ldr >= N (any), or NULL.
  *   Y        out, fp16, bf16 or fp32, row stride ldy; may be R, in place. */
 #define CLQ_ACT_SILU 3 /* h / (1 + exp(-h)) */
 clq_status clq_a8_linear_act(const void *Xq8, const float *x_scale, const void *Wq, const float *w_scale,

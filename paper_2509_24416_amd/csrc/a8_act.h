@@ -83,7 +83,6 @@ hipError_t launch_act_type(const Act8Args &g, hipStream_t stream) {
     t.sample_rows = (int)g.sample_rows;
     t.res = g.R;
     t.ldr = g.ldr;
-    t.res_vec = g.ldr % 8 == 0 && reinterpret_cast<uintptr_t>(g.R) % 16 == 0;
     t.Y = g.Y;
     t.ldy = g.ldy;
     t.M = g.M;

@@ -155,7 +155,6 @@ struct Args {
     const void *gate, *res;
     int64_t ldr;
     int sample_rows;
-    bool res_vec;   // the residual's rows are 16-byte aligned
     MxType bias_type, gate_type;
 };
 

@@ -427,6 +427,24 @@ def test_without_activation_it_is_the_linear(clq, M, K, N, bits):
     assert differ.double().mean() < 2.0 ** -10
 
 
+@pytest.mark.parametrize("t", [F16, BF16, F32])
+@pytest.mark.parametrize("M,K,N", [(5, 128, 13), (700, 512, 333), (700, 64, 2900), (6000, 128, 1001), (3000, 192, 3457)])
+def test_residuals_of_any_alignment(clq, M, K, N, t):
+    """Rows without padding, from an odd element on, and padded ones: the same result, bit for bit."""
+    g = gen(M + N)
+    q, xs, qw, _ = operands(clq, g, M, K, N, 8)
+    padded = torch.full((M, (N + 7) // 8 * 8), math.nan, device="cuda", dtype=t)[:, :N]
+    padded[:] = randn(g, M, N, dtype=t)
+    gate = randn(g, N, dtype=F16)
+    want = clq.clq_a8_linear_act(q, xs, qw, act="silu", gate=gate, residual=padded)
+    assert want.isfinite().all()
+    tight = padded.contiguous()
+    odd = torch.full((M * N + 1,), math.nan, device="cuda", dtype=t)[1:].view(M, N)
+    odd[:] = padded
+    for res in (tight, odd):
+        assert torch.equal(clq.clq_a8_linear_act(q, xs, qw, act="silu", gate=gate, residual=res), want)
+
+
 def test_linear_act_far_from_zero(clq):
     """Activations at large arguments: no overflow in between."""
     g = gen(9)
