@@ -357,8 +357,8 @@ def run(state):
         return clq.clq_a8_linear_act(q, scale, s["qw"], s["b"], act=s["act"], gate=s["g"], residual=s["r"],
                                      dtype=_TYPES[s["dtype"]])
     q, scale, stream = clq.clq_rms_norm_act8(s["x"], s["block"], s["n"], s["r"], EPS)
-    h = clq.clq_a8_linear_act(q, scale, s["qw1"], s["b1"], act="gelu", dtype=torch.float32)
-    q, scale = clq.clq_quantize_act8(h, s["block"])
+    h = clq.clq_a8_linear_act(q, scale, s["qw1"], s["b1"], act="gelu")
+    q, scale = clq.clq_rotate_quant_act8(h, s["block"])
     return clq.clq_a8_linear_act(q, scale, s["qw2"], s["b2"], gate=s["g"], residual=stream, dtype=stream.dtype)
 
 
