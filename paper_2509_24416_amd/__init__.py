@@ -616,7 +616,10 @@ def clq_weight8_bytes(N, K):
 
 def clq_rotate_quant_act8(X, block, perm=None, out=None, scale_out=None, stream=None):
     """clq_rotate_quant_act with 8-bit codes (x_scale = max|x~| / 127).
-    Returns (Xq8 uint8 [clq_act8_bytes(M, K)], x_scale fp32 [M])."""
+    Returns (Xq8 uint8 [clq_act8_bytes(M, K)], x_scale fp32 [M]).  bf16 and fp32
+    activations go to clq_quantize_act8."""
+    if isinstance(X, torch.Tensor) and X.dtype in (torch.bfloat16, torch.float32):
+        return clq_quantize_act8(X, block, perm, out, scale_out, stream)
     _dev(X, "X", torch.float16)
     if X.dim() != 2 or X.stride(1) != 1:
         raise ValueError("X must be 2-D [M, K] with unit column stride")

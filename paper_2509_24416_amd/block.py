@@ -47,6 +47,7 @@ _POSITIONS = {torch.int32: 0, torch.float32: 1}
 _F64, _F32, _U8 = (torch.float64,), (torch.float32,), (torch.uint8,)
 _NONE, _NO_RESIDUAL = (None, 0, 1), (None, 0, 0)
 _ACTS = {None: 0, "none": 0, "gelu": 1, "silu": 3}
+_WIDEST = 16384   # columns of the norm's rows and of those that are quantized from 32 bits
 
 
 def _flat_bytes(t):
@@ -184,7 +185,7 @@ def _sum(residual, sum_out, M, K, device):
 
 def _codes(M, K, device, out, scale_out, reads, where):
     """Buffers of 8-bit codes and their scales: the caller's, checked against what the call reads, or new ones."""
-    if not 0 < M < 2147483648 or not 64 <= K <= 16384 or K & 63:
+    if not 0 < M < 2147483648 or not 64 <= K <= _WIDEST or K & 63:
         raise ClqError(CLQ_ERR_SHAPE, where)
     n = (M + 31) // 32 * 32 * K
     if out is None:
@@ -384,11 +385,20 @@ def clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, we
     return Y
 
 
+def _result_type(act, N):
+    """Of a result whose caller names none.  Activated values go to the next linear's quantizer: rounded to 16 bits
+    ahead of it their codes part from the formula's next to a border (an MLP of 8192 x 1152 -> 4608 -> 1152 is
+    then 4.3 to 4.8e-4 off its definition instead of 3.0e-4).  Rows that the quantizer takes in 16 bits only stay
+    16 bits."""
+    return torch.float32 if act not in (None, "none") and N <= _WIDEST else torch.float16
+
+
 def clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual=None, dtype=None, out=None, stream=None):
     """clq_a8_linear with an epilogue: Y = residual + gate * act(X . W^T + bias), fp32 throughout and rounded
     once.  act: None, "gelu" (tanh form) or "silu".  gate: [N], or [samples, N] for rows of that many equal
-    samples.  residual: of Y's type [M, N].  dtype: of Y (by default that of `out`, of the residual, or fp16).
-    out: where, the residual itself included."""
+    samples.  residual: of Y's type [M, N].  dtype: of Y; by default that of `out` or of the residual, else fp32
+    behind an activation (what clq_rotate_quant_act8 takes unrounded: N <= 16384) and fp16 otherwise.  out: where,
+    the residual itself included."""
     N, K, bits, wq, ws, device = qw.N, qw.K, qw.bits, qw.wq, qw.w_scale, Xq8.device
     M = _rows8(Xq8, x_scale, K)
     if bits not in (4, 8):
@@ -410,7 +420,8 @@ def clq_a8_linear_act(Xq8, x_scale, qw, bias=None, act=None, gate=None, residual
         b = bias.data_ptr()
     g, gt, samples = _modulation(gate, "gate", N, M, device)
     if dtype is None:
-        dtype = out.dtype if out is not None else residual.dtype if residual is not None else torch.float16
+        given = out if out is not None else residual
+        dtype = given.dtype if given is not None else _result_type(act, N)
     r, ldr = None, 0
     if residual is not None:
         rows, columns, ldr = _rows2d(residual, "residual", (dtype,))
