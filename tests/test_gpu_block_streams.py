@@ -66,8 +66,9 @@ def cases(clq, g):
 @pytest.mark.parametrize("name", ["norm", "norm8", "quantize", "dequantize", "rope", "linear", "linear, typed",
                                   "norm, typed by its buffer"])
 def test_a_call_runs_on_its_stream(clq, name, given):
-    """The inputs get their values on the stream, behind a millisecond of other work: a call on the current stream
-    would read what they held before."""
+    """The inputs get their values on the stream, behind some milliseconds of other work: a call on the current
+    stream would read what they held before.  (Streams share a few hardware queues, and one that shares the current
+    stream's would wait all the same: neighbours do not both.)"""
     changes, call = cases(clq, gen(21))[name]
     first = [t.clone() for t in call(given)]
     kept = [(t, t.clone()) for t, _ in changes]
@@ -75,22 +76,23 @@ def test_a_call_runs_on_its_stream(clq, name, given):
         t.copy_(new)
     want = [t.clone() for t in call(given)]
     assert any(not torch.equal(a, b) for a, b in zip(first, want))
-    for t, old in kept:
-        t.copy_(old)
     busy = torch.zeros(4096, 4096, dtype=F16, device="cuda")
-    other = torch.cuda.Stream()
-    torch.cuda.synchronize()
-    with torch.cuda.stream(other):
-        for _ in range(12):
-            busy @ busy
-        for t, new in changes:
-            t.copy_(new)
-    got = call(given, stream=other)
-    other.synchronize()
-    torch.cuda.synchronize()
-    assert len(got) == len(want)
-    for a, b in zip(got, want):
-        assert a.dtype is b.dtype and torch.equal(a, b)
+    product = torch.empty_like(busy)
+    for other in (torch.cuda.Stream(), torch.cuda.Stream()):
+        for t, old in kept:
+            t.copy_(old)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            for _ in range(60):
+                torch.mm(busy, busy, out=product)
+            for t, new in changes:
+                t.copy_(new)
+        got = call(given, stream=other)
+        other.synchronize()
+        torch.cuda.synchronize()
+        assert len(got) == len(want)
+        for a, b in zip(got, want):
+            assert a.dtype is b.dtype and torch.equal(a, b)
 
 
 def test_two_streams_at_once(clq):
