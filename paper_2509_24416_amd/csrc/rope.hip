@@ -2,9 +2,10 @@
 // pair i of a head, (a, b) -> (a cos - b sin, b cos + a sin) at the angle
 // position[row, axis(i)] * freq[i].
 //
-// Angles are formed in fp64 as revolutions and reduced there (position * freq / 2 pi less its nearest
-// whole number), so that far positions lose nothing; sine and cosine then take an fp32 argument of half
-// a revolution at most.
+// Angles are formed as revolutions, position * freq / 2 pi, each of the two products as the sum of two fp64 numbers
+// (rounded once to fp64, 2^31 positions on, an angle is off by 2e-7, as much as 4 fp32 roundings of its sine), and
+// reduced there (less their nearest whole number), so that far positions are as exact as near ones; sine and cosine
+// then take an fp32 argument of half a revolution at most.
 //
 // What bounds it is memory (every value read and written once), and on few heads the sines, which a row's heads
 // share.  So a lane owns the same piece of every head that it works on, an item: eight columns (interleaved
@@ -99,7 +100,11 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeLaunch a)
         const int64_t at = (int64_t)(row % (uint32_t)a.tokens) * a.axes + axis;
         const double p = a.float_positions ? (double)static_cast<const float *>(a.positions)[at]
                                            : (double)static_cast<const int32_t *>(a.positions)[at];
-        double rev = p * a.freqs[i] * 0.15915494309189535;
+        // 1 / 2 pi = 0x1.45f306dc9c883p-3 + kLow, |kLow| under half a step of it
+        constexpr double kTurns = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;
+        const double f = a.freqs[i], angle = p * f, rest = __builtin_fma(p, f, -angle);
+        const double high = angle * kTurns;
+        double rev = high - rint(high) + __builtin_fma(angle, kLow, __builtin_fma(rest, kTurns, __builtin_fma(angle, kTurns, -high)));
         rev -= rint(rev);
         float2 t;
         sincospif(2.0f * (float)rev, &t.y, &t.x);
