@@ -35,8 +35,10 @@ extern "C" {
  *   sum      out, s rounded to R's type, row stride ld_sum; may be R, in place.  The norm is that of s
  *            before this rounding.
  * A row that holds a NaN or an infinity gives NaN where s / infinity is one and, in the 8-bit form, a
- * NaN scale.  Squares are summed in fp32: of values past 2^62 they overflow.  In the 8-bit form rows whose
- * rotated s W stays under 2^-119 are zeros. */
+ * NaN scale.  Squares are summed in fp32: a row whose sum of them reaches 2^128 (a root mean square of
+ * 2^64 / sqrt(K), 2^61 at K = 64 and 2^57 at K = 16384) counts as infinitely large: zeros, in the 8-bit form
+ * codes with a scale of 0, or a NaN one where its rotation passes fp32's range too.  In the 8-bit form rows
+ * whose rotated s W stays under 2^-119 are zeros. */
 
 /* Y = n in fp16, bf16 or fp32, row stride ldy; may be X, in place.  8 <= K <= 16384, K % 8 == 0. */
 clq_status clq_rms_norm(const void *X, clq_type x_type, int64_t ldx, const void *R, clq_type r_type, int64_t ldr,
@@ -77,7 +79,8 @@ clq_status clq_dequantize_act8(const void *Xq8, const float *x_scale, int64_t M,
  *   interleaved  1: pair i is columns 2i, 2i + 1; 0: columns i, i + P.
  *   inverse  1: by the opposite angle (the transpose).
  *   W        NULL, or fp16, bf16 or fp32 weights of an RMS norm of each head (all D columns) ahead of the
- *            turn, [D] (weight_heads 1) or [heads][D] (weight_heads = heads), contiguous; eps as for the norm.
+ *            turn, [D] (weight_heads 1) or [heads][D] (weight_heads = heads), contiguous; eps as for the norm, and
+ *            so its limit: a head whose squares add up to 2^128 is zeros.
  *   Y        out, X's type, strides ldy and lhy, no value of it in two places of the head's rows; may be X,
  *            in place. */
 clq_status clq_rope_axes(const void *X, clq_type type, int64_t ldx, int64_t lhx, const void *positions,

@@ -147,7 +147,8 @@ def clq_rms_norm(X, weight=None, residual=None, eps=1e-6, dtype=None, out=None, 
     """Y = s / sqrt(mean(s^2) + eps) * weight with s = X + residual, per row.  X: fp16, bf16 or fp32 [M, K], any
     row stride that is a multiple of 8.  weight: [K], or [samples, K] for rows of that many equal samples.
     residual: fp16, bf16 or fp32 [M, K]; the sum comes back too, in its type (sum_out: where, the residual
-    itself included).  dtype: of Y (X's by default).  out: where, X itself included."""
+    itself included).  dtype: of Y (X's by default).  out: where, X itself included.  Squares are summed in
+    fp32: rows whose sum of them reaches 2^128 come out as zeros."""
     M, K, ldx, xt, device, w, r = _norm_operands(X, weight, residual, sum_out)
     i = device.index
     if stream is not None or _current_device() != i:
