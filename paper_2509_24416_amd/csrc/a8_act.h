@@ -17,6 +17,7 @@ namespace {
 
 template <class C, class E>
 hipError_t launch_act_split(tg::Args a, hipStream_t stream) {
+    if (!tg::stage_each<C>(a)) return hipErrorInvalidValue;
     a.tiles_m = (int)tg::tile_count(a.M, C::BM);
     a.tiles_n = (int)tg::tile_count(a.N, C::BN);
     hipLaunchKernelGGL((tg::split_gemm_kernel<C, false, false, true, E>), dim3((unsigned)(a.tiles_m * a.tiles_n)),
@@ -57,7 +58,7 @@ hipError_t launch_act_shape(const tg::Args &a, hipStream_t stream) {
     using E = ActEpi<A, T>;
     const int64_t c = compute_units(), M = a.M, N = a.N;
     if (tg::tile_count(M, 32) * tg::tile_count(N, 32) <= 2 * c) return launch_act_rows<F, A, T>(a, stream);
-    if (tg::tile_count(M, 64) * tg::tile_count(N, 128) <= 2 * c && (a.K >> 6) >= tg::SplitCfg<F, 4>::KS)
+    if (tg::tile_count(M, 64) * tg::tile_count(N, 128) <= 2 * c && tg::stage_each<tg::SplitCfg<F, 4>>(a))
         return launch_act_split<tg::SplitCfg<F, 4>, E>(a, stream);
     const int64_t t128 = tg::tile_count(M, 256) * tg::tile_count(N, 128), t96 = tg::tile_count(M, 256) * tg::tile_count(N, 96);
     if ((t96 + c - 1) / c <= (t128 + c - 1) / c) return launch_act_direct<F, 4, 3, E>(a, stream);

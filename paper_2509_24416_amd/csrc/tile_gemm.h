@@ -790,8 +790,13 @@ __global__ void __launch_bounds__(C::NT, 2) split_gemm_kernel(Args a)
 // (token and channel counts reach 2^31 - 1)
 inline int64_t tile_count(int64_t rows, int64_t tile) { return (rows + tile - 1) / tile; }
 
+// Every wave of a split has a stage of the k loop (one without would read the stage before the first).
+template <class C>
+inline bool stage_each(const Args &a) { return (a.K >> 6) >= C::KS; }
+
 template <class C>
 hipError_t launch_split(Args a, bool i32out, bool ragged, hipStream_t stream) {
+    if (!stage_each<C>(a)) return hipErrorInvalidValue;
     a.tiles_m = (int)tile_count(a.M, C::BM);
     a.tiles_n = (int)tile_count(a.N, C::BN);
     const dim3 grid((unsigned)(a.tiles_m * a.tiles_n)), block(C::NT);
