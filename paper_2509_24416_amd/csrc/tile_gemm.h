@@ -636,7 +636,6 @@ struct SplitCfg {
     static constexpr int KS = KS_, NT = KS * 64, BN = 128, BM = 64;
     static constexpr int WU = FmtInfo<F>::WU, XU = FmtInfo<F>::XU;
     static constexpr int kDepth = F == Fmt::W8A8 || F == Fmt::F6 ? 2 : 3;
-    static constexpr int EPN = 2 * BN + BM;
     static_assert(KS == 2 || KS == 4, "recursive halving over 8 fragments");
 };
 
