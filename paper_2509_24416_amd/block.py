@@ -332,6 +332,17 @@ def _head_bytes(X, M, H, D, ld, lh):
     return X.data_ptr(), H, lh * size, ((M - 1) * ld + D) * size
 
 
+def _heads_meet(at, M, ld, H, lh, D):
+    """Whether two sets of M rows of H heads of one spacing meet, the second `at` behind the first."""
+    (n, outer), (m, inner) = ((M, ld), (H, lh)) if ld >= lh else ((H, lh), (M, ld))
+    span = (m - 1) * inner + D
+    for i in range(max(1 - n, (-at - span) // outer + 1), min(n - 1, (span - 1 - at) // outer) + 1):
+        j = max(1 - m, -((at + i * outer + D - 1) // inner))   # the first whose end lies behind the other's start
+        if j < m and at + i * outer + j * inner < D:
+            return True
+    return False
+
+
 def clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, weight=None, eps=1e-6, out=None,
                   stream=None):
     """Turns the first sum(axes) columns of each head by its row's position on each axis.  X: fp16 or bf16
@@ -375,7 +386,10 @@ def clq_rope_axes(X, positions, freqs, axes, interleaved=True, inverse=False, we
             raise ValueError(f"out must be [{M}, {H}, {D}]")
         _together(device, "out", out)
         Y, at = out, _head_bytes(out, M, H, D, ldy, lhy)
-        if not (_in_place(Y, X, ldy, ldx) and lhy == lhx):
+        if ldy == ldx >= D and lhy == lhx >= D:   # (others are refused by the call)
+            if not _in_place(Y, X, ldy, ldx) and _heads_meet((Y.data_ptr() - X.data_ptr()) // 2, M, ldx, H, lhx, D):
+                raise ValueError("the output overlaps an input")
+        else:
             _apart(at, _head_bytes(X, M, H, D, ldx, lhx))
         _apart(at, _flat_bytes(positions), _flat_bytes(freqs), *(() if weight is None else (_flat_bytes(weight),)))
     status = _lib.clq_rope_axes(X.data_ptr(), _TYPES[X.dtype], ldx, lhx, positions.data_ptr(), _POSITIONS[pt], tokens,
