@@ -52,7 +52,9 @@ hipError_t launch_act_rows(tg::Args a, hipStream_t stream) {
 //                            of 128 (8192 x 4608 -> 1152: 384 and 288 of them, two a unit, 51.8 / 57.8; 4096 x 1152 ->
 //                            4608: 768 and 576, three a unit, 36.0 / 37.4; 12000 x 4608 -> 1152: 564 and 423, 77.5 /
 //                            65.8; 6144: 288 and 216, 48.0 / 38.4; 8192 x 1152 -> 4608: 1536 and 1152, 63.6 / 61.7).
-// Tiles of 128 tokens and the k loop over two waves won nowhere by more than 3%.
+// Tiles of 128 tokens and the k loop over two waves won nowhere by more than 3%.  4-bit weights, residuals and fp32
+// results go by the same lines, which were not measured with them; with the k loop over four waves the epilogue spills 64
+// registers, 124 to 144 for fp32 results.
 template <tg::Fmt F, Act8 A, MxType T>
 hipError_t launch_act_shape(const tg::Args &a, hipStream_t stream) {
     using E = ActEpi<A, T>;

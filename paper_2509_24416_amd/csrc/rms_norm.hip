@@ -17,7 +17,9 @@
 // Measured (a copy reaches 5.2 to 5.7 TB/s): 43200 x 1152 with a 16-bit residual to 8 bits 67 to 75 us (4.6 to 5.2
 // TB/s), with an fp32 one 105 (5.2), without one 40 (3.7: vector instructions); plain with residual 77 (5.2); 8192 x 4608
 // plain with residual 53 (5.7); 3000 x 12288 57 (5.2), to 8 bits 65 (3.9: two chunks a lane), gathered 76; fp32 rows of 43200 x
-// 1152 quantized 45 (5.6).
+// 1152 quantized 45 (5.6).  Samples whose rows are no multiple of four: 43204 x 1152 in two plain with residual
+// 111 us (two samples of 21600 rows 76), to 8 bits 114 (67), without a residual 67 (38): weights are read for each row, and
+// registers spill.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -87,7 +89,9 @@ __device__ __forceinline__ void store_codes8(const float (&x)[4][8], const float
 
 enum class Res { None, F16, BF16, F32 };
 
-// Waves a SIMD that the registers are held to (what each form needs by itself, or a few less).
+// Waves a SIMD that the registers are held to: what the forms of one sample with a chunk a lane need by themselves or a few
+// less (4 of 57 spill, one register mostly, 10 at most).  It does not look at MIXED, whose forms spill up to 29 registers
+// with one chunk a lane and 32 to 101 with two; of one sample and two chunks those to 8 bits spill 8 to 22.
 template <int B, MxType XT, Res RT, bool NORM, int NCH>
 constexpr int waves_per_simd() {
     if (NCH == 2) return 4;   // (a workgroup of 16 waves)
